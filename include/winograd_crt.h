@@ -46,7 +46,9 @@
 extern "C" {
 #endif
 
-typedef enum { WG_F32 = 0, WG_F16 = 1, WG_BF16 = 2 } wg_dtype;
+/* WG_E4M3: 8 bits, 4 of exponent and 3 of mantissa, largest value 448; only as
+ * the 8-bit rows of the sequence operators below. */
+typedef enum { WG_F32 = 0, WG_F16 = 1, WG_BF16 = 2, WG_E4M3 = 3 } wg_dtype;
 
 typedef enum {
     WG_OK = 0,
@@ -377,6 +379,159 @@ wg_status winograd_direct_conv_f64(wg_dtype dtype, const wg_tensor* x, const wg_
  * aligned) also holds the per-block partial sums.  Asynchronous on stream. */
 wg_status winograd_sq_error_sums(wg_dtype dtype, const void* y, const double* ref, int64_t n, double* sums,
                                  hipStream_t stream);
+
+/* ---- Sequence operators ----------------------------------------------------
+ * What stands around winograd_conv1d in a sequence model: a gated linear
+ * recurrence, a root-mean-square norm and products with 4-bit weights.  All of
+ * them are asynchronous on stream, allocate nothing, and launch nothing when
+ * they return an error.  Sums, states and statistics are held in fp32; results
+ * are rounded once to their type.  Outputs must not overlap inputs, unless said
+ * otherwise. */
+
+/* Rows of C contiguous channels of a tensor [N][L][C] in a storage dtype, at
+ * data + n * stride_n + l * stride_l (strides in elements, not negative): slices
+ * of wider rows and inputs with stride 0 are fine; rows of an output must not
+ * overlap.  data is aligned to its elements. */
+typedef struct {
+    const void* data;
+    int64_t stride_n, stride_l;
+} wg_rows;
+
+/* Steps between two of the states that winograd_gated_scan keeps for its
+ * backward pass. */
+#define WG_SCAN_BLOCK 32
+
+/* The gated linear recurrence, per sequence n and channel c:
+ *   f = sigmoid(gate), h[l] = f h[l-1] + (1 - f) value[l], h[-1] = h0 (or 0)
+ *   y[l] = h[l], times out_gate sigmoid(out_gate) if out_gate.data is not NULL.
+ * gate, value, out_gate and y are [N][L][C] in dtype.  lengths (NULL: every
+ * sequence has L steps; values are clipped to [0, L]): steps from lengths[n] on
+ * are padding; nothing there is used, y is 0 and the state stays.  h0 (NULL:
+ * zeros), h_last (the state after the last step) [N][C] fp32 and lengths [N] are
+ * contiguous.  states (NULL: not wanted): fp32 [N][ceil(L / WG_SCAN_BLOCK)][C],
+ * the state ahead of each block of steps, for the backward pass.  workspace: of
+ * winograd_gated_scan_workspace bytes, 16-byte aligned (NULL if that is 0).
+ * N, C >= 1, L >= 0. */
+typedef struct {
+    int64_t dtype, N, L, C;
+    wg_rows gate, value, out_gate, y;
+    const float* h0;
+    const int32_t* lengths;
+    float* h_last;
+    float* states;
+    void* workspace;
+    int64_t workspace_bytes;
+} wg_gated_scan;
+wg_status winograd_gated_scan(const wg_gated_scan* args, hipStream_t stream);
+
+/* Its gradients, from dy [N][L][C] and dh_last (fp32 [N][C], NULL: zeros):
+ * dgate, dvalue and, with out_gate, dout_gate [N][L][C] in dtype (0 at padding)
+ * and dh0 fp32 [N][C] (NULL: not wanted).  gate, value, out_gate and lengths are
+ * the forward call's, states are those it kept.  The states within a block are
+ * recomputed from gate and value in fp32. */
+typedef struct {
+    int64_t dtype, N, L, C;
+    wg_rows dy, gate, value, out_gate, dgate, dvalue, dout_gate;
+    const float* states;
+    const float* dh_last;
+    const int32_t* lengths;
+    float* dh0;
+    void* workspace;
+    int64_t workspace_bytes;
+} wg_gated_scan_backward;
+wg_status winograd_gated_scan_backward(const wg_gated_scan_backward* args, hipStream_t stream);
+
+/* Bytes of workspace that the scan (backward = 0) or its gradients (1) need. */
+wg_status winograd_gated_scan_workspace(wg_dtype dtype, int64_t N, int64_t L, int64_t C, int backward, size_t* bytes);
+
+/* One step of the recurrence for N sequences: gate, value, out_gate and y are
+ * [N][C] (stride_l is not used), h and h_new contiguous fp32 [N][C] states ahead of
+ * and after the step; h_new may be h. */
+typedef struct {
+    int64_t dtype, N, C;
+    wg_rows gate, value, out_gate, y;
+    const float* h;
+    float* h_new;
+} wg_gated_step;
+wg_status winograd_gated_step(const wg_gated_step* args, hipStream_t stream);
+
+/* The root-mean-square norm of every row of C channels, with the residual's
+ * addition:  r = x + residual,  y = r / sqrt(mean(r^2) + eps) * weight.
+ * x, residual (data NULL: none) and r (data NULL: not wanted) are [N][L][C] in
+ * dtype, weight [C] in dtype.  r is rounded as it is stored, y is computed from
+ * the unrounded sum.  y_dtype: dtype, or WG_E4M3 for 8 bits with scales:
+ *   s = max(max |y|, 2^-100) / 448 of each group of `group` channels (32, 64 or
+ *   128; 0: the whole row; the last group may be short), y = e4m3(y / s),
+ * scales fp32 [N][L][ceil(C / group)] (one a row for group 0), contiguous.
+ * r may be x or residual itself (the same rows).  N, L >= 0, C >= 1. */
+typedef struct {
+    int64_t dtype, N, L, C;
+    wg_rows x, residual, r, y;
+    const void* weight;
+    float* scales;
+    double eps;
+    int64_t y_dtype, group;
+} wg_rms_norm;
+wg_status winograd_rms_norm(const wg_rms_norm* args, hipStream_t stream);
+
+/* Its gradients at the rows r that were normalised (the forward's r, or x where
+ * there was no residual), with dr (data NULL: none), the gradient that reaches r
+ * from elsewhere: dx [N][L][C] in dtype, the gradient of r, and so of both x and
+ * the residual; dweight fp32 [C], summed in a fixed order.  workspace: of
+ * winograd_rms_norm_workspace bytes, 16-byte aligned.  dx may be dy or dr itself. */
+typedef struct {
+    int64_t dtype, N, L, C;
+    wg_rows dy, r, dr, dx;
+    const void* weight;
+    float* dweight;
+    double eps;
+    void* workspace;
+    int64_t workspace_bytes;
+} wg_rms_norm_backward;
+wg_status winograd_rms_norm_backward(const wg_rms_norm_backward* args, hipStream_t stream);
+wg_status winograd_rms_norm_workspace(wg_dtype dtype, int64_t N, int64_t L, int64_t C, size_t* bytes);
+
+/* A matrix of R rows and K columns in 4 bits with group scales:
+ *   w[j][k] = (code[j][k] - 8) * scale[j][k / group],  code 0 .. 15.
+ * codes: 32-bit words [ceil(R/16)][ceil(K/128)][4][16][4], 16-byte aligned: of the
+ * tile of rows 16 a .. and columns 128 b .., word [q][i][s] holds row 16 a + i,
+ * columns 128 b + 32 s + 8 q + j for j = 0 .. 7, code j at bit 4 (j / 2) of the
+ * lower (j even) or upper (j odd) half, the word then rotated left by 3 bits.
+ * Codes of padding rows and columns are 8.  scales: bf16
+ * [ceil(R/16)][ceil(K/group)][16], 0 for padding rows.  group: 32, 64 or 128. */
+typedef struct {
+    const void* codes;
+    const void* scales;
+    int64_t rows, cols, group;
+} wg_w4;
+
+/* y[m][j] = sum_k x[m][k] w[j][k] for the M rows of x [M][K] in x_dtype: M row
+ * vectors (sums in fp32; the weights' codes enter exactly).  For x in WG_E4M3
+ * x_scales is fp32 [M][G] (contiguous), G = 1 (a scale a row) or ceil(K/group)
+ * with the weights' group; NULL otherwise.  y [M][R] in y_dtype (WG_F32, WG_F16,
+ * WG_BF16).  x and y rows start ldx and ldy elements apart. */
+typedef struct {
+    wg_w4 w;
+    int64_t M, x_dtype, y_dtype;
+    const void* x;
+    int64_t ldx;
+    const float* x_scales;
+    int64_t x_groups;
+    void* y;
+    int64_t ldy;
+} wg_matvec_w4;
+wg_status winograd_matvec_w4(const wg_matvec_w4* args, hipStream_t stream);
+
+/* Codes and scales of a matrix m [rows][cols] (dtype, rows ldm elements apart)
+ * by rounding to the nearest: scale = bf16 of the group's max |m| / 7, codes
+ * round(m / scale) + 8 (a group of zeros has scale 0 and codes 8). */
+wg_status winograd_quantize_w4(const wg_w4* w, wg_dtype dtype, const void* m, int64_t ldm, hipStream_t stream);
+/* Codes and scales from a matrix of codes in plain order: nibbles [rows]
+ * [ceil(cols/2)] bytes, the even column in the lower half, and scales bf16
+ * [rows][ceil(cols/group)]. */
+wg_status winograd_pack_w4(const wg_w4* w, const void* nibbles, const void* scales, hipStream_t stream);
+/* The matrix m [rows][cols] (dtype, rows ldm elements apart) that w stands for. */
+wg_status winograd_dequantize_w4(const wg_w4* w, wg_dtype dtype, void* m, int64_t ldm, hipStream_t stream);
 
 /* Message describing the last error of the calling thread ("" if none). */
 const char* winograd_last_error(void);

@@ -110,6 +110,19 @@ def lib():
         "winograd_direct_conv_f64": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(WgTensor),
                                                     ctypes.POINTER(WgTensor), P, P]),
         "winograd_sq_error_sums": (ctypes.c_int, [ctypes.c_int, P, P, i64, P, P]),
+        # the sequence operators' argument structures come packed in one buffer
+        "winograd_gated_scan": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_gated_scan_backward": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_gated_scan_workspace": (ctypes.c_int, [ctypes.c_int, i64, i64, i64, ctypes.c_int,
+                                                         ctypes.POINTER(sz)]),
+        "winograd_gated_step": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_rms_norm": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_rms_norm_backward": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_rms_norm_workspace": (ctypes.c_int, [ctypes.c_int, i64, i64, i64, ctypes.POINTER(sz)]),
+        "winograd_matvec_w4": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_quantize_w4": (ctypes.c_int, [ctypes.c_char_p, ctypes.c_int, P, i64, P]),
+        "winograd_pack_w4": (ctypes.c_int, [ctypes.c_char_p, P, P, P]),
+        "winograd_dequantize_w4": (ctypes.c_int, [ctypes.c_char_p, ctypes.c_int, P, i64, P]),
         "winograd_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sigs.items():

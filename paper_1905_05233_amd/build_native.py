@@ -41,6 +41,10 @@ UNITS = [
     ("layer_ops.hip", DEVICE, "layer_ops.o"),
     ("conv1d.hip", DEVICE, "conv1d.o"),
     ("contract_pairwise.hip", DEVICE, "contract_pairwise.o"),
+    ("sequence_api.hip", DEVICE, "sequence_api.o"),
+    ("gated_scan.hip", DEVICE, "gated_scan.o"),
+    ("rms_norm.hip", DEVICE, "rms_norm.o"),
+    ("matvec_w4.hip", DEVICE, "matvec_w4.o"),
 ]
 
 

@@ -16,6 +16,7 @@
 
 #include "kernels.hpp"
 #include "plan.hpp"
+#include "status.hpp"
 #include "winograd_crt.h"
 
 // Workspace of winograd_conv2d_static (U, V and M of one layer), one copy per
@@ -37,9 +38,9 @@ struct wg_plan_s {
     wg::OutputTable otab{};
 };
 
-namespace {
+namespace wg {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 wg_status fail(wg_status s, const std::string& msg) {
     g_last_error = msg;
@@ -50,6 +51,13 @@ wg_status from_hip(hipError_t e, const char* what) {
     if (e == hipSuccess) return WG_OK;
     return fail(WG_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+}  // namespace wg
+
+using wg::fail;
+using wg::from_hip;
+
+namespace {
 
 template <typename F>
 wg_status guarded(F&& f) {
@@ -869,6 +877,6 @@ wg_status winograd_sq_error_sums(wg_dtype dtype, const void* y, const double* re
     return from_hip(e, "error sums");
 }
 
-const char* winograd_last_error(void) { return g_last_error.c_str(); }
+const char* winograd_last_error(void) { return wg::g_last_error.c_str(); }
 
 }  // extern "C"
