@@ -28,6 +28,7 @@
 
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "rows.hpp"
 #include "sequence.hpp"
 
 namespace wg {
@@ -37,30 +38,6 @@ namespace {
 constexpr int kStepThreads = 256;
 constexpr int kScanBlock = WG_SCAN_BLOCK;
 constexpr int kScanChannels = 32;   // channels of a workgroup
-
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-// 16 bytes at any element's address: the hardware takes such accesses whole
-struct __attribute__((packed, aligned(2))) Bytes16 {
-    u32x4 v;
-};
-
-template <typename Elem> struct Vec {
-    static constexpr int V = 16 / sizeof(Elem);
-    static __device__ __forceinline__ void widen(const u32x4& b, float (&f)[V]) {
-        const auto e = __builtin_bit_cast(Packed, b);
-#pragma unroll
-        for (int q = 0; q < V; ++q) f[q] = Storage<Elem>::to_f32(e.v[q]);
-    }
-    static __device__ __forceinline__ u32x4 narrow(const float (&f)[V]) {
-        Packed e;
-#pragma unroll
-        for (int q = 0; q < V; ++q) e.v[q] = Storage<Elem>::from_f32(f[q]);
-        return __builtin_bit_cast(u32x4, e);
-    }
-    struct Packed {
-        Elem v[V];
-    };
-};
 
 // sigmoid(z) and sigmoid(-z), both to fp32 accuracy for any z (1 - f would lose
 // the small one): with e = exp(-z) they are 1 / (1 + e) and e / (1 + e), which is 1
@@ -132,18 +109,6 @@ __device__ __forceinline__ void load_steps(const Elem* row, int64_t sl, int32_t 
                 if (j < valid) e.v[j] = q[j];
             raw[k] = __builtin_bit_cast(u32x4, e);
         }
-    }
-}
-
-template <typename Elem, bool FULL>
-__device__ __forceinline__ void store_run(Elem* p, int valid, const u32x4& bits) {
-    if (FULL || valid == Vec<Elem>::V) {
-        reinterpret_cast<Bytes16*>(p)->v = bits;
-    } else {
-        const auto e = __builtin_bit_cast(typename Vec<Elem>::Packed, bits);
-#pragma unroll
-        for (int j = 0; j < Vec<Elem>::V; ++j)
-            if (j < valid) p[j] = e.v[j];
     }
 }
 
