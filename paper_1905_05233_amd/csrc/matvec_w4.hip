@@ -8,6 +8,7 @@
 
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "rows.hpp"
 #include "sequence.hpp"
 
 namespace wg {
@@ -45,37 +46,213 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
     return static_cast<int>(v >> (4 * (j / 2) + 16 * (j % 2)) & 15u);
 }
 
-template <int D> struct XTypeOf { using type = typename DTypeOf<D>::type; };
-template <> struct XTypeOf<3> { using type = uint8_t; };
-template <typename T> __device__ __forceinline__ float x_value(T v) {
-    if constexpr (sizeof(T) == 1) return __builtin_amdgcn_cvt_f32_fp8(v, 0);
-    else return Storage<T>::to_f32(v);
+// The product on the matrix cores.  A wave multiplies RT tiles of 16 rows of the
+// matrix with up to 16 rows of x (v_mfma_f32_16x16x32: 32 columns an instruction);
+// a lane's 16 bytes of a tile of 128 columns are its fragments for four of them.
+//
+// A code becomes a 16-bit float without arithmetic: four bits at bit 3 of the
+// fraction of a number whose ones there count 1 (16 in bf16, 128 in fp16), so that
+// a word gives its eight weights, plus 16 or 128, in seven and/or/shift
+// instructions.  What was added, and the codes' 8, leaves through the accumulator,
+// which starts each group from another product, of a constant matrix (-24 or -136)
+// with the same x: shared by the RT tiles, and exact up to the accumulator's fp32.
+// The group's sum times its scale goes to the running fp32 sum of the output.
+//
+// Rows of x in fp32 are cut into three bf16 parts of 8 bits each, which hold all 24
+// bits; fp8 becomes bf16 exactly.
+//
+// The waves of a workgroup take the tiles of columns in turn, each wave's next
+// tiles in flight, and their sums are added in a fixed order at the end; how many
+// waves depends on the matrix alone, so that an output does not depend on the
+// other rows of x.
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+constexpr int kTokens = 16;     // rows of x that a wave takes
+constexpr int kAhead = 4;       // tiles of columns in flight
+
+template <bool F16> __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, const f32x4& c) {
+    if constexpr (F16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                       0);
 }
 
-// One wave per output; lanes take words of eight columns.
-template <int XD, int YD>
-__global__ __launch_bounds__(kW4Threads) void matvec_kernel(W4 w, int64_t M, const void* xp, int64_t ldx,
-                                                            const float* xs, int64_t x_groups, void* yp, int64_t ldy) {
+// The eight codes of a word as 16-bit floats, plus 16 (bf16) or 128 (fp16).
+template <bool F16> __device__ __forceinline__ u32x4 widen_codes(uint32_t w) {
+    constexpr uint32_t kMask = 0x00780078u, kOne = F16 ? 0x58005800u : 0x41804180u;
+    return u32x4{(w & kMask) | kOne, (w >> 4 & kMask) | kOne, (w >> 8 & kMask) | kOne,
+                 (__builtin_amdgcn_alignbit(w, w, 12) & kMask) | kOne};
+}
+// What must go again: -24 in bf16, -136 in fp16.
+template <bool F16> constexpr uint32_t kOffset = F16 ? 0xd840d840u : 0xc1c0c1c0u;
+
+template <int D> struct XTypeOf { using type = typename DTypeOf<D>::type; };
+template <> struct XTypeOf<3> { using type = uint8_t; };
+
+// Eight columns of a row of x as 16-bit parts: one, or three for fp32.
+template <int XD> constexpr int kPlanes = XD == 0 ? 3 : 1;
+
+__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+
+template <int XD>
+__device__ __forceinline__ void load_x(const typename XTypeOf<XD>::type* p, int valid, u32x4 (&planes)[kPlanes<XD>]) {
     using X = typename XTypeOf<XD>::type;
-    using Y = typename DTypeOf<YD>::type;
-    const int lane = threadIdx.x % 64;
-    const int64_t waves = static_cast<int64_t>(gridDim.x) * (kW4Threads / 64);
-    for (int64_t id = static_cast<int64_t>(blockIdx.x) * (kW4Threads / 64) + threadIdx.x / 64; id < M * w.rows; id += waves) {
-        const int64_t m = id / w.rows, j = id % w.rows;
-        const X* x = static_cast<const X*>(xp) + m * ldx;
-        float sum = 0.0f;
-        for (int64_t c = lane * 8; c < w.cols; c += 64 * 8) {
-            const uint32_t word = w.codes[word_at(w, j, c)];
-            const int64_t g = c / w.group;
-            float part = 0.0f;
-            for (int e = 0; e < 8 && c + e < w.cols; ++e)
-                part = fmaf(static_cast<float>(code_of(word, e) - 8), x_value(x[c + e]), part);
-            float s = Storage<bf16_t>::to_f32(w.scales[scale_at(w, j, g)]);
-            if (XD == 3) s *= xs[m * x_groups + (x_groups == 1 ? 0 : g)];
-            sum = fmaf(s, part, sum);
+    struct __attribute__((packed, aligned(1))) Run { X v[8]; } run;
+    if (valid >= 8) {
+        run = *reinterpret_cast<const Run*>(p);
+    } else {
+        run = Run{};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < valid) run.v[j] = p[j];
+    }
+    if constexpr (XD == 1 || XD == 2) {
+        planes[0] = __builtin_bit_cast(u32x4, run);
+    } else if constexpr (XD == 3) {
+        const u32x2 b = __builtin_bit_cast(u32x2, run);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(b[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b[h], true);
+            planes[0][2 * h] = upper_halves(__float_as_uint(lo[0]), __float_as_uint(lo[1]));
+            planes[0][2 * h + 1] = upper_halves(__float_as_uint(hi[0]), __float_as_uint(hi[1]));
         }
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) (static_cast<Y*>(yp) + m * ldy)[j] = Storage<Y>::from_f32(sum);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float f0 = run.v[2 * j], f1 = run.v[2 * j + 1];
+#pragma unroll
+            for (int part = 0; part < 3; ++part) {
+                const uint32_t b0 = __float_as_uint(f0), b1 = __float_as_uint(f1);
+                planes[part][j] = upper_halves(b0, b1);
+                f0 -= __uint_as_float(b0 & 0xffff0000u);
+                f1 -= __uint_as_float(b1 & 0xffff0000u);
+            }
+        }
+    }
+}
+
+struct MatvecArgs {
+    W4 w;
+    int64_t M;
+    const void* x;
+    int64_t ldx;
+    const float* x_scales;
+    int64_t x_groups;
+    void* y;
+    int64_t ldy;
+    int y_dtype;
+};
+
+// GPT: groups of a tile of 128 columns; XG: x's scales go by groups.
+template <int XD, int GPT, int RT, bool XG>
+__global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
+    using X = typename XTypeOf<XD>::type;
+    constexpr bool F16 = XD == 1;
+    constexpr int SPG = 4 / GPT;   // instructions of a group
+    extern __shared__ float sums[];   // [wave][RT][lane][4]
+    const W4& w = a.w;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    const int quarter = lane / 16;
+    const int64_t row_tiles = (w.rows + 15) / 16, rt0 = static_cast<int64_t>(blockIdx.x) * RT;
+    const int64_t token = static_cast<int64_t>(blockIdx.y) * kTokens + lane % 16;
+    const bool live = token < a.M;
+    const int ktiles = static_cast<int>(w.ktiles);
+
+    const u32x4* codes[RT];
+    const u32x2* scales[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {   // tiles past the last one repeat it
+        const int64_t rt = min(rt0 + t, row_tiles - 1);
+        codes[t] = reinterpret_cast<const u32x4*>(w.codes) + rt * w.ktiles * 64 + lane;
+        scales[t] = reinterpret_cast<const u32x2*>(w.scales + rt * w.groups * 16) + quarter;
+    }
+    const X* x = static_cast<const X*>(a.x) + (live ? token : 0) * a.ldx;
+    const float* xs = XG ? a.x_scales + (live ? token : 0) * a.x_groups : nullptr;
+
+    f32x4 acc[RT];
+    u32x4 buf[kAhead][RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int p = 0; p < kAhead; ++p)
+        if (wave + p * waves < ktiles)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) buf[p][t] = codes[t][static_cast<int64_t>(wave + p * waves) * 64];
+    for (int k0 = wave; k0 < ktiles; k0 += kAhead * waves) {
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) {
+            const int kt = k0 + p * waves;
+            if (kt >= ktiles) break;
+            u32x4 cur[RT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) cur[t] = buf[p][t];
+            const int next = kt + kAhead * waves;
+            if (next < ktiles)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) buf[p][t] = codes[t][static_cast<int64_t>(next) * 64];
+            u32x4 xp[4][kPlanes<XD>];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int64_t c = static_cast<int64_t>(kt) * 128 + 32 * s + 8 * quarter;
+                const int64_t left = live ? w.cols - c : 0;
+                if (left > 0) {
+                    load_x<XD>(x + c, left < 8 ? static_cast<int>(left) : 8, xp[s]);
+                } else {
+#pragma unroll
+                    for (int part = 0; part < kPlanes<XD>; ++part) xp[s][part] = u32x4{0, 0, 0, 0};
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < GPT; ++g) {
+                // groups past the matrix's last one have no columns
+                const int64_t group = min(static_cast<int64_t>(kt) * GPT + g, w.groups - 1);
+                f32x4 start{0, 0, 0, 0};
+                const u32x4 offset{kOffset<F16>, kOffset<F16>, kOffset<F16>, kOffset<F16>};
+#pragma unroll
+                for (int s = g * SPG; s < (g + 1) * SPG; ++s)
+#pragma unroll
+                    for (int part = 0; part < kPlanes<XD>; ++part) start = mma<F16>(offset, xp[s][part], start);
+                float by = 1.0f;
+                if (XG) by = xs[group];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const u32x2 sc = scales[t][group * 4];
+                    f32x4 sum = start;
+#pragma unroll
+                    for (int s = g * SPG; s < (g + 1) * SPG; ++s) {
+                        const u32x4 frag = widen_codes<F16>(cur[t][s]);
+#pragma unroll
+                        for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(frag, xp[s][part], sum);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float f = __uint_as_float(i % 2 ? sc[i / 2] & 0xffff0000u : sc[i / 2] << 16);
+                        if (XG) f *= by;
+                        acc[t][i] = fmaf(f, sum[i], acc[t][i]);
+                    }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+        *reinterpret_cast<f32x4*>(sums + ((wave * RT + t) * 64 + lane) * 4) = acc[t];
+    __syncthreads();
+    // an output a thread: [tile][quarter][row of x][row in the quarter]
+    for (int id = threadIdx.x; id < RT * 256; id += blockDim.x) {
+        const int64_t j = (rt0 + id / 256) * 16 + id % 256 / 64 * 4 + id % 4;
+        const int64_t m = static_cast<int64_t>(blockIdx.y) * kTokens + id % 64 / 4;
+        if (m >= a.M || j >= w.rows) continue;
+        float s = 0.0f;
+        for (int k = 0; k < waves; ++k) s += sums[k * RT * 256 + id];
+        if (XD == 3 && !XG) s *= a.x_scales[m];
+        const int64_t at = m * a.ldy + j;
+        if (a.y_dtype == 0) static_cast<float*>(a.y)[at] = s;
+        else if (a.y_dtype == 1) static_cast<_Float16*>(a.y)[at] = Storage<_Float16>::from_f32(s);
+        else static_cast<bf16_t*>(a.y)[at] = Storage<bf16_t>::from_f32(s);
     }
 }
 
@@ -144,25 +321,35 @@ hipError_t blocks_for(int64_t threads, unsigned* blocks) {
     return hipSuccess;
 }
 
-template <int XD, int YD> hipError_t matvec_t(const wg_matvec_w4& a, hipStream_t stream) {
-    const int64_t waves = a.M * a.w.rows, blocks = (waves + kW4Threads / 64 - 1) / (kW4Threads / 64);
-    matvec_kernel<XD, YD><<<static_cast<unsigned>(blocks < 65536 ? blocks : 65536), kW4Threads, 0, stream>>>(
-        w4_of(a.w), a.M, a.x, a.ldx, a.x_scales, a.x_groups, a.y, a.ldy);
+template <int XD, int GPT, int RT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hipStream_t stream) {
+    const int64_t row_tiles = (k.w.rows + 15) / 16, x = (row_tiles + RT - 1) / RT, y = (k.M + kTokens - 1) / kTokens;
+    const int waves = k.w.ktiles >= 16 ? 16 : k.w.ktiles >= 8 ? 8 : 4;
+    if (x * waves * 64 > 0xffffffffLL || y > 0xffff) return hipErrorInvalidValue;
+    matvec_kernel<XD, GPT, RT, XG><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), waves * 64,
+                                     waves * RT * 256 * sizeof(float), stream>>>(k);
     return hipGetLastError();
 }
-template <int XD> hipError_t matvec_x(const wg_matvec_w4& a, hipStream_t stream) {
-    return a.y_dtype == WG_F32 ? matvec_t<XD, 0>(a, stream)
-                               : a.y_dtype == WG_F16 ? matvec_t<XD, 1>(a, stream) : matvec_t<XD, 2>(a, stream);
+// Tiles of rows a wave: x is read once for all of them, which counts the more the
+// more rows x has.
+template <int XD, int GPT, bool XG> hipError_t matvec_rt(const MatvecArgs& k, hipStream_t stream) {
+    if (k.M <= 2) return matvec_t<XD, GPT, 1, XG>(k, stream);
+    return matvec_t<XD, GPT, 2, XG>(k, stream);
+}
+template <int XD, bool XG> hipError_t matvec_x(const MatvecArgs& k, hipStream_t stream) {
+    return k.w.group == 32 ? matvec_rt<XD, 4, XG>(k, stream)
+                           : k.w.group == 64 ? matvec_rt<XD, 2, XG>(k, stream) : matvec_rt<XD, 1, XG>(k, stream);
 }
 
 }  // namespace
 
 hipError_t launch_matvec_w4(const wg_matvec_w4& a, hipStream_t stream) {
+    const MatvecArgs k{w4_of(a.w), a.M, a.x, a.ldx, a.x_scales, a.x_groups, a.y, a.ldy, static_cast<int>(a.y_dtype)};
     switch (a.x_dtype) {
-        case WG_F32: return matvec_x<0>(a, stream);
-        case WG_F16: return matvec_x<1>(a, stream);
-        case WG_BF16: return matvec_x<2>(a, stream);
-        default: return matvec_x<3>(a, stream);
+        case WG_F32: return matvec_x<0, false>(k, stream);
+        case WG_F16: return matvec_x<1, false>(k, stream);
+        case WG_BF16: return matvec_x<2, false>(k, stream);
+        // one group: its scale is the row's
+        default: return a.x_groups > 1 ? matvec_x<3, true>(k, stream) : matvec_x<3, false>(k, stream);
     }
 }
 
