@@ -89,6 +89,13 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
     return (m < kFp8Least ? kFp8Least : m) / kFp8Max;
 }
 
+template <typename Elem> __device__ __forceinline__ u32x4 load_one(const Elem* p, const RunShape& shape, int C) {
+    u32x4 bits[1];
+    const Elem* const at[1] = {p};
+    load_runs<Elem, false, 1>(at, shape, C, bits);
+    return bits[0];
+}
+
 // Reductions over a row's TPR threads; above a wave through LDS, by all threads of
 // the workgroup, which then holds one row.  `slot` alternates between calls, so
 // that one barrier a call is enough.
@@ -129,13 +136,13 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
     __shared__ float lds[4][16];
     const int lane = threadIdx.x % TPR;
     const int C = static_cast<int>(a.C);
-    int valid[NV];
+    RunShape shape[NV];
     float w[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int c = (j * TPR + lane) * V;
-        valid[j] = min(V, max(0, C - c));
-        Vec<Elem>::widen(load_run(a.weight + c, valid[j]), w[j]);
+        shape[j] = run_shape<Elem>(c, C);
+        Vec<Elem>::widen(load_one(a.weight + c, shape[j], C), w[j]);
     }
     int slot = 0;
     for (int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR; row < a.rows;
@@ -144,11 +151,11 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
         float r[NV][V];
         u32x4 raw[NV], raw2[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) raw[j] = load_run(x + (j * TPR + lane) * V, valid[j]);
+        for (int j = 0; j < NV; ++j) raw[j] = load_one(x + (j * TPR + lane) * V, shape[j], C);
         if (a.residual.data) {
             const Elem* res = row_at<const Elem>(a.residual, a.index, row);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) raw2[j] = load_run(res + (j * TPR + lane) * V, valid[j]);
+            for (int j = 0; j < NV; ++j) raw2[j] = load_one(res + (j * TPR + lane) * V, shape[j], C);
         }
         float ss = 0.0f;
 #pragma unroll
@@ -167,7 +174,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
             Elem* out = row_at<Elem>(a.r, a.index, row);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                if (valid[j]) store_run<Elem, false>(out + (j * TPR + lane) * V, valid[j], Vec<Elem>::narrow(r[j]));
+                if (shape[j].valid) store_run<Elem, false>(out + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(r[j]));
         }
         ss = RowReduce<TPR>::sum(ss, lds, slot);
         const float rstd = 1.0f / sqrtf(ss / static_cast<float>(C) + a.eps);
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
             Elem* y = row_at<Elem>(a.y, a.index, row);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                if (valid[j]) store_run<Elem, false>(y + (j * TPR + lane) * V, valid[j], Vec<Elem>::narrow(r[j]));
+                if (shape[j].valid) store_run<Elem, false>(y + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(r[j]));
         } else {
             uint32_t top[NV];
 #pragma unroll
@@ -188,7 +195,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
 #pragma unroll
                 for (int q = 0; q < V; ++q) {   // channels past the row's end hold zeros
                     const uint32_t v = __float_as_uint(r[j][q]) & 0x7fffffffu;
-                    top[j] = q < valid[j] && v > top[j] ? v : top[j];
+                    top[j] = q < shape[j].valid && v > top[j] ? v : top[j];
                 }
             }
             uint8_t* y = row_at<uint8_t>(a.y, a.index, row);
@@ -203,7 +210,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
                 for (int j = 0; j < NV; ++j) {
 #pragma unroll
                     for (int q = 0; q < V; ++q) r[j][q] *= inv;
-                    if (valid[j]) store_e4m3<V>(y + (j * TPR + lane) * V, valid[j], r[j]);
+                    if (shape[j].valid) store_e4m3<V>(y + (j * TPR + lane) * V, shape[j].valid, r[j]);
                 }
             } else {
                 // a group is 4 to 32 adjacent threads, all of a row's waves' own
@@ -217,10 +224,10 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
                     if (per > 16) o = other_half<32>(m), m = o > m ? o : m;
                     const float scale = scale_of(m), inv = 1.0f / scale;
                     const int c = (j * TPR + lane) * V;
-                    if (lane % per == 0 && valid[j]) a.scales[row * groups + c / static_cast<int>(a.group)] = scale;
+                    if (lane % per == 0 && shape[j].valid) a.scales[row * groups + c / static_cast<int>(a.group)] = scale;
 #pragma unroll
                     for (int q = 0; q < V; ++q) r[j][q] *= inv;
-                    if (valid[j]) store_e4m3<V>(y + c, valid[j], r[j]);
+                    if (shape[j].valid) store_e4m3<V>(y + c, shape[j].valid, r[j]);
                 }
             }
         }
@@ -302,13 +309,13 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
     __shared__ float share[ROWS > 1 ? ROWS * TPR * NV * V : 1];
     const int lane = threadIdx.x % TPR;
     const int C = static_cast<int>(a.C);
-    int valid[NV];
+    RunShape shape[NV];
     float w[NV][V], dw[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int c = (j * TPR + lane) * V;
-        valid[j] = min(V, max(0, C - c));
-        Vec<Elem>::widen(load_run(a.weight + c, valid[j]), w[j]);
+        shape[j] = run_shape<Elem>(c, C);
+        Vec<Elem>::widen(load_one(a.weight + c, shape[j], C), w[j]);
 #pragma unroll
         for (int q = 0; q < V; ++q) dw[j][q] = 0.0f;
     }
@@ -319,13 +326,13 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
         const Elem* dp = row_at<const Elem>(a.dy, a.index, row);
         u32x4 rr[NV], dd[NV], ee[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) rr[j] = load_run(rp + (j * TPR + lane) * V, valid[j]);
+        for (int j = 0; j < NV; ++j) rr[j] = load_one(rp + (j * TPR + lane) * V, shape[j], C);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) dd[j] = load_run(dp + (j * TPR + lane) * V, valid[j]);
+        for (int j = 0; j < NV; ++j) dd[j] = load_one(dp + (j * TPR + lane) * V, shape[j], C);
         if (a.dr.data) {
             const Elem* ep = row_at<const Elem>(a.dr, a.index, row);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) ee[j] = load_run(ep + (j * TPR + lane) * V, valid[j]);
+            for (int j = 0; j < NV; ++j) ee[j] = load_one(ep + (j * TPR + lane) * V, shape[j], C);
         }
         float r[NV][V], d[NV][V];
         float ss = 0.0f, gr = 0.0f;
@@ -354,7 +361,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
                 o[q] = rstd * (d[j][q] * w[j][q] - r[j][q] * mean);
                 if (a.dr.data) o[q] += e[q];
             }
-            if (valid[j]) store_run<Elem, false>(out + (j * TPR + lane) * V, valid[j], Vec<Elem>::narrow(o));
+            if (shape[j].valid) store_run<Elem, false>(out + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(o));
         }
     }
     float* part = a.partial + static_cast<int64_t>(blockIdx.x) * a.C;
@@ -363,7 +370,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int q = 0; q < V; ++q)
-                if (q < valid[j]) part[(j * TPR + lane) * V + q] = dw[j][q];
+                if (q < shape[j].valid) part[(j * TPR + lane) * V + q] = dw[j][q];
     } else {
         constexpr int W = TPR * NV * V;   // channels' room of a row
         const int mine = static_cast<int>(threadIdx.x) / TPR;

@@ -33,25 +33,76 @@ template <typename Elem> struct Vec {
     };
 };
 
+// A run of V channels from c0 of a row of C: how many it has, and how many too many
+// it would have (0 for a whole run).
+struct RunShape {
+    int valid, over;
+};
+template <typename Elem> __device__ __forceinline__ RunShape run_shape(int c0, int C) {
+    constexpr int V = Vec<Elem>::V;
+    return {max(0, min(V, C - c0)), max(0, c0 + V - C)};
+}
+
+// Without its first n elements, zeros behind.
+template <typename Elem> __device__ __forceinline__ u32x4 drop_first(const u32x4& b, int n) {
+    if (n >= Vec<Elem>::V) return u32x4{0, 0, 0, 0};
+    const uint64_t lo = static_cast<uint64_t>(b[1]) << 32 | b[0], hi = static_cast<uint64_t>(b[3]) << 32 | b[2];
+    const int s = n * 8 * static_cast<int>(sizeof(Elem));
+    const uint64_t l = s >= 64 ? hi >> (s - 64) : s > 0 ? lo >> s | hi << (64 - s) : lo;
+    const uint64_t h = s >= 64 ? 0 : hi >> s;
+    return u32x4{static_cast<uint32_t>(l), static_cast<uint32_t>(l >> 32), static_cast<uint32_t>(h),
+                 static_cast<uint32_t>(h >> 32)};
+}
+
+// Runs from p.  A short run is the end of its row: 16 bytes that end with the row
+// are loaded and shifted (rows of fewer than V channels are loaded one by one),
+// which takes the same load as the other lanes' whole runs.
+template <typename Elem, bool FULL, int S>
+__device__ __forceinline__ void load_runs(const Elem* const (&p)[S], const RunShape& r, int C, u32x4 (&raw)[S]) {
+    constexpr int V = Vec<Elem>::V;
+    if (FULL || C >= V) {
+#pragma unroll
+        for (int k = 0; k < S; ++k) raw[k] = reinterpret_cast<const Bytes16*>(p[k] - (FULL ? 0 : r.over))->v;
+        if (!FULL && r.over > 0) {
+#pragma unroll
+            for (int k = 0; k < S; ++k) raw[k] = drop_first<Elem>(raw[k], r.over);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+            typename Vec<Elem>::Packed e{};
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (j < r.valid) e.v[j] = p[k][j];
+            raw[k] = __builtin_bit_cast(u32x4, e);
+        }
+    }
+}
+
+// Stores a run, a short one in up to three pieces.
 template <typename Elem, bool FULL>
 __device__ __forceinline__ void store_run(Elem* p, int valid, const u32x4& bits) {
     if (FULL || valid == Vec<Elem>::V) {
         reinterpret_cast<Bytes16*>(p)->v = bits;
-    } else {
-        const auto e = __builtin_bit_cast(typename Vec<Elem>::Packed, bits);
-#pragma unroll
-        for (int j = 0; j < Vec<Elem>::V; ++j)
-            if (j < valid) p[j] = e.v[j];
+        return;
     }
-}
-
-template <typename Elem> __device__ __forceinline__ u32x4 load_run(const Elem* p, int valid) {
-    if (valid == Vec<Elem>::V) return reinterpret_cast<const Bytes16*>(p)->v;
-    typename Vec<Elem>::Packed e{};
-#pragma unroll
-    for (int j = 0; j < Vec<Elem>::V; ++j)
-        if (j < valid) e.v[j] = p[j];
-    return __builtin_bit_cast(u32x4, e);
+    constexpr int kPer8 = 8 / sizeof(Elem);
+    uint64_t w = static_cast<uint64_t>(bits[1]) << 32 | bits[0];
+    if (valid & kPer8) {
+        __builtin_memcpy(p, &w, 8);
+        p += kPer8;
+        w = static_cast<uint64_t>(bits[3]) << 32 | bits[2];
+    }
+    if (sizeof(Elem) == 4 ? valid & 1 : valid & 2) {
+        const uint32_t x = static_cast<uint32_t>(w);
+        __builtin_memcpy(p, &x, 4);
+        p += 4 / sizeof(Elem);
+        w >>= 32;
+    }
+    if (sizeof(Elem) == 2 && valid & 1) {
+        const uint16_t x = static_cast<uint16_t>(w);
+        __builtin_memcpy(p, &x, 2);
+    }
 }
 
 // The value of the lane whose number differs in bit N / 2 .. (N a power of two, 2 to
