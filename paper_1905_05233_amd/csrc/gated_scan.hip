@@ -40,7 +40,7 @@ constexpr int kHeld = 16;             // gates that a thread holds of a tile
 constexpr int kThreads = 512;
 constexpr int grad_threads(int lanes) { return lanes == 8 ? 256 : 512; }
 // Groups of channels that fill the chip, and workgroups that chunks make of fewer.
-constexpr int64_t kFull = 192, kChunked = 512, kMostChunks = 256;
+constexpr int64_t kFull = 192, kChunked = 512, kMostChunks = 256, kWalked = 4;
 // LANES: 16-byte runs of channels of a workgroup
 template <typename Elem, int LANES> constexpr int kChannels = LANES * (16 / static_cast<int>(sizeof(Elem)));
 
@@ -620,9 +620,10 @@ Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
     p.lanes = dtype == kF32 || p.split.columns >= 8 * kFull || p.split.columns < 4 * kFull ? 8 : 4;
     const int64_t groups = (p.split.columns + p.lanes - 1) / p.lanes;
     p.split.groups = static_cast<uint32_t>(std::min<int64_t>(groups, 0xffffffffLL));
-    const int64_t tile = (backward ? grad_threads(p.lanes) : kThreads) / (p.lanes * V) * kHeld, tiles = (L + tile - 1) / tile;
+    const int threads = backward ? grad_threads(p.lanes) : kThreads;
+    const int64_t tile = threads / (p.lanes * V) * kHeld, tiles = (L + tile - 1) / tile;
     int64_t chunks = 1;
-    if (groups < kFull && tiles >= 4) chunks = std::min<int64_t>({tiles, kChunked / groups, kMostChunks});
+    if (groups < kFull && tiles > kWalked) chunks = std::min<int64_t>({tiles, kChunked / groups, kMostChunks});
     const int64_t each = std::max<int64_t>(1, (tiles + chunks - 1) / chunks);
     p.split.tiles = static_cast<int32_t>(tiles);
     p.split.chunk = static_cast<int32_t>(each);

@@ -71,6 +71,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kTokens = 16;     // rows of x that a wave takes
 constexpr int kAhead = 4;       // tiles of columns in flight
+constexpr int64_t kTwoTiles = 8192;   // rows of the matrix from which a wave takes two tiles of them
 
 template <bool F16> __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, const f32x4& c) {
     if constexpr (F16)
@@ -97,11 +98,15 @@ template <int XD> constexpr int kPlanes = XD == 0 ? 3 : 1;
 
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 
-template <int XD>
+template <typename X> struct __attribute__((packed, aligned(1))) XRun {
+    X v[8];
+};
+template <int XD, bool WHOLE>
 __device__ __forceinline__ void load_x(const typename XTypeOf<XD>::type* p, int valid, u32x4 (&planes)[kPlanes<XD>]) {
     using X = typename XTypeOf<XD>::type;
-    struct __attribute__((packed, aligned(1))) Run { X v[8]; } run;
-    if (valid >= 8) {
+    using Run = XRun<X>;
+    Run run;
+    if (WHOLE || valid >= 8) {
         run = *reinterpret_cast<const Run*>(p);
     } else {
         run = Run{};
@@ -158,7 +163,6 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
     const int quarter = lane / 16;
     const int64_t row_tiles = (w.rows + 15) / 16, rt0 = static_cast<int64_t>(blockIdx.x) * RT;
     const int64_t token = static_cast<int64_t>(blockIdx.y) * kTokens + lane % 16;
-    const bool live = token < a.M;
     const int ktiles = static_cast<int>(w.ktiles);
 
     const u32x4* codes[RT];
@@ -169,8 +173,10 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
         codes[t] = reinterpret_cast<const u32x4*>(w.codes) + rt * w.ktiles * 64 + lane;
         scales[t] = reinterpret_cast<const u32x2*>(w.scales + rt * w.groups * 16) + quarter;
     }
-    const X* x = static_cast<const X*>(a.x) + (live ? token : 0) * a.ldx;
-    const float* xs = XG ? a.x_scales + (live ? token : 0) * a.x_groups : nullptr;
+    // past the last row of x the last one is taken again: outputs do not mix, and none is stored
+    const int64_t row = min(token, a.M - 1);
+    const X* x = static_cast<const X*>(a.x) + row * a.ldx + 8 * quarter;
+    const float* xs = XG ? a.x_scales + row * a.x_groups : nullptr;
 
     f32x4 acc[RT];
     u32x4 buf[kAhead][RT];
@@ -194,15 +200,15 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t) buf[p][t] = codes[t][static_cast<int64_t>(next) * 64];
             u32x4 xp[4][kPlanes<XD>];
+            const X* xk = x + static_cast<int64_t>(kt) * 128;
+            if (static_cast<int64_t>(kt) * 128 + 128 <= w.cols) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int64_t c = static_cast<int64_t>(kt) * 128 + 32 * s + 8 * quarter;
-                const int64_t left = live ? w.cols - c : 0;
-                if (left > 0) {
-                    load_x<XD>(x + c, left < 8 ? static_cast<int>(left) : 8, xp[s]);
-                } else {
+                for (int s = 0; s < 4; ++s) load_x<XD, true>(xk + 32 * s, 8, xp[s]);
+            } else {
 #pragma unroll
-                    for (int part = 0; part < kPlanes<XD>; ++part) xp[s][part] = u32x4{0, 0, 0, 0};
+                for (int s = 0; s < 4; ++s) {
+                    const int64_t left = w.cols - (static_cast<int64_t>(kt) * 128 + 32 * s + 8 * quarter);
+                    load_x<XD, false>(xk + 32 * s, left < 0 ? 0 : left < 8 ? static_cast<int>(left) : 8, xp[s]);
                 }
             }
 #pragma unroll
@@ -323,16 +329,16 @@ hipError_t blocks_for(int64_t threads, unsigned* blocks) {
 
 template <int XD, int GPT, int RT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hipStream_t stream) {
     const int64_t row_tiles = (k.w.rows + 15) / 16, x = (row_tiles + RT - 1) / RT, y = (k.M + kTokens - 1) / kTokens;
-    const int waves = k.w.ktiles >= 16 ? 16 : k.w.ktiles >= 8 ? 8 : 4;
+    const int waves = static_cast<int>(k.w.ktiles < 16 ? k.w.ktiles : 16);
     if (x * waves * 64 > 0xffffffffLL || y > 0xffff) return hipErrorInvalidValue;
     matvec_kernel<XD, GPT, RT, XG><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), waves * 64,
                                      waves * RT * 256 * sizeof(float), stream>>>(k);
     return hipGetLastError();
 }
-// Tiles of rows a wave: x is read once for all of them, which counts the more the
-// more rows x has.
+// Tiles of rows a wave: x is read once for all of them, which pays where enough
+// tiles remain for every compute unit.
 template <int XD, int GPT, bool XG> hipError_t matvec_rt(const MatvecArgs& k, hipStream_t stream) {
-    if (k.M <= 2) return matvec_t<XD, GPT, 1, XG>(k, stream);
+    if (k.M <= 2 || k.w.rows < kTwoTiles) return matvec_t<XD, GPT, 1, XG>(k, stream);
     return matvec_t<XD, GPT, 2, XG>(k, stream);
 }
 template <int XD, bool XG> hipError_t matvec_x(const MatvecArgs& k, hipStream_t stream) {

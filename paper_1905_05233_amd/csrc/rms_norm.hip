@@ -89,10 +89,11 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
     return (m < kFp8Least ? kFp8Least : m) / kFp8Max;
 }
 
-template <typename Elem> __device__ __forceinline__ u32x4 load_one(const Elem* p, const RunShape& shape, int C) {
-    u32x4 bits[1];
+// FULL: the row's channels are whole runs.
+template <typename Elem, bool FULL> __device__ __forceinline__ u32x4 load_one(const Elem* p, const RunShape& shape, int C) {
+    u32x4 bits[1]{};
     const Elem* const at[1] = {p};
-    load_runs<Elem, false, 1>(at, shape, C, bits);
+    if (!FULL || shape.valid) load_runs<Elem, FULL, 1>(at, shape, C, bits);
     return bits[0];
 }
 
@@ -130,7 +131,7 @@ template <int TPR> struct RowReduce {
 
 constexpr int block_of(int tpr) { return tpr > kNormThreads ? tpr : kNormThreads; }
 
-template <typename Elem, int TPR, int NV, bool QUANT>
+template <typename Elem, int TPR, int NV, bool FULL, bool QUANT>
 __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
     constexpr int V = Vec<Elem>::V, ROWS = block_of(TPR) / TPR;
     __shared__ float lds[4][16];
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
     for (int j = 0; j < NV; ++j) {
         const int c = (j * TPR + lane) * V;
         shape[j] = run_shape<Elem>(c, C);
-        Vec<Elem>::widen(load_one(a.weight + c, shape[j], C), w[j]);
+        Vec<Elem>::widen(load_one<Elem, FULL>(a.weight + c, shape[j], C), w[j]);
     }
     int slot = 0;
     for (int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR; row < a.rows;
@@ -151,11 +152,11 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
         float r[NV][V];
         u32x4 raw[NV], raw2[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) raw[j] = load_one(x + (j * TPR + lane) * V, shape[j], C);
+        for (int j = 0; j < NV; ++j) raw[j] = load_one<Elem, FULL>(x + (j * TPR + lane) * V, shape[j], C);
         if (a.residual.data) {
             const Elem* res = row_at<const Elem>(a.residual, a.index, row);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) raw2[j] = load_one(res + (j * TPR + lane) * V, shape[j], C);
+            for (int j = 0; j < NV; ++j) raw2[j] = load_one<Elem, FULL>(res + (j * TPR + lane) * V, shape[j], C);
         }
         float ss = 0.0f;
 #pragma unroll
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
             Elem* out = row_at<Elem>(a.r, a.index, row);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                if (shape[j].valid) store_run<Elem, false>(out + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(r[j]));
+                if (shape[j].valid) store_run<Elem, FULL>(out + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(r[j]));
         }
         ss = RowReduce<TPR>::sum(ss, lds, slot);
         const float rstd = 1.0f / sqrtf(ss / static_cast<float>(C) + a.eps);
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
             Elem* y = row_at<Elem>(a.y, a.index, row);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                if (shape[j].valid) store_run<Elem, false>(y + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(r[j]));
+                if (shape[j].valid) store_run<Elem, FULL>(y + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(r[j]));
         } else {
             uint32_t top[NV];
 #pragma unroll
@@ -302,7 +303,7 @@ template <typename Elem> struct NormGradArgs {
     float* rstd;      // of long rows, one a row
 };
 
-template <typename Elem, int TPR, int NV>
+template <typename Elem, int TPR, int NV, bool FULL>
 __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<Elem> a) {
     constexpr int V = Vec<Elem>::V, ROWS = block_of(TPR) / TPR;
     __shared__ float lds[4][16];
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
     for (int j = 0; j < NV; ++j) {
         const int c = (j * TPR + lane) * V;
         shape[j] = run_shape<Elem>(c, C);
-        Vec<Elem>::widen(load_one(a.weight + c, shape[j], C), w[j]);
+        Vec<Elem>::widen(load_one<Elem, FULL>(a.weight + c, shape[j], C), w[j]);
 #pragma unroll
         for (int q = 0; q < V; ++q) dw[j][q] = 0.0f;
     }
@@ -326,13 +327,13 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
         const Elem* dp = row_at<const Elem>(a.dy, a.index, row);
         u32x4 rr[NV], dd[NV], ee[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) rr[j] = load_one(rp + (j * TPR + lane) * V, shape[j], C);
+        for (int j = 0; j < NV; ++j) rr[j] = load_one<Elem, FULL>(rp + (j * TPR + lane) * V, shape[j], C);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) dd[j] = load_one(dp + (j * TPR + lane) * V, shape[j], C);
+        for (int j = 0; j < NV; ++j) dd[j] = load_one<Elem, FULL>(dp + (j * TPR + lane) * V, shape[j], C);
         if (a.dr.data) {
             const Elem* ep = row_at<const Elem>(a.dr, a.index, row);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) ee[j] = load_one(ep + (j * TPR + lane) * V, shape[j], C);
+            for (int j = 0; j < NV; ++j) ee[j] = load_one<Elem, FULL>(ep + (j * TPR + lane) * V, shape[j], C);
         }
         float r[NV][V], d[NV][V];
         float ss = 0.0f, gr = 0.0f;
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
                 o[q] = rstd * (d[j][q] * w[j][q] - r[j][q] * mean);
                 if (a.dr.data) o[q] += e[q];
             }
-            if (shape[j].valid) store_run<Elem, false>(out + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(o));
+            if (shape[j].valid) store_run<Elem, FULL>(out + (j * TPR + lane) * V, shape[j].valid, Vec<Elem>::narrow(o));
         }
     }
     float* part = a.partial + static_cast<int64_t>(blockIdx.x) * a.C;
@@ -388,19 +389,28 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
     }
 }
 
-// dweight from its parts: 32 channels a workgroup, the parts over 32 threads a channel.
+// dweight from its parts: 16 channels a workgroup, the parts over 64 threads a
+// channel, eight of them in flight (1024 parts of 512 channels: 3 us).
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* partial, int64_t parts, int64_t C, float* dweight) {
-    __shared__ float lds[32][33];
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.x % 32;
-    const int k = threadIdx.x / 32;
+    constexpr int kChannels = 16, kSlices = 64;
+    __shared__ float lds[kSlices][kChannels + 1];
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kChannels + threadIdx.x % kChannels;
+    const int k = threadIdx.x / kChannels;
     float s = 0.0f;
     if (c < C)
-        for (int64_t p = k; p < parts; p += 32) s += partial[p * C + c];
-    lds[k][threadIdx.x % 32] = s;
+        for (int64_t p = k; p < parts; p += 8 * kSlices) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = p + u * kSlices < parts ? partial[(p + u * kSlices) * C + c] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += v[u];
+        }
+    lds[k][threadIdx.x % kChannels] = s;
     __syncthreads();
-    s = lanes_sum<32>(lds[threadIdx.x % 32][k]);
-    const int64_t out = static_cast<int64_t>(blockIdx.x) * 32 + k;
-    if (threadIdx.x % 32 == 0 && out < C) dweight[out] = s;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;   // a wave a channel
+    s = lanes_sum<64>(lds[lane][wave]);
+    const int64_t out = static_cast<int64_t>(blockIdx.x) * kChannels + wave;
+    if (lane == 0 && out < C) dweight[out] = s;
 }
 
 // The gradients of rows of any length: 1 / sqrt of each row, dweight's parts by
@@ -503,13 +513,16 @@ template <int D> hipError_t launch_rms_norm_t(const wg_rms_norm& a, hipStream_t 
     const NormArgs<Elem> k{rows, a.C, index_of(a.N, a.L, a.x, a.residual, a.r, a.y), at(a.x), at(a.residual), at(a.r),
                            at(a.y), static_cast<const Elem*>(a.weight), a.scales, static_cast<float>(a.eps),
                            a.group && a.group < a.C ? a.group : a.C};
-    const bool quant = a.y_dtype == WG_E4M3;
+    const bool quant = a.y_dtype == WG_E4M3, full = a.C % Vec<Elem>::V == 0;
     const Shape s = shape_of(D, a.C);
     const unsigned blocks = static_cast<unsigned>(s.tpr ? walkers(rows, s.tpr, kNormPerCu) : std::min(rows, kLongBlocks));
 #define WG_NORM_CASE(TPR, NV)                                                                     \
     if (s.tpr == TPR && s.nv == NV) {                                                             \
-        if (quant) norm_kernel<Elem, TPR, NV, true><<<blocks, block_of(TPR), 0, stream>>>(k);     \
-        else norm_kernel<Elem, TPR, NV, false><<<blocks, block_of(TPR), 0, stream>>>(k);          \
+        const unsigned threads = block_of(TPR);                                                   \
+        if (full && quant) norm_kernel<Elem, TPR, NV, true, true><<<blocks, threads, 0, stream>>>(k);   \
+        else if (full) norm_kernel<Elem, TPR, NV, true, false><<<blocks, threads, 0, stream>>>(k);      \
+        else if (quant) norm_kernel<Elem, TPR, NV, false, true><<<blocks, threads, 0, stream>>>(k);     \
+        else norm_kernel<Elem, TPR, NV, false, false><<<blocks, threads, 0, stream>>>(k);         \
         return hipGetLastError();                                                                 \
     }
     WG_NORM_SHAPES(WG_NORM_CASE)
@@ -526,12 +539,15 @@ template <int D> hipError_t launch_rms_norm_backward_t(const wg_rms_norm_backwar
                          static_cast<const Elem*>(a.weight), a.dweight, static_cast<float>(a.eps),
                          static_cast<float*>(a.workspace), 0, nullptr};
     const Shape s = shape_of(D, a.C);
-    const unsigned column_blocks = static_cast<unsigned>((a.C + 31) / 32);
+    const unsigned column_blocks = static_cast<unsigned>((a.C + 15) / 16);
     if (s.tpr && rows > 0) {
         k.parts = walkers(rows, s.tpr, kGradPerCu);
         const unsigned blocks = static_cast<unsigned>(k.parts);
 #define WG_NORM_CASE(TPR, NV) \
-    if (s.tpr == TPR && s.nv == NV) norm_grad_kernel<Elem, TPR, NV><<<blocks, block_of(TPR), 0, stream>>>(k);
+    if (s.tpr == TPR && s.nv == NV) {                                                                             \
+        if (a.C % Vec<Elem>::V == 0) norm_grad_kernel<Elem, TPR, NV, true><<<blocks, block_of(TPR), 0, stream>>>(k); \
+        else norm_grad_kernel<Elem, TPR, NV, false><<<blocks, block_of(TPR), 0, stream>>>(k);                     \
+    }
         WG_NORM_SHAPES(WG_NORM_CASE)
 #undef WG_NORM_CASE
     } else if (rows > 0) {

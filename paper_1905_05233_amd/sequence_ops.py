@@ -71,18 +71,31 @@ def _check(t, name, shape, dtype, dev):
 
 def _rows(t, name, shape, dtype, dev):
     """(address, stride_n, stride_l) of [N][L][C], or of [L][C] as one sequence."""
-    _check(t, name, shape, dtype, dev)
-    s = t.stride()
-    if s[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{name}: the channels of a row must be contiguous")
-    return (t.data_ptr(), s[0], s[1]) if len(s) == 3 else (t.data_ptr(), 0, s[0])
+    try:
+        s = t.stride()
+        if t.dtype == dtype and t.shape == shape and t.get_device() == dev and (s[-1] == 1 or shape[-1] <= 1):
+            return (t.data_ptr(), s[0], s[1]) if len(s) == 3 else (t.data_ptr(), 0, s[0])
+    except AttributeError:
+        pass
+    _check(t, name, shape, dtype, dev)   # raises, or the strides are at fault
+    raise ValueError(f"{name}: the channels of a row must be contiguous")
 
 
 def _dense(t, name, shape, dtype, dev):
+    try:
+        if t.dtype == dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     _check(t, name, shape, dtype, dev)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _new(like, shape, dtype):
+    """A contiguous tensor on like's GPU, the quickest way that torch has."""
+    if like.dtype == dtype and like.shape == shape and like.is_contiguous():
+        return torch.empty_like(like)
+    return like.new_empty(shape, dtype=dtype)
 
 
 def _size(query, *args):
@@ -100,7 +113,7 @@ def _size(query, *args):
 
 
 def _workspace(need, like):
-    return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
+    return like.new_empty(need, dtype=torch.uint8) if need else None
 
 
 def _keep(stream, dev, *tensors):
@@ -127,14 +140,14 @@ def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_s
     o = _NO_ROWS if out_gate is None else _rows(out_gate, "out_gate", shape, dt, dev)
     own_y = y is None
     if own_y:
-        y = torch.empty(shape, dtype=dt, device=gate.device)
+        y = _new(gate, shape, dt)
     yr = _rows(y, "y", shape, dt, dev)
     h0p = 0 if h0 is None else _dense(h0, "h0", (Nn, C), torch.float32, dev)
     lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
-    h_last = torch.empty((Nn, C), dtype=torch.float32, device=gate.device)
+    h_last = _new(gate if h0 is None else h0, (Nn, C), torch.float32)
     states = None
     if save_states:
-        states = torch.empty((Nn, -(-L // SCAN_BLOCK), C), dtype=torch.float32, device=gate.device)
+        states = gate.new_empty((Nn, -(-L // SCAN_BLOCK), C), dtype=torch.float32)
     need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 0)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan(
@@ -167,13 +180,13 @@ def gated_scan_backward(dy, gate, value, states, out_gate=None, dh_last=None, le
     lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
     own = out is None
     if own:
-        out = [torch.empty(shape, dtype=dt, device=gate.device) for _ in range(2 if out_gate is None else 3)]
+        out = [_new(dy, shape, dt) for _ in range(2 if out_gate is None else 3)]
     elif len(out) != (2 if out_gate is None else 3):
         raise ValueError("out must hold dgate, dvalue and, with out_gate, dout_gate")
     rows = [_rows(t, name, shape, dt, dev) for t, name in zip(out, ("dgate", "dvalue", "dout_gate"))]
     if out_gate is None:
         rows.append(_NO_ROWS)
-    dh0 = torch.empty((Nn, C), dtype=torch.float32, device=gate.device)
+    dh0 = _new(gate if dh_last is None else dh_last, (Nn, C), torch.float32)
     need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 1)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan_backward(
@@ -200,9 +213,9 @@ def gated_step(gate, value, h, out_gate=None, h_new=None, y=None, stream=None):
     hp = _dense(h, "h", shape, torch.float32, dev)
     own_y, own_h = y is None, h_new is None
     if own_y:
-        y = torch.empty(shape, dtype=dt, device=gate.device)
+        y = _new(gate, shape, dt)
     if own_h:
-        h_new = torch.empty(shape, dtype=torch.float32, device=gate.device)
+        h_new = torch.empty_like(h)
     yr = _rows(y, "y", shape, dt, dev)
     hnp = _dense(h_new, "h_new", shape, torch.float32, dev)
     st = N.lib().winograd_gated_step(
@@ -228,7 +241,7 @@ def _norm(x, weight, residual, eps, out, r, quant, group, stream):
         rr = _rows(residual, "residual", shape, dt, dev)
         own_r = r is None
         if own_r:
-            r = torch.empty(shape, dtype=dt, device=x.device)
+            r = _new(x, shape, dt)
         sr = _rows(r, "r", shape, dt, dev)
     elif r is not None:
         raise ValueError("r is the sum with the residual: there is none")
@@ -236,11 +249,11 @@ def _norm(x, weight, residual, eps, out, r, quant, group, stream):
     odt = torch.float8_e4m3fn if quant else dt
     own = out is None
     if own:
-        out = torch.empty(shape, dtype=odt, device=x.device)
+        out = _new(x, shape, odt)
     yr = _rows(out, "y", shape, odt, dev)
     scales = None
     if quant:
-        scales = torch.empty((*shape[:-1], -(-C // group) if group > 0 else 1), dtype=torch.float32, device=x.device)
+        scales = x.new_empty((*shape[:-1], -(-C // group) if group > 0 else 1), dtype=torch.float32)
     st = N.lib().winograd_rms_norm(
         _pack_norm(code, Nn, L, C, *xr, *rr, *sr, *yr, wp, 0 if scales is None else scales.data_ptr(), eps,
                    _E4M3 if quant else code, group), _raw_stream(stream))
@@ -282,9 +295,9 @@ def rms_norm_backward(dy, r, weight, dr=None, eps=1e-6, dx=None, stream=None):
     wp = _dense(weight, "weight", (C,), dt, dev)
     own = dx is None
     if own:
-        dx = torch.empty(shape, dtype=dt, device=r.device)
+        dx = _new(dy, shape, dt)
     xr = _rows(dx, "dx", shape, dt, dev)
-    dweight = torch.empty((C,), dtype=torch.float32, device=r.device)
+    dweight = r.new_empty((C,), dtype=torch.float32)
     need = _size("winograd_rms_norm_workspace", code, Nn, L, C)
     ws = _workspace(need, r)
     st = N.lib().winograd_rms_norm_backward(
@@ -389,7 +402,7 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
     if own:
         if dtype is None:
             dtype = torch.bfloat16 if x8 else xdt
-        y = torch.empty((M, w.rows), dtype=dtype, device=x.device)
+        y = x.new_empty((M, w.rows), dtype=dtype)
     elif dtype is not None and dtype != y.dtype:
         raise TypeError("dtype is that of y")
     yp, _, ldy = _rows(y, "y", (M, w.rows), y.dtype, dev)
