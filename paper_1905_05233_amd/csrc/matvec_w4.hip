@@ -46,7 +46,7 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
     return static_cast<int>(v >> (4 * (j / 2) + 16 * (j % 2)) & 15u);
 }
 
-// The product on the matrix cores.  A wave multiplies RT tiles of 16 rows of the
+// The product on the matrix cores.  A workgroup multiplies a tile of 16 rows of the
 // matrix with up to 16 rows of x (v_mfma_f32_16x16x32: 32 columns an instruction);
 // a lane's 16 bytes of a tile of 128 columns are its fragments for four of them.
 //
@@ -55,14 +55,15 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
 // a word gives its eight weights, plus 16 or 128, in seven and/or/shift
 // instructions.  What was added, and the codes' 8, leaves through the accumulator,
 // which starts each group from another product, of a constant matrix (-24 or -136)
-// with the same x: shared by the RT tiles, and exact up to the accumulator's fp32.
+// with the same x, and so exactly up to the accumulator's fp32.
 // The group's sum times its scale goes to the running fp32 sum of the output.
 //
 // Rows of x in fp32 are cut into three bf16 parts of 8 bits each, which hold all 24
 // bits; fp8 becomes bf16 exactly.
 //
-// The waves of a workgroup take the tiles of columns in turn, each wave's next
-// tiles in flight, and their sums are added in a fixed order at the end; how many
+// The waves of a workgroup take the tiles of columns in turn, each wave's next tile
+// in flight (two or more ahead are no faster: 25088 -> 4096 14.2 us with one, 15.8
+// with two), and their sums are added in a fixed order at the end; how many
 // waves depends on the matrix alone, so that an output does not depend on the
 // other rows of x.
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -70,8 +71,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kTokens = 16;     // rows of x that a wave takes
-constexpr int kAhead = 4;       // tiles of columns in flight
-constexpr int64_t kTwoTiles = 8192;   // rows of the matrix from which a wave takes two tiles of them
 
 template <bool F16> __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, const f32x4& c) {
     if constexpr (F16)
@@ -101,19 +100,17 @@ __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { ret
 template <typename X> struct __attribute__((packed, aligned(1))) XRun {
     X v[8];
 };
-template <int XD, bool WHOLE>
-__device__ __forceinline__ void load_x(const typename XTypeOf<XD>::type* p, int valid, u32x4 (&planes)[kPlanes<XD>]) {
-    using X = typename XTypeOf<XD>::type;
-    using Run = XRun<X>;
-    Run run;
-    if (WHOLE || valid >= 8) {
-        run = *reinterpret_cast<const Run*>(p);
-    } else {
-        run = Run{};
+// Eight columns as they lie in memory, from p on; past the end of a row, zeros.
+template <typename X> __device__ __forceinline__ XRun<X> load_x(const X* p, int64_t valid) {
+    if (valid >= 8) return *reinterpret_cast<const XRun<X>*>(p);
+    XRun<X> run{};
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < valid) run.v[j] = p[j];
-    }
+    for (int j = 0; j < 8; ++j)
+        if (j < valid) run.v[j] = p[j];
+    return run;
+}
+template <int XD>
+__device__ __forceinline__ void widen_x(const XRun<typename XTypeOf<XD>::type>& run, u32x4 (&planes)[kPlanes<XD>]) {
     if constexpr (XD == 1 || XD == 2) {
         planes[0] = __builtin_bit_cast(u32x4, run);
     } else if constexpr (XD == 3) {
@@ -152,108 +149,84 @@ struct MatvecArgs {
 };
 
 // GPT: groups of a tile of 128 columns; XG: x's scales go by groups.
-template <int XD, int GPT, int RT, bool XG>
+template <int XD, int GPT, bool XG>
 __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
     using X = typename XTypeOf<XD>::type;
     constexpr bool F16 = XD == 1;
     constexpr int SPG = 4 / GPT;   // instructions of a group
-    extern __shared__ float sums[];   // [wave][RT][lane][4]
+    extern __shared__ float sums[];   // [wave][lane][4]
     const W4& w = a.w;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     const int quarter = lane / 16;
-    const int64_t row_tiles = (w.rows + 15) / 16, rt0 = static_cast<int64_t>(blockIdx.x) * RT;
-    const int64_t token = static_cast<int64_t>(blockIdx.y) * kTokens + lane % 16;
+    const int64_t rt = blockIdx.x;
     const int ktiles = static_cast<int>(w.ktiles);
-
-    const u32x4* codes[RT];
-    const u32x2* scales[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {   // tiles past the last one repeat it
-        const int64_t rt = min(rt0 + t, row_tiles - 1);
-        codes[t] = reinterpret_cast<const u32x4*>(w.codes) + rt * w.ktiles * 64 + lane;
-        scales[t] = reinterpret_cast<const u32x2*>(w.scales + rt * w.groups * 16) + quarter;
-    }
+    const u32x4* codes = reinterpret_cast<const u32x4*>(w.codes) + rt * w.ktiles * 64 + lane;
+    const u32x2* scales = reinterpret_cast<const u32x2*>(w.scales + rt * w.groups * 16) + quarter;
     // past the last row of x the last one is taken again: outputs do not mix, and none is stored
-    const int64_t row = min(token, a.M - 1);
+    const int64_t row = min(static_cast<int64_t>(blockIdx.y) * kTokens + lane % 16, a.M - 1);
     const X* x = static_cast<const X*>(a.x) + row * a.ldx + 8 * quarter;
     const float* xs = XG ? a.x_scales + row * a.x_groups : nullptr;
 
-    f32x4 acc[RT];
-    u32x4 buf[kAhead][RT];
+    struct Tile {
+        u32x4 codes;
+        XRun<X> x[4];
+    };
+    auto load = [&](int kt, Tile& tile) {
+        tile.codes = codes[static_cast<int64_t>(kt) * 64];
+        const X* xk = x + static_cast<int64_t>(kt) * 128;
+        const int64_t left = w.cols - static_cast<int64_t>(kt) * 128;
+        if (left >= 128) {
 #pragma unroll
-    for (int t = 0; t < RT; ++t) acc[t] = f32x4{0, 0, 0, 0};
+            for (int s = 0; s < 4; ++s) tile.x[s] = load_x(xk + 32 * s, 8);
+        } else {
 #pragma unroll
-    for (int p = 0; p < kAhead; ++p)
-        if (wave + p * waves < ktiles)
+            for (int s = 0; s < 4; ++s) tile.x[s] = load_x(xk + 32 * s, left - 32 * s - 8 * quarter);
+        }
+    };
+    f32x4 acc{0, 0, 0, 0};
+    Tile tile;
+    load(wave, tile);   // there are at least as many tiles as waves
+    for (int kt = wave; kt < ktiles; kt += waves) {
+        const u32x4 cur = tile.codes;
+        u32x4 xp[4][kPlanes<XD>];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) buf[p][t] = codes[t][static_cast<int64_t>(wave + p * waves) * 64];
-    for (int k0 = wave; k0 < ktiles; k0 += kAhead * waves) {
+        for (int s = 0; s < 4; ++s) widen_x<XD>(tile.x[s], xp[s]);
+        if (kt + waves < ktiles) load(kt + waves, tile);
 #pragma unroll
-        for (int p = 0; p < kAhead; ++p) {
-            const int kt = k0 + p * waves;
-            if (kt >= ktiles) break;
-            u32x4 cur[RT];
+        for (int g = 0; g < GPT; ++g) {
+            // groups past the matrix's last one have no columns
+            const int64_t group = min(static_cast<int64_t>(kt) * GPT + g, w.groups - 1);
+            const u32x2 sc = scales[group * 4];
+            const u32x4 offset{kOffset<F16>, kOffset<F16>, kOffset<F16>, kOffset<F16>};
+            f32x4 sum{0, 0, 0, 0};
 #pragma unroll
-            for (int t = 0; t < RT; ++t) cur[t] = buf[p][t];
-            const int next = kt + kAhead * waves;
-            if (next < ktiles)
+            for (int s = g * SPG; s < (g + 1) * SPG; ++s)
 #pragma unroll
-                for (int t = 0; t < RT; ++t) buf[p][t] = codes[t][static_cast<int64_t>(next) * 64];
-            u32x4 xp[4][kPlanes<XD>];
-            const X* xk = x + static_cast<int64_t>(kt) * 128;
-            if (static_cast<int64_t>(kt) * 128 + 128 <= w.cols) {
+                for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(offset, xp[s][part], sum);
 #pragma unroll
-                for (int s = 0; s < 4; ++s) load_x<XD, true>(xk + 32 * s, 8, xp[s]);
-            } else {
+            for (int s = g * SPG; s < (g + 1) * SPG; ++s) {
+                const u32x4 frag = widen_codes<F16>(cur[s]);
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int64_t left = w.cols - (static_cast<int64_t>(kt) * 128 + 32 * s + 8 * quarter);
-                    load_x<XD, false>(xk + 32 * s, left < 0 ? 0 : left < 8 ? static_cast<int>(left) : 8, xp[s]);
-                }
+                for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(frag, xp[s][part], sum);
             }
+            const float by = XG ? xs[group] : 1.0f;
 #pragma unroll
-            for (int g = 0; g < GPT; ++g) {
-                // groups past the matrix's last one have no columns
-                const int64_t group = min(static_cast<int64_t>(kt) * GPT + g, w.groups - 1);
-                f32x4 start{0, 0, 0, 0};
-                const u32x4 offset{kOffset<F16>, kOffset<F16>, kOffset<F16>, kOffset<F16>};
-#pragma unroll
-                for (int s = g * SPG; s < (g + 1) * SPG; ++s)
-#pragma unroll
-                    for (int part = 0; part < kPlanes<XD>; ++part) start = mma<F16>(offset, xp[s][part], start);
-                float by = 1.0f;
-                if (XG) by = xs[group];
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const u32x2 sc = scales[t][group * 4];
-                    f32x4 sum = start;
-#pragma unroll
-                    for (int s = g * SPG; s < (g + 1) * SPG; ++s) {
-                        const u32x4 frag = widen_codes<F16>(cur[t][s]);
-#pragma unroll
-                        for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(frag, xp[s][part], sum);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float f = __uint_as_float(i % 2 ? sc[i / 2] & 0xffff0000u : sc[i / 2] << 16);
-                        if (XG) f *= by;
-                        acc[t][i] = fmaf(f, sum[i], acc[t][i]);
-                    }
-                }
+            for (int i = 0; i < 4; ++i) {
+                float f = __uint_as_float(i % 2 ? sc[i / 2] & 0xffff0000u : sc[i / 2] << 16);
+                if (XG) f *= by;
+                acc[i] = fmaf(f, sum[i], acc[i]);
             }
         }
     }
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-        *reinterpret_cast<f32x4*>(sums + ((wave * RT + t) * 64 + lane) * 4) = acc[t];
+    *reinterpret_cast<f32x4*>(sums + (wave * 64 + lane) * 4) = acc;
     __syncthreads();
-    // an output a thread: [tile][quarter][row of x][row in the quarter]
-    for (int id = threadIdx.x; id < RT * 256; id += blockDim.x) {
-        const int64_t j = (rt0 + id / 256) * 16 + id % 256 / 64 * 4 + id % 4;
+    // an output a thread: [quarter][row of x][row in the quarter]
+    for (int id = threadIdx.x; id < 256; id += blockDim.x) {
+        const int64_t j = rt * 16 + id / 64 * 4 + id % 4;
         const int64_t m = static_cast<int64_t>(blockIdx.y) * kTokens + id % 64 / 4;
         if (m >= a.M || j >= w.rows) continue;
         float s = 0.0f;
-        for (int k = 0; k < waves; ++k) s += sums[k * RT * 256 + id];
+        for (int k = 0; k < waves; ++k) s += sums[k * 256 + id];
         if (XD == 3 && !XG) s *= a.x_scales[m];
         const int64_t at = m * a.ldy + j;
         if (a.y_dtype == 0) static_cast<float*>(a.y)[at] = s;
@@ -327,23 +300,17 @@ hipError_t blocks_for(int64_t threads, unsigned* blocks) {
     return hipSuccess;
 }
 
-template <int XD, int GPT, int RT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hipStream_t stream) {
-    const int64_t row_tiles = (k.w.rows + 15) / 16, x = (row_tiles + RT - 1) / RT, y = (k.M + kTokens - 1) / kTokens;
+template <int XD, int GPT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hipStream_t stream) {
+    const int64_t x = (k.w.rows + 15) / 16, y = (k.M + kTokens - 1) / kTokens;
     const int waves = static_cast<int>(k.w.ktiles < 16 ? k.w.ktiles : 16);
     if (x * waves * 64 > 0xffffffffLL || y > 0xffff) return hipErrorInvalidValue;
-    matvec_kernel<XD, GPT, RT, XG><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), waves * 64,
-                                     waves * RT * 256 * sizeof(float), stream>>>(k);
+    matvec_kernel<XD, GPT, XG><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), waves * 64,
+                                 waves * 256 * sizeof(float), stream>>>(k);
     return hipGetLastError();
 }
-// Tiles of rows a wave: x is read once for all of them, which pays where enough
-// tiles remain for every compute unit.
-template <int XD, int GPT, bool XG> hipError_t matvec_rt(const MatvecArgs& k, hipStream_t stream) {
-    if (k.M <= 2 || k.w.rows < kTwoTiles) return matvec_t<XD, GPT, 1, XG>(k, stream);
-    return matvec_t<XD, GPT, 2, XG>(k, stream);
-}
 template <int XD, bool XG> hipError_t matvec_x(const MatvecArgs& k, hipStream_t stream) {
-    return k.w.group == 32 ? matvec_rt<XD, 4, XG>(k, stream)
-                           : k.w.group == 64 ? matvec_rt<XD, 2, XG>(k, stream) : matvec_rt<XD, 1, XG>(k, stream);
+    return k.w.group == 32 ? matvec_t<XD, 4, XG>(k, stream)
+                           : k.w.group == 64 ? matvec_t<XD, 2, XG>(k, stream) : matvec_t<XD, 1, XG>(k, stream);
 }
 
 }  // namespace
