@@ -59,7 +59,7 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
 // The group's sum times its scale goes to the running fp32 sum of the output.
 //
 // Rows of x in fp32 are cut into three bf16 parts of 8 bits each, which hold all 24
-// bits; fp8 becomes bf16 exactly.
+// bits, and meet the weights themselves; fp8 becomes bf16 exactly.
 //
 // The waves of a workgroup take the tiles of columns in turn, each wave's next tile
 // in flight (two or more ahead are no faster: 25088 -> 4096 14.2 us with one, 15.8
@@ -89,13 +89,23 @@ template <bool F16> __device__ __forceinline__ u32x4 widen_codes(uint32_t w) {
 // What must go again: -24 in bf16, -136 in fp16.
 template <bool F16> constexpr uint32_t kOffset = F16 ? 0xd840d840u : 0xc1c0c1c0u;
 
+// The weights themselves, codes less 8, for fp32: what is added above would cost
+// fp32 rows three of their bits (over 4096 columns 1.0e-6 off, and 1.2e-7 without).
+__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+__device__ __forceinline__ u32x4 exact_codes(uint32_t w) {
+    u32x4 f = widen_codes<false>(w);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        f[j] = upper_halves(__float_as_uint(__uint_as_float(f[j] << 16) - 24.0f),
+                            __float_as_uint(__uint_as_float(f[j] & 0xffff0000u) - 24.0f));
+    return f;
+}
+
 template <int D> struct XTypeOf { using type = typename DTypeOf<D>::type; };
 template <> struct XTypeOf<3> { using type = uint8_t; };
 
 // Eight columns of a row of x as 16-bit parts: one, or three for fp32.
 template <int XD> constexpr int kPlanes = XD == 0 ? 3 : 1;
-
-__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 
 template <typename X> struct __attribute__((packed, aligned(1))) XRun {
     X v[8];
@@ -199,13 +209,13 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
             const u32x2 sc = scales[group * 4];
             const u32x4 offset{kOffset<F16>, kOffset<F16>, kOffset<F16>, kOffset<F16>};
             f32x4 sum{0, 0, 0, 0};
+            if constexpr (XD != 0) {
 #pragma unroll
-            for (int s = g * SPG; s < (g + 1) * SPG; ++s)
-#pragma unroll
-                for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(offset, xp[s][part], sum);
+                for (int s = g * SPG; s < (g + 1) * SPG; ++s) sum = mma<F16>(offset, xp[s][0], sum);
+            }
 #pragma unroll
             for (int s = g * SPG; s < (g + 1) * SPG; ++s) {
-                const u32x4 frag = widen_codes<F16>(cur[s]);
+                const u32x4 frag = XD == 0 ? exact_codes(cur[s]) : widen_codes<F16>(cur[s]);
 #pragma unroll
                 for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(frag, xp[s][part], sum);
             }
