@@ -66,6 +66,11 @@ wg_status check_rows(const wg_rows& r, const char* name, int64_t N, int64_t L, i
     return WG_OK;
 }
 
+// Channels of a row that is normalised: workgroups of the gradients' sums count them.
+wg_status check_row(int64_t C) {
+    return C <= (int64_t(1) << 25) ? WG_OK : fail(WG_ERR_UNSUPPORTED, "rows of more than 2^25 channels");
+}
+
 // Steps of a scan: the kernels count them in 32 bits, a tile past the end.
 wg_status check_steps(int64_t L) {
     return L <= 0x7fff0000 ? WG_OK : fail(WG_ERR_UNSUPPORTED, "more than 2^31 - 2^16 steps");
@@ -189,6 +194,7 @@ wg_status winograd_rms_norm(const wg_rms_norm* a, hipStream_t stream) {
             return fail(WG_ERR_UNSUPPORTED, "group must be 0 or, for 8 bits, 32, 64 or 128");
         const int64_t N = a->N, L = a->L, C = a->C, es = wg::dtype_bytes(static_cast<int>(a->dtype));
         WG_TRY(check_sizes(N, L, C, 0, 0));
+        WG_TRY(check_row(C));
         if (!std::isfinite(a->eps) || a->eps < 0) return fail(WG_ERR_ARG, "eps must be finite and not negative");
         if (N == 0 || L == 0) return WG_OK;
         WG_TRY(check_rows(a->x, "x", N, L, C, es, false));
@@ -207,6 +213,7 @@ wg_status winograd_rms_norm_workspace(wg_dtype dtype, int64_t N, int64_t L, int6
         if (!bytes) return fail(WG_ERR_ARG, "null argument");
         if (!storage(dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
         WG_TRY(check_sizes(N, L, C, 0, 0));
+        WG_TRY(check_row(C));
         *bytes = wg::rms_norm_workspace(dtype, N, L, C);
         return WG_OK;
     });
@@ -218,6 +225,7 @@ wg_status winograd_rms_norm_backward(const wg_rms_norm_backward* a, hipStream_t 
         if (!storage(a->dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
         const int64_t N = a->N, L = a->L, C = a->C, es = wg::dtype_bytes(static_cast<int>(a->dtype));
         WG_TRY(check_sizes(N, L, C, 0, 0));
+        WG_TRY(check_row(C));
         if (!std::isfinite(a->eps) || a->eps < 0) return fail(WG_ERR_ARG, "eps must be finite and not negative");
         WG_TRY(check_rows(a->dy, "dy", N, L, C, es, false));
         WG_TRY(check_rows(a->r, "r", N, L, C, es, false));

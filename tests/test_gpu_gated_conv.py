@@ -1,0 +1,105 @@
+"""The example layer that runs the sequence operators around the 1D convolution:
+its forward pass against the formula in 64 bits, its gradients against
+differences, and its single tokens against its forward pass."""
+import numpy as np
+import pytest
+import torch
+
+import sequence_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _reference(layer, x, res, weight):
+    """y and r in 64 bits with the weights [3C][3][C]."""
+    r, n, _ = R.norm(_np(x), None if res is None else _np(res), _np(layer.norm_weight), layer.eps)
+    N, L, C = r.shape
+    pad = np.concatenate((np.zeros((N, 2, C)), n), 1)
+    u = sum(pad[:, j:j + L] @ weight[:, j].T for j in range(3))
+    return R.scan(u[..., :C], u[..., C:2 * C], u[..., 2 * C:], None, None)["y"][0], r
+
+
+@pytest.mark.parametrize("shape", [(2, 37, 64), (1, 1, 32), (3, 300, 96)], ids=str)
+def test_forward_against_the_formula(shape):
+    """fp32 with F(2, 3), whose transforms have entries of at most 1: the
+    convolution's sums of 3 C products are off by some 1e-6 of their size, the
+    gates' slopes and the recurrence keep that below 1e-4 here."""
+    from paper_1905_05233_amd.gated_conv import GatedConv
+    layer = GatedConv(shape[2], dtype="f32", seed=1)
+    layer.norm_weight.copy_(torch.rand(shape[2]) + 0.5)
+    x, res = torch.randn(shape, device="cuda"), torch.randn(shape, device="cuda")
+    y, r, _ = layer.forward(x, residual=res)
+    want, rr = _reference(layer, x, res, _np(layer.weight))
+    assert np.abs(_np(r) - rr).max() <= 1e-6 and np.abs(_np(y) - want).max() <= 1e-4
+
+
+def test_gradients_against_differences():
+    """Central differences of the fp32 layer with step 2^-7: off by the third
+    derivative times step^2 and by the outputs' 1e-5 over the step."""
+    from paper_1905_05233_amd.gated_conv import GatedConv
+    shape = (2, 40, 32)
+    layer = GatedConv(32, dtype="f32", seed=2)
+    x, dy, dr = (torch.randn(shape, device="cuda") for _ in range(3))
+    res = torch.randn(shape, device="cuda")
+    y, r, saved = layer.forward(x, residual=res)
+    dx, dweight, dnorm = layer.backward(dy, saved, dr=dr)
+
+    def loss():
+        y, r, _ = layer.forward(x, residual=res)
+        return float((y.double() * dy.double()).sum() + (r.double() * dr.double()).sum())
+
+    for t, grad in ((x, dx), (res, dx), (layer.weight, dweight), (layer.norm_weight, dnorm)):
+        d = torch.randn_like(t)
+        keep, step = t.clone(), 2.0 ** -7
+        t.copy_(keep + step * d)
+        up = loss()
+        t.copy_(keep - step * d)
+        down = loss()
+        t.copy_(keep)
+        num, scale = (up - down) / (2 * step), float(torch.linalg.vector_norm(grad.double()))
+        assert abs(num - float((grad.double() * d.double()).sum())) <= 1e-2 * scale + 1e-2
+
+
+@pytest.mark.parametrize("eight_bit", [False, True])
+def test_tokens_follow_the_prompt(eight_bit):
+    """Tokens one at a time after a prompt give what the forward pass over all of
+    them gives, with the weights that the 4 bits stand for.  In 16 bits the two
+    differ by roundings to bf16 (2^-8 each) of norms, gates and values; in 8 bits the
+    norms are off by up to 2^-4 each, which sums over 192 channels average."""
+    from paper_1905_05233_amd.gated_conv import GatedConv
+    N, L, C = 3, 20, 64
+    layer = GatedConv(C, dtype="bf16", seed=3)
+    w4 = layer.quantize(group=64)
+    layer.weight.copy_(w4.dequantize().view(3 * C, 3, C))
+    x = torch.randn((N, L, C), device="cuda").bfloat16()
+    full, r, _ = layer.forward(x)
+    for start in (1, 2, 11):
+        y, _, state = layer.prompt(x[:, :start], eight_bit=eight_bit)
+        assert torch.equal(y, full[:, :start])
+        for l in range(start, L):
+            y, _ = layer.step(x[:, l], state, w4)
+            off = (y.float() - full[:, l].float()).abs().max()
+            assert float(off) <= (0.3 if eight_bit else 0.04), (start, l, float(off))
+
+
+def test_two_layers_train():
+    """A few steps of gradient descent through two layers lower the loss."""
+    from paper_1905_05233_amd.gated_conv import GatedConv
+    layers = [GatedConv(64, dtype="f32", seed=k) for k in (4, 5)]
+    x, target = torch.randn((4, 50, 64), device="cuda"), torch.randn((4, 50, 64), device="cuda") * 0.3
+    losses = []
+    for _ in range(15):
+        y0, r0, s0 = layers[0].forward(x)
+        y1, r1, s1 = layers[1].forward(y0, residual=r0)
+        d = (y1 - target) * (2.0 / y1.numel())
+        losses.append(float(((y1 - target) ** 2).mean()))
+        dr, dw1, dn1 = layers[1].backward(d, s1)
+        _, dw0, dn0 = layers[0].backward(dr, s0, dr=dr)
+        for layer, dw, dn in ((layers[0], dw0, dn0), (layers[1], dw1, dn1)):
+            layer.weight.sub_(5.0 * dw)
+            layer.norm_weight.sub_(5.0 * dn)
+    assert losses[-1] < 0.9 * losses[0], losses
