@@ -38,9 +38,11 @@ constexpr int kStepThreads = 256;
 constexpr int kScanBlock = WG_SCAN_BLOCK;
 constexpr int kHeld = 16;             // gates that a thread holds of a tile
 constexpr int kThreads = 512;
+// Sequences of at most kShort steps: a tile of as many (300 x 2 x 2048 fp32: 512 threads would idle).
+constexpr int short_threads(int V) { return 2 * 8 * V; }
 constexpr int grad_threads(int lanes) { return lanes == 8 ? 256 : 512; }
 // Groups of channels that fill the chip, and workgroups that chunks make of fewer.
-constexpr int64_t kFull = 192, kChunked = 512, kMostChunks = 256, kWalked = 4;
+constexpr int64_t kFull = 192, kChunked = 512, kMostChunks = 256, kWalked = 4, kShort = 2 * kHeld;
 // LANES: 16-byte runs of channels of a workgroup
 template <typename Elem, int LANES> constexpr int kChannels = LANES * (16 / static_cast<int>(sizeof(Elem)));
 
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(T) void scan_kernel(ScanArgs<Elem> a) {
 
     u32x4 z[S], v[S], o[S];
     auto load = [&](const Place& p) {
-        if (!p.shape.valid) return;
+        if (!p.shape.valid || p.l0 >= p.steps) return;   // what is not loaded is replaced
         load_steps<Elem, FULL, S>(a.gate.at(p.n, 0) + p.c0, a.gate.sl, p.l0, L, p.shape, a.C, z);
         load_steps<Elem, FULL, S>(a.value.at(p.n, 0) + p.c0, a.value.sl, p.l0, L, p.shape, a.C, v);
         if (OUT && !MAPS) load_steps<Elem, FULL, S>(a.out_gate.at(p.n, 0) + p.c0, a.out_gate.sl, p.l0, L, p.shape, a.C, o);
@@ -419,7 +421,7 @@ __global__ __launch_bounds__(T) void scan_grad_kernel(GradArgs<Elem> a) {
 
     u32x4 z[S], v[S], o[S], d[S];
     auto load = [&](const Place& p) {
-        if (!p.shape.valid) return;
+        if (!p.shape.valid || p.l0 >= p.steps) return;   // what is not loaded is replaced
         load_steps<Elem, FULL, S>(a.gate.at(p.n, 0) + p.c0, a.gate.sl, p.l0, L, p.shape, a.C, z);
         load_steps<Elem, FULL, S>(a.dy.at(p.n, 0) + p.c0, a.dy.sl, p.l0, L, p.shape, a.C, d);
         if (!MAPS) load_steps<Elem, FULL, S>(a.value.at(p.n, 0) + p.c0, a.value.sl, p.l0, L, p.shape, a.C, v);
@@ -610,18 +612,18 @@ __global__ __launch_bounds__(kStepThreads) void step_kernel(StepArgs<Elem> a) {
 // How a call is cut.
 struct Plan {
     Split split;
-    int lanes;
+    int lanes, threads;
 };
 Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
     const int V = 16 / dtype_bytes(dtype);
     Plan p;
     p.split.runs = static_cast<int32_t>((C + V - 1) / V);
     p.split.columns = N * p.split.runs;
-    p.lanes = dtype == kF32 || p.split.columns >= 8 * kFull || p.split.columns < 4 * kFull ? 8 : 4;
+    p.lanes = dtype == kF32 || L <= kShort || p.split.columns >= 8 * kFull || p.split.columns < 4 * kFull ? 8 : 4;
     const int64_t groups = (p.split.columns + p.lanes - 1) / p.lanes;
     p.split.groups = static_cast<uint32_t>(std::min<int64_t>(groups, 0xffffffffLL));
-    const int threads = backward ? grad_threads(p.lanes) : kThreads;
-    const int64_t tile = threads / (p.lanes * V) * kHeld, tiles = (L + tile - 1) / tile;
+    p.threads = L <= kShort ? short_threads(V) : backward ? grad_threads(p.lanes) : kThreads;
+    const int64_t tile = p.threads / (p.lanes * V) * kHeld, tiles = (L + tile - 1) / tile;
     int64_t chunks = 1;
     if (groups < kFull && tiles > kWalked) chunks = std::min<int64_t>({tiles, kChunked / groups, kMostChunks});
     const int64_t each = std::max<int64_t>(1, (tiles + chunks - 1) / chunks);
@@ -631,9 +633,9 @@ Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
     return p;
 }
 
-template <typename F> hipError_t launch_chunks(const Plan& p, int threads, F&& launch) {
+template <typename F> hipError_t launch_chunks(const Plan& p, F&& launch) {
     const int64_t x = p.lanes == 8 ? p.split.groups : (static_cast<int64_t>(p.split.groups) + 15) / 16 * 16;
-    if (x * threads > 0xffffffffLL) return hipErrorInvalidValue;
+    if (x * p.threads > 0xffffffffLL) return hipErrorInvalidValue;
     const unsigned y = static_cast<unsigned>(p.split.chunks);
     // nothing reads the last chunk's map
     launch(dim3(static_cast<unsigned>(x), y - 1), dim3(static_cast<unsigned>(x), y));
@@ -654,18 +656,20 @@ size_t gated_scan_workspace(int dtype, int64_t N, int64_t L, int64_t C, bool bac
 
 template <int D> hipError_t launch_gated_scan_t(const wg_gated_scan& a, hipStream_t stream) {
     using Elem = typename DTypeOf<D>::type;
-    constexpr int T = kThreads;
+    constexpr int SHORT = short_threads(Vec<Elem>::V);
     const Plan p = plan_scan(D, a.N, a.L, a.C, false);
     const ScanArgs<Elem> k{a.N, static_cast<int32_t>(a.L), static_cast<int32_t>(a.C), rows_of<const Elem>(a.gate),
                            rows_of<const Elem>(a.value), rows_of<const Elem>(a.out_gate), rows_of<Elem>(a.y), a.h0,
                            a.lengths, a.h_last, a.states, static_cast<float2*>(a.workspace), p.split};
     const bool out = a.out_gate.data != nullptr, full = a.C % Vec<Elem>::V == 0;
-    return launch_chunks(p, kThreads, [&](dim3 ahead, dim3 grid) {
-#define WG_SCAN_CASE(LANES, OUT, FULL)                                                                           \
-    if constexpr (LANES == 8 || D != kF32)                                                                       \
-        if (p.lanes == LANES && out == OUT && full == FULL) {                                                    \
-            if (ahead.y > 0) scan_kernel<Elem, T, LANES, false, FULL, true><<<ahead, T, 0, stream>>>(k);         \
-            scan_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                            \
+    return launch_chunks(p, [&](dim3 ahead, dim3 grid) {
+#define WG_SCAN_CASE(LANES, OUT, FULL)                                                                               \
+    if constexpr (LANES == 8 || D != kF32)                                                                           \
+        if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
+            constexpr int T = kThreads;                                                                              \
+            if (ahead.y > 0) scan_kernel<Elem, T, LANES, false, FULL, true><<<ahead, T, 0, stream>>>(k);             \
+            if (LANES == 8 && p.threads == SHORT) scan_kernel<Elem, SHORT, 8, OUT, FULL, false><<<grid, SHORT, 0, stream>>>(k); \
+            else scan_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                           \
         }
         WG_SCAN_CASES(WG_SCAN_CASE)
 #undef WG_SCAN_CASE
@@ -674,19 +678,22 @@ template <int D> hipError_t launch_gated_scan_t(const wg_gated_scan& a, hipStrea
 
 template <int D> hipError_t launch_gated_scan_backward_t(const wg_gated_scan_backward& a, hipStream_t stream) {
     using Elem = typename DTypeOf<D>::type;
+    constexpr int SHORT = short_threads(Vec<Elem>::V);
     const Plan p = plan_scan(D, a.N, a.L, a.C, true);
     const GradArgs<Elem> k{a.N, static_cast<int32_t>(a.L), static_cast<int32_t>(a.C), rows_of<const Elem>(a.dy),
                            rows_of<const Elem>(a.gate), rows_of<const Elem>(a.value), rows_of<const Elem>(a.out_gate),
                            rows_of<Elem>(a.dgate), rows_of<Elem>(a.dvalue), rows_of<Elem>(a.dout_gate), a.states,
                            a.dh_last, a.lengths, a.dh0, static_cast<float2*>(a.workspace), p.split};
     const bool out = a.out_gate.data != nullptr, full = a.C % Vec<Elem>::V == 0;
-    return launch_chunks(p, grad_threads(p.lanes), [&](dim3 ahead, dim3 grid) {
-#define WG_SCAN_CASE(LANES, OUT, FULL)                                                                           \
-    if constexpr (LANES == 8 || D != kF32)                                                                       \
-        if (p.lanes == LANES && out == OUT && full == FULL) {                                                    \
-            constexpr int T = grad_threads(LANES);                                                               \
-            if (ahead.y > 0) scan_grad_kernel<Elem, T, LANES, OUT, FULL, true><<<ahead, T, 0, stream>>>(k);      \
-            scan_grad_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                       \
+    return launch_chunks(p, [&](dim3 ahead, dim3 grid) {
+#define WG_SCAN_CASE(LANES, OUT, FULL)                                                                               \
+    if constexpr (LANES == 8 || D != kF32)                                                                           \
+        if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
+            constexpr int T = grad_threads(LANES);                                                                   \
+            if (ahead.y > 0) scan_grad_kernel<Elem, T, LANES, OUT, FULL, true><<<ahead, T, 0, stream>>>(k);          \
+            if (LANES == 8 && p.threads == SHORT)                                                                    \
+                scan_grad_kernel<Elem, SHORT, 8, OUT, FULL, false><<<grid, SHORT, 0, stream>>>(k);                   \
+            else scan_grad_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                      \
         }
         WG_SCAN_CASES(WG_SCAN_CASE)
 #undef WG_SCAN_CASE
