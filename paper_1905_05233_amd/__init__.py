@@ -6,6 +6,8 @@ The computation lives in the native library ``libwinograd_crt.so`` (C ABI in
 hand-written HIP kernels for the kernel, input and output transforms and the
 matrix-core contraction.  ``Plan`` is a thin binding over it; importing this
 package does not load the library (``workloads`` is usable without it).
+``sequence_ops`` holds the operators around the 1D convolution of sequences,
+``gated_conv`` a layer made of them.
 """
 
 __all__ = ["Plan", "WinogradError", "build_native"]

@@ -9,17 +9,24 @@
 // All of it in fp32; each result is rounded once to its type.
 //
 // Both directions are a scan of maps s -> A s + B, which compose: a run of steps
-// has A the product of its gates.  A workgroup takes 128 bytes of channels (runs of
-// 64 bytes hold a card at 3.8 TB/s, of 128 bytes at 4.8) and a tile of steps, of
-// which a thread holds 16 bytes of each of S steps in registers, kHeld gates in all.
-// It composes its steps; the maps of the threads go through LDS, where a thread per
-// (channel, kHeld steps) composes them, a shift-and-compose over a channel's
-// lanes follows, and every thread gets the state ahead of its own steps.  Rows are
-// read once and written once, whatever the length.
+// has A the product of its gates.  A workgroup takes a group of channels and walks
+// tiles of steps; of a tile a thread holds 16 bytes of each of S steps in registers,
+// kHeld gates in all.  It composes its steps; the maps of the threads go through
+// LDS, where a thread per (channel, kHeld steps) composes them, a
+// shift-and-compose over a channel's lanes follows, and every thread gets the
+// state ahead of its own steps.  The next tile's loads are in flight during that.
+// Rows are read once and written once, whatever the length.
 //
 // Where the channels do not fill the chip, the length is cut into chunks, a
 // workgroup each: a first kernel composes each chunk's map (reading the gates a
 // second time), the second one starts each chunk from the maps ahead of it.
+//
+// What bounds it: memory, for many channels (64 x 512 x 2048 in bf16: 118 us
+// forward, 4.6 TB/s; 204 us backward, 4.6 TB/s), held back where a workgroup's runs
+// are 64 bytes long: a card copies those at 3.8 TB/s, runs of 128 bytes at 4.8.
+// 16 x 4096 x 512, of 64-byte runs: 76 us forward (3.5 TB/s), 113 us backward (4.2).
+// One sequence of 16381 x 512 reads its gates twice: 10 + 15 us, 67 MB of inputs and
+// outputs (2.9 TB/s for the call).  A few short sequences take one tile's latency.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -36,13 +43,35 @@ namespace {
 
 constexpr int kStepThreads = 256;
 constexpr int kScanBlock = WG_SCAN_BLOCK;
-constexpr int kHeld = 16;             // gates that a thread holds of a tile
+// Gates that a thread holds of a tile: with 32 the gradients spill registers, and the
+// forward pass of 64 x 512 x 2048 bf16 takes 132 us instead of 118.
+constexpr int kHeld = 16;
+
+// Which form a call takes.  LANES, 16-byte runs of a group: 8 make a 128-byte run of
+// channels, 4 a 64-byte one with twice as many groups.  8 where that still gives
+// kFull groups (three quarters of the compute units; 64 x 512 x 2048 bf16: 118 us
+// against 139 forward, 204 against 237 backward), and where the length is cut into
+// chunks anyway (16381 x 512 backward: 43 against 50 us).  4 in between
+// (16 x 4096 x 512, 128 groups of 128 bytes or 256 of 64: 74 against 101 us forward,
+// 127 against 161 backward).  fp32 has one form.
+constexpr int64_t kFull = 192;
+// Chunks, where there are fewer groups than kFull: so many that there are kChunked
+// workgroups (16381 x 512 forward: 25.2 us; with 256 28.0, with 1024 26.4), and at
+// most kMostChunks, whose maps each chunk composes (32768 x 64: 16.9 us forward, with
+// 64 chunks 22.0).  Sequences of kWalked tiles or fewer are walked (3 us a tile,
+// against a second launch); 8 tiles cost 22.6 us walked, 4 + 6 in chunks
+// (gradients of 4 x 1000 x 96 fp32).
+constexpr int64_t kChunked = 512, kMostChunks = 256, kWalked = 4;
+// Threads of a workgroup.  The gradients hold twice the values: with 256 threads two
+// workgroups share a compute unit (64 x 512 x 2048: 204 us, with 512 225); where there
+// is one group a compute unit, more threads keep more loads in flight
+// (16 x 4096 x 512: 127 us with 512, 137 with 256).
 constexpr int kThreads = 512;
-// Sequences of at most kShort steps: a tile of as many (300 x 2 x 2048 fp32: 512 threads would idle).
-constexpr int short_threads(int V) { return 2 * 8 * V; }
 constexpr int grad_threads(int lanes) { return lanes == 8 ? 256 : 512; }
-// Groups of channels that fill the chip, and workgroups that chunks make of fewer.
-constexpr int64_t kFull = 192, kChunked = 512, kMostChunks = 256, kWalked = 4, kShort = 2 * kHeld;
+// Sequences of at most kShort steps take a tile of as many: 37 x 4 x 1024 fp32 takes
+// 11.8 us a call (bound by the host) instead of 16.4.
+constexpr int64_t kShort = 2 * kHeld;
+constexpr int short_threads(int V) { return 2 * 8 * V; }
 // LANES: 16-byte runs of channels of a workgroup
 template <typename Elem, int LANES> constexpr int kChannels = LANES * (16 / static_cast<int>(sizeof(Elem)));
 
@@ -592,6 +621,7 @@ template <typename Elem> struct StepArgs {
     float* h_new;
 };
 
+// One thread per channel of a sequence: 16 x 512 take 2.6 us, a launch's latency.
 template <typename Elem>
 __global__ __launch_bounds__(kStepThreads) void step_kernel(StepArgs<Elem> a) {
     using S = Storage<Elem>;
