@@ -289,7 +289,6 @@ __global__ __launch_bounds__(T) void scan_kernel(ScanArgs<Elem> a) {
     // the state ahead of the tile at hand, or the map of the chunk's tiles so far
     float carry = !MAPS && sc.scans && a.h0 ? a.h0[sc.n * a.C + sc.c] : 0.0f;
     float product = 1.0f;
-    if (!MAPS && chunk > 0) carry = reach_chunk<P>(maps, map_stride, chunk, part, carry);
 
     u32x4 z[S], v[S], o[S];
     auto load = [&](const Place& p) {
@@ -299,6 +298,7 @@ __global__ __launch_bounds__(T) void scan_kernel(ScanArgs<Elem> a) {
         if (OUT && !MAPS) load_steps<Elem, FULL, S>(a.out_gate.at(p.n, 0) + p.c0, a.out_gate.sl, p.l0, L, p.shape, a.C, o);
     };
     if (chunk * a.split.chunk < end) load(at);
+    if (!MAPS && chunk > 0) carry = reach_chunk<P>(maps, map_stride, chunk, part, carry);
     for (int tile = chunk * a.split.chunk, buf = 0; tile < end; ++tile, buf ^= 1) {
         float f[S][V], b[S][V], s[S][V];
         float A[V], B[V];
@@ -446,7 +446,6 @@ __global__ __launch_bounds__(T) void scan_grad_kernel(GradArgs<Elem> a) {
     // the gradient behind the tile at hand, or the map of the chunk's tiles so far
     float carry = !MAPS && sc.scans && a.dh_last ? a.dh_last[sc.n * a.C + sc.c] : 0.0f;
     float product = 1.0f;
-    if (!MAPS && chunk > 0) carry = reach_chunk<P>(maps, map_stride, chunk, part, carry);
 
     u32x4 z[S], v[S], o[S], d[S];
     auto load = [&](const Place& p) {
@@ -457,6 +456,7 @@ __global__ __launch_bounds__(T) void scan_grad_kernel(GradArgs<Elem> a) {
         if (OUT) load_steps<Elem, FULL, S>(a.out_gate.at(p.n, 0) + p.c0, a.out_gate.sl, p.l0, L, p.shape, a.C, o);
     };
     if (chunk * a.split.chunk < end) load(at);
+    if (!MAPS && chunk > 0) carry = reach_chunk<P>(maps, map_stride, chunk, part, carry);
     for (int tile = chunk * a.split.chunk, buf = 0; tile < end; ++tile, buf ^= 1) {
         // g: the gradient at a step's state from its own output; q: what times
         // the state is the output gate's gradient
@@ -667,7 +667,7 @@ template <typename F> hipError_t launch_chunks(const Plan& p, F&& launch) {
     const int64_t x = p.lanes == 8 ? p.split.groups : (static_cast<int64_t>(p.split.groups) + 15) / 16 * 16;
     if (x * p.threads > 0xffffffffLL) return hipErrorInvalidValue;
     const unsigned y = static_cast<unsigned>(p.split.chunks);
-    // nothing reads the last chunk's map
+    // nothing reads the last chunk's map; chunks are of groups of 8 LANES (fewer than kFull groups)
     launch(dim3(static_cast<unsigned>(x), y - 1), dim3(static_cast<unsigned>(x), y));
     return hipGetLastError();
 }
@@ -697,7 +697,7 @@ template <int D> hipError_t launch_gated_scan_t(const wg_gated_scan& a, hipStrea
     if constexpr (LANES == 8 || D != kF32)                                                                           \
         if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
             constexpr int T = kThreads;                                                                              \
-            if (ahead.y > 0) scan_kernel<Elem, T, LANES, false, FULL, true><<<ahead, T, 0, stream>>>(k);             \
+            if (LANES == 8 && ahead.y > 0) scan_kernel<Elem, T, 8, false, FULL, true><<<ahead, T, 0, stream>>>(k);   \
             if (LANES == 8 && p.threads == SHORT) scan_kernel<Elem, SHORT, 8, OUT, FULL, false><<<grid, SHORT, 0, stream>>>(k); \
             else scan_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                           \
         }
@@ -720,7 +720,8 @@ template <int D> hipError_t launch_gated_scan_backward_t(const wg_gated_scan_bac
     if constexpr (LANES == 8 || D != kF32)                                                                           \
         if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
             constexpr int T = grad_threads(LANES);                                                                   \
-            if (ahead.y > 0) scan_grad_kernel<Elem, T, LANES, OUT, FULL, true><<<ahead, T, 0, stream>>>(k);          \
+            if (LANES == 8 && ahead.y > 0)                                                                           \
+                scan_grad_kernel<Elem, grad_threads(8), 8, OUT, FULL, true><<<ahead, grad_threads(8), 0, stream>>>(k); \
             if (LANES == 8 && p.threads == SHORT)                                                                    \
                 scan_grad_kernel<Elem, SHORT, 8, OUT, FULL, false><<<grid, SHORT, 0, stream>>>(k);                   \
             else scan_grad_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                      \

@@ -66,6 +66,15 @@ def test_scan_and_gradients(shape, dtype):
     _call(shape, dtype, seed=shape[1] + 7, out_gate=False, h0=shape[2] % 2 == 1)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("shape", [(100, 600, 72), (200, 300, 64), (130, 270, 61), (2000, 20, 40), (3, 5000, 128)], ids=str)
+def test_many_channels_over_several_tiles(shape, dtype):
+    """Channels that fill the chip, in groups of 64 and of 128 bytes, over several
+    tiles of steps; many short sequences; chunks of a tile."""
+    print(f"[scan] {shape} {dtype}", flush=True)
+    _call(shape, dtype, 17, out_gate=shape[0] != 200, h0=True, lengths=[(37 * k) % (shape[1] + 9) for k in range(shape[0])])
+
+
 @pytest.mark.parametrize("layout", ["fused", "steps"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(3, 70, 24), (2, 300, 37), (1, 9, 3), (2, 40, 130)], ids=str)

@@ -72,6 +72,32 @@ def test_norm_fp8(shape, group, dtype):
         assert (np.abs(_np(q.float())) <= 448).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(70000, 16), (17000, 104), (9000, 520), (2600, 4100), (3, 20000), (2, 33000)], ids=str)
+def test_norm_many_and_long_rows(shape, dtype):
+    """More rows than workgroups walk at a time, and rows of a whole workgroup or
+    more: outputs in both types and gradients."""
+    from paper_1905_05233_amd import sequence_ops as S
+    print(f"[norm] {shape} {dtype}", flush=True)
+    (x, dy), w = _inputs(shape, dtype, 5, 2)
+    y, r = S.rms_norm(x, w, residual=dy, eps=EPS)
+    rr, want, bound = R.norm(_np(x), _np(dy), _np(w), EPS)
+    R.assert_close(_np(y), want, bound, dtype, "y")
+    R.assert_close(_np(r), rr, np.abs(rr) * 2.0 ** -24, dtype, "r")
+    C = shape[1]
+    for group in (0, 128):
+        q, scales, _ = S.rms_norm_fp8(x, w, residual=dy, eps=EPS, group=group)
+        s = np.repeat(_np(scales), group or C, 1)[:, :C]
+        got = _np(q.float()) * s
+        assert (np.abs(got - want) <= np.maximum(np.abs(want) * 2.0 ** -4, s * 2.0 ** -10) + 2 * bound).all()
+        tops = np.abs(np.pad(want, ((0, 0), (0, -C % (group or C))))).reshape(shape[0], -1, group or C).max(2)
+        assert (np.abs(_np(scales) - tops / 448) <= (C / 2 + 16) * 2.0 ** -24 * tops / 448).all()
+    dx, dw = S.rms_norm_backward(dy, x, w, eps=EPS)
+    want, bx, wantw, bw = R.norm_gradients(_np(dy), _np(x), _np(w), None, EPS)
+    R.assert_close(_np(dx), want, bx, dtype, "dx")
+    R.assert_close(_np(dw), wantw, bw, "f32", "dweight")
+
+
 def test_norm_special_rows():
     """Rows of zeros; rows with NaN or infinity poison themselves alone."""
     from paper_1905_05233_amd import sequence_ops as S
