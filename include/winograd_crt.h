@@ -411,7 +411,7 @@ typedef struct {
  * contiguous.  states (NULL: not wanted): fp32 [N][ceil(L / WG_SCAN_BLOCK)][C],
  * the state ahead of each block of steps, for the backward pass.  workspace: of
  * winograd_gated_scan_workspace bytes, 16-byte aligned (NULL if that is 0).
- * N, C >= 1, L >= 0. */
+ * N >= 1, 1 <= C <= 2^30, 0 <= L <= 2^31 - 2^16. */
 typedef struct {
     int64_t dtype, N, L, C;
     wg_rows gate, value, out_gate, y;
@@ -463,7 +463,7 @@ wg_status winograd_gated_step(const wg_gated_step* args, hipStream_t stream);
  *   s = max(max |y|, 2^-100) / 448 of each group of `group` channels (32, 64 or
  *   128; 0: the whole row; the last group may be short), y = e4m3(y / s),
  * scales fp32 [N][L][ceil(C / group)] (one a row for group 0), contiguous.
- * r may be x or residual itself (the same rows).  N, L >= 0, C >= 1. */
+ * r may be x or residual itself (the same rows).  N, L >= 0, 1 <= C <= 2^25. */
 typedef struct {
     int64_t dtype, N, L, C;
     wg_rows x, residual, r, y;

@@ -71,9 +71,10 @@ wg_status check_row(int64_t C) {
     return C <= (int64_t(1) << 25) ? WG_OK : fail(WG_ERR_UNSUPPORTED, "rows of more than 2^25 channels");
 }
 
-// Steps of a scan: the kernels count them in 32 bits, a tile past the end.
-wg_status check_steps(int64_t L) {
-    return L <= 0x7fff0000 ? WG_OK : fail(WG_ERR_UNSUPPORTED, "more than 2^31 - 2^16 steps");
+// Steps and channels of a scan: the kernels count them in 32 bits, past the end too.
+wg_status check_steps(int64_t L, int64_t C) {
+    if (L > 0x7fff0000) return fail(WG_ERR_UNSUPPORTED, "more than 2^31 - 2^16 steps");
+    return C <= (int64_t(1) << 30) ? WG_OK : fail(WG_ERR_UNSUPPORTED, "more than 2^30 channels");
 }
 
 wg_status check_f32(const void* p, const char* name, bool optional = true) {
@@ -114,7 +115,7 @@ wg_status winograd_gated_scan_workspace(wg_dtype dtype, int64_t N, int64_t L, in
         if (!bytes) return fail(WG_ERR_ARG, "null argument");
         if (!storage(dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
         WG_TRY(check_sizes(N, L, C, 1, 0));
-        WG_TRY(check_steps(L));
+        WG_TRY(check_steps(L, C));
         *bytes = wg::gated_scan_workspace(dtype, N, L, C, backward != 0);
         return WG_OK;
     });
@@ -126,7 +127,7 @@ wg_status winograd_gated_scan(const wg_gated_scan* a, hipStream_t stream) {
         if (!storage(a->dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
         const int64_t N = a->N, L = a->L, C = a->C, es = wg::dtype_bytes(static_cast<int>(a->dtype));
         WG_TRY(check_sizes(N, L, C, 1, 0));
-        WG_TRY(check_steps(L));
+        WG_TRY(check_steps(L, C));
         WG_TRY(check_rows(a->gate, "gate", N, L, C, es, false));
         WG_TRY(check_rows(a->value, "value", N, L, C, es, false));
         if (a->out_gate.data) WG_TRY(check_rows(a->out_gate, "out_gate", N, L, C, es, false));
@@ -147,7 +148,7 @@ wg_status winograd_gated_scan_backward(const wg_gated_scan_backward* a, hipStrea
         if (!storage(a->dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
         const int64_t N = a->N, L = a->L, C = a->C, es = wg::dtype_bytes(static_cast<int>(a->dtype));
         WG_TRY(check_sizes(N, L, C, 1, 0));
-        WG_TRY(check_steps(L));
+        WG_TRY(check_steps(L, C));
         WG_TRY(check_rows(a->dy, "dy", N, L, C, es, false));
         WG_TRY(check_rows(a->gate, "gate", N, L, C, es, false));
         WG_TRY(check_rows(a->value, "value", N, L, C, es, false));

@@ -31,6 +31,7 @@ def _message():
     (ARG, "sizes", dict(n=1 << 31)),
     (UNSUPPORTED, "large", dict(n=1 << 20, l=1 << 21)),
     (UNSUPPORTED, "steps", dict(n=1, l=(1 << 31) - 1, c=8)),
+    (UNSUPPORTED, "channels", dict(n=1, l=8, c=(1 << 30) + 1)),
     (ARG, "null tensor gate", dict(gate=NONE)),
     (ARG, "aligned", dict(value=(P + 1, 640, 64))),
     (ARG, "strides", dict(value=(P, -1, 64))),
