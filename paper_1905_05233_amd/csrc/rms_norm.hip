@@ -502,15 +502,25 @@ int64_t walkers(int64_t rows, int tpr, int per_cu) {
 }
 
 constexpr int kNormPerCu = 8, kGradPerCu = 4;
+// The gradients' workgroups.  A few rows are one workgroup's, whose dweight is the
+// whole of it: a round of rows takes some 1 us there, the second launch and its
+// workspace 5 us of the host's time.
+constexpr int64_t kOneRounds = 4;
+int64_t grad_walkers(int64_t rows, int tpr) {
+    return rows <= kOneRounds * (block_of(tpr) / tpr) ? 1 : walkers(rows, tpr, kGradPerCu);
+}
 constexpr int64_t kLongBlocks = 4096, kColumnParts = 64;
 
 }  // namespace
 
-// dweight's parts, and behind them, for long rows, the rows' 1 / sqrt.
+// dweight's parts (one part is dweight), and behind them, for long rows, the rows' 1 / sqrt.
 size_t rms_norm_workspace(int dtype, int64_t N, int64_t L, int64_t C) {
     const Shape s = shape_of(dtype, C);
     const int64_t rows = N * L;
-    if (s.tpr) return static_cast<size_t>((walkers(rows, s.tpr, kGradPerCu) * C * 4 + 15) / 16 * 16);
+    if (s.tpr) {
+        const int64_t parts = grad_walkers(rows, s.tpr);
+        return parts == 1 ? 0 : static_cast<size_t>((parts * C * 4 + 15) / 16 * 16);
+    }
     return static_cast<size_t>(((std::min(rows, kColumnParts) * C + rows) * 4 + 15) / 16 * 16 + 16);
 }
 
@@ -548,7 +558,8 @@ template <int D> hipError_t launch_rms_norm_backward_t(const wg_rms_norm_backwar
     const Shape s = shape_of(D, a.C);
     const unsigned column_blocks = static_cast<unsigned>((a.C + 15) / 16);
     if (s.tpr && rows > 0) {
-        k.parts = walkers(rows, s.tpr, kGradPerCu);
+        k.parts = grad_walkers(rows, s.tpr);
+        if (k.parts == 1) k.partial = a.dweight;
         const unsigned blocks = static_cast<unsigned>(k.parts);
 #define WG_NORM_CASE(TPR, NV) \
     if (s.tpr == TPR && s.nv == NV) {                                                                             \
@@ -566,6 +577,7 @@ template <int D> hipError_t launch_rms_norm_backward_t(const wg_rms_norm_backwar
                                          static_cast<unsigned>(k.parts)), kNormThreads, 0, stream>>>(k);
         norm_grad_long_kernel<Elem><<<blocks, kNormThreads, 0, stream>>>(k);
     }
+    if (k.partial == a.dweight) return hipGetLastError();
     norm_parts_kernel<<<column_blocks, 1024, 0, stream>>>(k.partial, k.parts, a.C, a.dweight);
     return hipGetLastError();
 }

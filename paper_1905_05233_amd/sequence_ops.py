@@ -26,6 +26,7 @@ SCAN_BLOCK = 32      # WG_SCAN_BLOCK
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _E4M3 = 3
 _NO_ROWS = (0, 0, 0)
+_DENSE = torch.contiguous_format
 _pack_scan = struct.Struct("4q" + "Pqq" * 4 + "4PPq").pack
 _pack_scan_backward = struct.Struct("4q" + "Pqq" * 7 + "4PPq").pack
 _pack_step = struct.Struct("3q" + "Pqq" * 4 + "2P").pack
@@ -73,7 +74,7 @@ def _rows(t, name, shape, dtype, dev):
     """(address, stride_n, stride_l) of [N][L][C], or of [L][C] as one sequence."""
     try:
         s = t.stride()
-        if t.dtype == dtype and t.shape == shape and t.get_device() == dev and (s[-1] == 1 or shape[-1] <= 1):
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev and (s[-1] == 1 or shape[-1] <= 1):
             return (t.data_ptr(), s[0], s[1]) if len(s) == 3 else (t.data_ptr(), 0, s[0])
     except AttributeError:
         pass
@@ -83,7 +84,7 @@ def _rows(t, name, shape, dtype, dev):
 
 def _dense(t, name, shape, dtype, dev):
     try:
-        if t.dtype == dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
             return t.data_ptr()
     except AttributeError:
         pass
@@ -91,11 +92,22 @@ def _dense(t, name, shape, dtype, dev):
     raise ValueError(f"{name} must be contiguous")
 
 
-def _new(like, shape, dtype):
-    """A contiguous tensor on like's GPU, the quickest way that torch has."""
-    if like.dtype == dtype and like.shape == shape and like.is_contiguous():
-        return torch.empty_like(like)
-    return like.new_empty(shape, dtype=dtype)
+def _out(t, name, like, dtype, dev):
+    """(tensor, its rows): t, or if it is None a new contiguous one of like's shape."""
+    if t is not None:
+        return t, _rows(t, name, like.shape, dtype, dev)
+    # the quickest way that torch has (1.3 us; new_empty takes 1.8, and is checked again)
+    t = torch.empty_like(like, dtype=dtype, memory_format=_DENSE)
+    shape = like.shape
+    if len(shape) == 3:
+        return t, (t.data_ptr(), shape[1] * shape[2], shape[2])
+    return t, (t.data_ptr(), 0, shape[1])
+
+
+def _new_f32(like, *shape):
+    """A contiguous fp32 tensor of two or three dimensions on like's GPU."""
+    strides = (shape[1], 1) if len(shape) == 2 else (shape[1] * shape[2], shape[2], 1)
+    return torch.empty_strided(shape, strides, dtype=torch.float32, device=like.device)
 
 
 def _size(query, *args):
@@ -113,7 +125,7 @@ def _size(query, *args):
 
 
 def _workspace(need, like):
-    return like.new_empty(need, dtype=torch.uint8) if need else None
+    return torch.empty_strided((need,), (1,), dtype=torch.uint8, device=like.device) if need else None
 
 
 def _keep(stream, dev, *tensors):
@@ -139,15 +151,13 @@ def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_s
     v = _rows(value, "value", shape, dt, dev)
     o = _NO_ROWS if out_gate is None else _rows(out_gate, "out_gate", shape, dt, dev)
     own_y = y is None
-    if own_y:
-        y = _new(gate, shape, dt)
-    yr = _rows(y, "y", shape, dt, dev)
+    y, yr = _out(y, "y", gate, dt, dev)
     h0p = 0 if h0 is None else _dense(h0, "h0", (Nn, C), torch.float32, dev)
     lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
-    h_last = _new(gate if h0 is None else h0, (Nn, C), torch.float32)
+    h_last = _new_f32(gate, Nn, C)
     states = None
     if save_states:
-        states = gate.new_empty((Nn, -(-L // SCAN_BLOCK), C), dtype=torch.float32)
+        states = _new_f32(gate, Nn, -(-L // SCAN_BLOCK), C)
     need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 0)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan(
@@ -180,23 +190,23 @@ def gated_scan_backward(dy, gate, value, states, out_gate=None, dh_last=None, le
     lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
     own = out is None
     if own:
-        out = [_new(dy, shape, dt) for _ in range(2 if out_gate is None else 3)]
+        out = (None, None) if out_gate is None else (None, None, None)
     elif len(out) != (2 if out_gate is None else 3):
         raise ValueError("out must hold dgate, dvalue and, with out_gate, dout_gate")
-    rows = [_rows(t, name, shape, dt, dev) for t, name in zip(out, ("dgate", "dvalue", "dout_gate"))]
-    if out_gate is None:
-        rows.append(_NO_ROWS)
-    dh0 = _new(gate if dh_last is None else dh_last, (Nn, C), torch.float32)
+    dgate, zr = _out(out[0], "dgate", gate, dt, dev)
+    dvalue, vr = _out(out[1], "dvalue", gate, dt, dev)
+    dout_gate, outr = (None, _NO_ROWS) if out_gate is None else _out(out[2], "dout_gate", gate, dt, dev)
+    dh0 = _new_f32(gate, Nn, C)
     need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 1)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan_backward(
-        _pack_scan_backward(code, Nn, L, C, *d, *g, *v, *o, *rows[0], *rows[1], *rows[2], sp, dhp, lp, dh0.data_ptr(),
+        _pack_scan_backward(code, Nn, L, C, *d, *g, *v, *o, *zr, *vr, *outr, sp, dhp, lp, dh0.data_ptr(),
                             0 if ws is None else ws.data_ptr(), need), _raw_stream(stream))
     if st != N.WG_OK:
         N.check(st)
     if stream is not None:
-        _keep(stream, dev, *(out if own else ()), dh0, ws)
-    return out[0], out[1], (None if out_gate is None else out[2]), dh0
+        _keep(stream, dev, *((dgate, dvalue, dout_gate) if own else ()), dh0, ws)
+    return dgate, dvalue, dout_gate, dh0
 
 
 def gated_step(gate, value, h, out_gate=None, h_new=None, y=None, stream=None):
@@ -212,12 +222,12 @@ def gated_step(gate, value, h, out_gate=None, h_new=None, y=None, stream=None):
     o = _NO_ROWS if out_gate is None else _rows(out_gate, "out_gate", shape, dt, dev)
     hp = _dense(h, "h", shape, torch.float32, dev)
     own_y, own_h = y is None, h_new is None
-    if own_y:
-        y = _new(gate, shape, dt)
+    y, yr = _out(y, "y", gate, dt, dev)
     if own_h:
         h_new = torch.empty_like(h)
-    yr = _rows(y, "y", shape, dt, dev)
-    hnp = _dense(h_new, "h_new", shape, torch.float32, dev)
+        hnp = h_new.data_ptr()
+    else:
+        hnp = _dense(h_new, "h_new", shape, torch.float32, dev)
     st = N.lib().winograd_gated_step(
         _pack_step(code, Nn, C, g[0], g[2], 0, v[0], v[2], 0, o[0], o[2], 0, yr[0], yr[2], 0, hp, hnp),
         _raw_stream(stream))
@@ -240,20 +250,16 @@ def _norm(x, weight, residual, eps, out, r, quant, group, stream):
     if residual is not None:
         rr = _rows(residual, "residual", shape, dt, dev)
         own_r = r is None
-        if own_r:
-            r = _new(x, shape, dt)
-        sr = _rows(r, "r", shape, dt, dev)
+        r, sr = _out(r, "r", x, dt, dev)
     elif r is not None:
         raise ValueError("r is the sum with the residual: there is none")
     wp = _dense(weight, "weight", (C,), dt, dev)
     odt = torch.float8_e4m3fn if quant else dt
     own = out is None
-    if own:
-        out = _new(x, shape, odt)
-    yr = _rows(out, "y", shape, odt, dev)
+    out, yr = _out(out, "y", x, odt, dev)
     scales = None
     if quant:
-        scales = x.new_empty((*shape[:-1], -(-C // group) if group > 0 else 1), dtype=torch.float32)
+        scales = _new_f32(x, *shape[:-1], -(-C // group) if group > 0 else 1)
     st = N.lib().winograd_rms_norm(
         _pack_norm(code, Nn, L, C, *xr, *rr, *sr, *yr, wp, 0 if scales is None else scales.data_ptr(), eps,
                    _E4M3 if quant else code, group), _raw_stream(stream))
@@ -294,10 +300,8 @@ def rms_norm_backward(dy, r, weight, dr=None, eps=1e-6, dx=None, stream=None):
     dd = _NO_ROWS if dr is None else _rows(dr, "dr", shape, dt, dev)
     wp = _dense(weight, "weight", (C,), dt, dev)
     own = dx is None
-    if own:
-        dx = _new(dy, shape, dt)
-    xr = _rows(dx, "dx", shape, dt, dev)
-    dweight = r.new_empty((C,), dtype=torch.float32)
+    dx, xr = _out(dx, "dx", r, dt, dev)
+    dweight = torch.empty_like(weight, dtype=torch.float32)
     need = _size("winograd_rms_norm_workspace", code, Nn, L, C)
     ws = _workspace(need, r)
     st = N.lib().winograd_rms_norm_backward(
@@ -402,10 +406,12 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
     if own:
         if dtype is None:
             dtype = torch.bfloat16 if x8 else xdt
-        y = x.new_empty((M, w.rows), dtype=dtype)
-    elif dtype is not None and dtype != y.dtype:
-        raise TypeError("dtype is that of y")
-    yp, _, ldy = _rows(y, "y", (M, w.rows), y.dtype, dev)
+        y = torch.empty_strided((M, w.rows), (w.rows, 1), dtype=dtype, device=x.device)
+        yp, ldy = y.data_ptr(), w.rows
+    else:
+        if dtype is not None and dtype != y.dtype:
+            raise TypeError("dtype is that of y")
+        yp, _, ldy = _rows(y, "y", (M, w.rows), y.dtype, dev)
     st = N.lib().winograd_matvec_w4(
         _pack_matvec(*w._packed, M, xcode, _code(y, "y"), xp, ldx, sp, groups, yp, ldy), _raw_stream(stream))
     if st != N.WG_OK:

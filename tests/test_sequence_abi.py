@@ -82,6 +82,8 @@ def test_workspaces():
     assert lib.winograd_gated_scan_workspace(2, 1, 5, 5, 0, None) == ARG
     assert lib.winograd_rms_norm_workspace(0, 0, 5, 5, ctypes.byref(size)) == 0
     assert lib.winograd_rms_norm_workspace(0, 1, 5, 1 << 26, ctypes.byref(size)) == UNSUPPORTED
+    assert lib.winograd_rms_norm_workspace(2, 1, 16, 512, ctypes.byref(size)) == 0 and size.value == 0   # one part
+    assert lib.winograd_rms_norm_workspace(2, 1, 17, 512, ctypes.byref(size)) == 0 and size.value == 5 * 512 * 4
 
 
 @pytest.mark.parametrize("status,words,args", [
@@ -103,8 +105,8 @@ def test_norm_refusals(status, words, args):
 
 
 def test_norm_backward_refusals():
-    def call(weight=P, dweight=P, ws=P, nbytes=1 << 20, dx=ROWS):
-        return N.lib().winograd_rms_norm_backward(S._pack_norm_backward(2, 2, 10, 64, *ROWS, *ROWS, *NONE, *dx, weight,
+    def call(weight=P, dweight=P, ws=P, nbytes=1 << 20, dx=(P, 64000, 64)):
+        return N.lib().winograd_rms_norm_backward(S._pack_norm_backward(2, 2, 1000, 64, *ROWS, *ROWS, *NONE, *dx, weight,
                                                                         dweight, 1e-6, ws, nbytes), None)
     assert call(weight=P + 1) == ARG and "weight" in _message()
     assert call(dweight=0) == ARG and "dweight" in _message()
