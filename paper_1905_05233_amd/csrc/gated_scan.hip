@@ -62,12 +62,13 @@ constexpr int64_t kFull = 192;
 // against a second launch); 8 tiles cost 22.6 us walked, 4 + 6 in chunks
 // (gradients of 4 x 1000 x 96 fp32).
 constexpr int64_t kChunked = 512, kMostChunks = 256, kWalked = 4;
-// Threads of a workgroup.  The gradients hold twice the values: with 256 threads two
-// workgroups share a compute unit (64 x 512 x 2048: 204 us, with 512 225); where there
-// is one group a compute unit, more threads keep more loads in flight
-// (16 x 4096 x 512: 127 us with 512, 137 with 256).
-constexpr int kThreads = 512;
-constexpr int grad_threads(int lanes) { return lanes == 8 ? 256 : 512; }
+// Threads of a workgroup.  The gradients hold twice the values: with kGradPairs of them
+// two workgroups share a compute unit (64 x 512 x 2048: 204 us, with 512 threads 225).
+// More threads are better where there is one group a compute unit, for the loads in
+// flight (16 x 4096 x 512: 127 us with 512, 137 with 256), and where their longer tiles
+// save the second launch: training 8 x 400 x 256 bf16 takes 27 us a pass instead of 32,
+// but 3 x 500 x 75 fp16, whose short runs make slow tiles, 39 instead of 32.
+constexpr int kThreads = 512, kGradPairs = 256;
 // Sequences of at most kShort steps take a tile of as many: 37 x 4 x 1024 fp32 takes
 // 11.8 us a call (bound by the host) instead of 16.4.
 constexpr int64_t kShort = 2 * kHeld;
@@ -652,7 +653,9 @@ Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
     p.lanes = dtype == kF32 || L <= kShort || p.split.columns >= 8 * kFull || p.split.columns < 4 * kFull ? 8 : 4;
     const int64_t groups = (p.split.columns + p.lanes - 1) / p.lanes;
     p.split.groups = static_cast<uint32_t>(std::min<int64_t>(groups, 0xffffffffLL));
-    p.threads = L <= kShort ? short_threads(V) : backward ? grad_threads(p.lanes) : kThreads;
+    p.threads = L <= kShort ? short_threads(V) : kThreads;
+    const bool one_launch = C % V == 0 && L <= kWalked * (kThreads / (8 * V) * kHeld);
+    if (backward && L > kShort && p.lanes == 8 && (groups >= kFull || !one_launch)) p.threads = kGradPairs;
     const int64_t tile = p.threads / (p.lanes * V) * kHeld, tiles = (L + tile - 1) / tile;
     int64_t chunks = 1;
     if (groups < kFull && tiles > kWalked) chunks = std::min<int64_t>({tiles, kChunked / groups, kMostChunks});
@@ -719,11 +722,12 @@ template <int D> hipError_t launch_gated_scan_backward_t(const wg_gated_scan_bac
 #define WG_SCAN_CASE(LANES, OUT, FULL)                                                                               \
     if constexpr (LANES == 8 || D != kF32)                                                                           \
         if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
-            constexpr int T = grad_threads(LANES);                                                                   \
-            if (LANES == 8 && ahead.y > 0)                                                                           \
-                scan_grad_kernel<Elem, grad_threads(8), 8, OUT, FULL, true><<<ahead, grad_threads(8), 0, stream>>>(k); \
+            constexpr int T = kThreads, PAIRS = kGradPairs;                                                          \
+            if (LANES == 8 && ahead.y > 0) scan_grad_kernel<Elem, PAIRS, 8, OUT, FULL, true><<<ahead, PAIRS, 0, stream>>>(k); \
             if (LANES == 8 && p.threads == SHORT)                                                                    \
                 scan_grad_kernel<Elem, SHORT, 8, OUT, FULL, false><<<grid, SHORT, 0, stream>>>(k);                   \
+            else if (LANES == 8 && p.threads == PAIRS)                                                               \
+                scan_grad_kernel<Elem, PAIRS, 8, OUT, FULL, false><<<grid, PAIRS, 0, stream>>>(k);                   \
             else scan_grad_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                      \
         }
         WG_SCAN_CASES(WG_SCAN_CASE)

@@ -10,6 +10,11 @@ import sequence_reference as R
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1)
+
+
 def _np(t):
     return t.double().cpu().numpy()
 
@@ -67,9 +72,12 @@ def test_gradients_against_differences():
 @pytest.mark.parametrize("eight_bit", [False, True])
 def test_tokens_follow_the_prompt(eight_bit):
     """Tokens one at a time after a prompt give what the forward pass over all of
-    them gives, with the weights that the 4 bits stand for.  In 16 bits the two
-    differ by roundings to bf16 (2^-8 each) of norms, gates and values; in 8 bits the
-    norms are off by up to 2^-4 each, which sums over 192 channels average."""
+    them gives, with the weights that the 4 bits stand for, to the 2-norm of all
+    tokens.  In 16 bits both start from the same norms; the convolution's
+    transforms put it off by at most 1.4e-2 in bf16, the product and the outputs by
+    2^-8 roundings (some 4e-3), and gate, value and output gate hand that on with
+    slopes of at most 1.1 each: below 4e-2.  In 8 bits a norm is off by up to 2^-4, 2.6%
+    in the mean square, in every product: three times 4.5% at most."""
     from paper_1905_05233_amd.gated_conv import GatedConv
     N, L, C = 3, 20, 64
     layer = GatedConv(C, dtype="bf16", seed=3)
@@ -80,10 +88,11 @@ def test_tokens_follow_the_prompt(eight_bit):
     for start in (1, 2, 11):
         y, _, state = layer.prompt(x[:, :start], eight_bit=eight_bit)
         assert torch.equal(y, full[:, :start])
-        for l in range(start, L):
-            y, _ = layer.step(x[:, l], state, w4)
-            off = (y.float() - full[:, l].float()).abs().max()
-            assert float(off) <= (0.3 if eight_bit else 0.04), (start, l, float(off))
+        tokens = torch.stack([layer.step(x[:, l], state, w4)[0] for l in range(start, L)], 1).double()
+        want = full[:, start:].double()
+        off = float((tokens - want).norm() / want.norm())
+        print(f"[layer] tokens from {start}: {off:.3e}", flush=True)
+        assert off <= (0.135 if eight_bit else 0.04), (start, off)
 
 
 def test_two_layers_train():

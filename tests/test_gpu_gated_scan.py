@@ -10,6 +10,11 @@ from gpu_helpers import TORCH
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1)
+
 # sequences, steps, channels: one of everything, odd channels, steps around the
 # kernels' blocks and tiles, few long rows, many short ones
 SHAPES = [(1, 1, 1), (2, 3, 5), (1, 8, 8), (1, 31, 64), (2, 33, 75), (1, 64, 512), (3, 255, 24), (2, 257, 9),

@@ -9,6 +9,11 @@ from gpu_helpers import TORCH
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1)
+
 E4M3 = torch.float8_e4m3fn
 # rows of x, columns, rows of the matrix
 SHAPES = [(1, 1, 1), (1, 8, 16), (3, 33, 17), (1, 127, 100), (2, 128, 64), (5, 129, 31), (16, 512, 48), (17, 300, 20),

@@ -9,6 +9,11 @@ from gpu_helpers import TORCH
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1)
+
 EPS = 1e-5
 SHAPES = [(1, 1), (3, 5), (7, 8), (1, 64), (16, 512), (5, 75), (33, 100), (9, 1000), (3, 1024), (2, 4099), (2, 8192),
           (1, 30001), (700, 24), (3000, 16)]

@@ -6,6 +6,11 @@ import torch
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1)
+
+
 @pytest.fixture(scope="module")
 def far():
     """bf16 rows whose last one starts some 11 GiB behind the first."""
