@@ -24,7 +24,7 @@
 // What bounds it: memory, for many channels (64 x 512 x 2048 in bf16: 118 us
 // forward, 4.6 TB/s; 204 us backward, 4.6 TB/s), held back where a workgroup's runs
 // are 64 bytes long: a card copies those at 3.8 TB/s, runs of 128 bytes at 4.8.
-// 16 x 4096 x 512, of 64-byte runs: 76 us forward (3.5 TB/s), 113 us backward (4.2).
+// 16 x 4096 x 512, of 64-byte runs: 74 us forward (3.6 TB/s), 114 us backward (4.1).
 // One sequence of 16381 x 512 reads its gates twice: 10 + 15 us, 67 MB of inputs and
 // outputs (2.9 TB/s for the call).  A few short sequences take one tile's latency.
 #include <hip/hip_runtime.h>
@@ -58,9 +58,9 @@ constexpr int64_t kFull = 192;
 // Chunks, where there are fewer groups than kFull: so many that there are kChunked
 // workgroups (16381 x 512 forward: 25.2 us; with 256 28.0, with 1024 26.4), and at
 // most kMostChunks, whose maps each chunk composes (32768 x 64: 16.9 us forward, with
-// 64 chunks 22.0).  Sequences of kWalked tiles or fewer are walked (3 us a tile,
-// against a second launch); 8 tiles cost 22.6 us walked, 4 + 6 in chunks
-// (gradients of 4 x 1000 x 96 fp32).
+// 64 chunks 22.0).  Sequences of kWalked tiles or fewer are walked (3 to 4 us a tile,
+// against a second launch and its workspace, 5 us of the host's time); 8 tiles of the
+// gradients of 4 x 1000 x 96 fp32 cost 22.6 us walked, 4 + 6 in chunks.
 constexpr int64_t kChunked = 512, kMostChunks = 256, kWalked = 4;
 // Threads of a workgroup.  The gradients hold twice the values: with kGradPairs of them
 // two workgroups share a compute unit (64 x 512 x 2048: 204 us, with 512 threads 225).
