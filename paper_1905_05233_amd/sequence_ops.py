@@ -11,7 +11,8 @@ what stands around ``Plan.conv1d`` in a sequence model.
 Tensors are f32, f16 or bf16 on the current GPU.  Rows [N][L][C] may have any
 strides as long as the channels are contiguous (slices of a projection's rows,
 a buffer with a leading row); states, scales and weights are contiguous.  Calls
-are asynchronous on ``stream`` or the current stream.  Outputs must not overlap
+are asynchronous on ``stream`` or the current stream; work that another stream
+has still to do on the inputs is the caller's to wait for.  Outputs must not overlap
 inputs, unless said otherwise.
 """
 import ctypes
@@ -128,13 +129,31 @@ def _workspace(need, like):
     return torch.empty_strided((need,), (1,), dtype=torch.uint8, device=like.device) if need else None
 
 
-def _keep(stream, dev, *tensors):
-    """Memory allocated here on the current stream but used on another one: keep
-    the caching allocator from reusing it before that stream's work is done."""
-    if stream is not None and stream != torch.cuda.current_stream(dev):
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+def _tensors(values):
+    for v in values:
+        if isinstance(v, torch.Tensor):
+            yield v
+        elif isinstance(v, W4Matrix):
+            yield from (v.tiles, v.scales)
+        elif isinstance(v, (tuple, list)):
+            yield from _tensors(v)
+
+
+def _on(stream, call, *args):
+    """call(*args) with ``stream`` as the current one.  What is allocated within belongs
+    to that stream, so that no other stream's work is still to be done on it; the
+    caching allocator is told which other tensors the stream uses, and that the
+    caller's stream uses the results."""
+    caller = torch.cuda.current_stream()
+    if stream == caller:
+        return call(*args)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in _tensors(args):
+        t.record_stream(stream)
+    for t in _tensors((out,)):
+        t.record_stream(caller)
+    return out
 
 
 def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_states=False, stream=None):
@@ -143,6 +162,8 @@ def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_s
     are padding: y is 0 and the state stays).  Returns (y, h_last), h_last fp32
     [N][C] the last state; with ``save_states`` also the fp32 states ahead of every
     SCAN_BLOCK steps, for ``gated_scan_backward``."""
+    if stream is not None:
+        return _on(stream, gated_scan, gate, value, out_gate, h0, lengths, y, save_states)
     dev = _first(gate, "gate", (3,))
     dt, shape = gate.dtype, gate.shape
     code = _code(gate, "gate")
@@ -150,7 +171,6 @@ def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_s
     g = _rows(gate, "gate", shape, dt, dev)
     v = _rows(value, "value", shape, dt, dev)
     o = _NO_ROWS if out_gate is None else _rows(out_gate, "out_gate", shape, dt, dev)
-    own_y = y is None
     y, yr = _out(y, "y", gate, dt, dev)
     h0p = 0 if h0 is None else _dense(h0, "h0", (Nn, C), torch.float32, dev)
     lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
@@ -163,11 +183,9 @@ def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_s
     st = N.lib().winograd_gated_scan(
         _pack_scan(code, Nn, L, C, *g, *v, *o, *yr, h0p, lp, h_last.data_ptr(),
                    0 if states is None else states.data_ptr(), 0 if ws is None else ws.data_ptr(), need),
-        _raw_stream(stream))
+        _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
-    if stream is not None:
-        _keep(stream, dev, y if own_y else None, h_last, states, ws)
     return (y, h_last, states) if save_states else (y, h_last)
 
 
@@ -177,6 +195,8 @@ def gated_scan_backward(dy, gate, value, states, out_gate=None, dh_last=None, le
     it kept them.  Returns (dgate, dvalue, dout_gate, dh0), dout_gate None without
     out_gate.  ``out``: tensors [N][L][C] for the first two or three, as slices of
     the gradient of one projection."""
+    if stream is not None:
+        return _on(stream, gated_scan_backward, dy, gate, value, states, out_gate, dh_last, lengths, out)
     dev = _first(gate, "gate", (3,))
     dt, shape = gate.dtype, gate.shape
     code = _code(gate, "gate")
@@ -188,8 +208,7 @@ def gated_scan_backward(dy, gate, value, states, out_gate=None, dh_last=None, le
     sp = _dense(states, "states", (Nn, -(-L // SCAN_BLOCK), C), torch.float32, dev)
     dhp = 0 if dh_last is None else _dense(dh_last, "dh_last", (Nn, C), torch.float32, dev)
     lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
-    own = out is None
-    if own:
+    if out is None:
         out = (None, None) if out_gate is None else (None, None, None)
     elif len(out) != (2 if out_gate is None else 3):
         raise ValueError("out must hold dgate, dvalue and, with out_gate, dout_gate")
@@ -201,17 +220,17 @@ def gated_scan_backward(dy, gate, value, states, out_gate=None, dh_last=None, le
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan_backward(
         _pack_scan_backward(code, Nn, L, C, *d, *g, *v, *o, *zr, *vr, *outr, sp, dhp, lp, dh0.data_ptr(),
-                            0 if ws is None else ws.data_ptr(), need), _raw_stream(stream))
+                            0 if ws is None else ws.data_ptr(), need), _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
-    if stream is not None:
-        _keep(stream, dev, *((dgate, dvalue, dout_gate) if own else ()), dh0, ws)
     return dgate, dvalue, dout_gate, dh0
 
 
 def gated_step(gate, value, h, out_gate=None, h_new=None, y=None, stream=None):
     """One step for N sequences: gate, value and out_gate [N][C], h fp32 [N][C] the
     states.  Returns (y, h_new); ``h_new=h`` updates the states in place."""
+    if stream is not None:
+        return _on(stream, gated_step, gate, value, h, out_gate, h_new, y)
     dev = _first(gate, "gate", (2,))
     dt, shape = gate.dtype, gate.shape
     code = _code(gate, "gate")
@@ -221,24 +240,21 @@ def gated_step(gate, value, h, out_gate=None, h_new=None, y=None, stream=None):
     v = _rows(value, "value", shape, dt, dev)
     o = _NO_ROWS if out_gate is None else _rows(out_gate, "out_gate", shape, dt, dev)
     hp = _dense(h, "h", shape, torch.float32, dev)
-    own_y, own_h = y is None, h_new is None
     y, yr = _out(y, "y", gate, dt, dev)
-    if own_h:
+    if h_new is None:
         h_new = torch.empty_like(h)
         hnp = h_new.data_ptr()
     else:
         hnp = _dense(h_new, "h_new", shape, torch.float32, dev)
     st = N.lib().winograd_gated_step(
         _pack_step(code, Nn, C, g[0], g[2], 0, v[0], v[2], 0, o[0], o[2], 0, yr[0], yr[2], 0, hp, hnp),
-        _raw_stream(stream))
+        _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
-    if stream is not None:
-        _keep(stream, dev, y if own_y else None, h_new if own_h else None)
     return y, h_new
 
 
-def _norm(x, weight, residual, eps, out, r, quant, group, stream):
+def _norm(x, weight, residual, eps, out, r, quant, group):
     dev = _first(x, "x", (2, 3))
     dt, shape = x.dtype, x.shape
     code = _code(x, "x")
@@ -246,27 +262,22 @@ def _norm(x, weight, residual, eps, out, r, quant, group, stream):
     Nn, L = (1, shape[0]) if len(shape) == 2 else (shape[0], shape[1])
     xr = _rows(x, "x", shape, dt, dev)
     rr = sr = _NO_ROWS
-    own_r = False
     if residual is not None:
         rr = _rows(residual, "residual", shape, dt, dev)
-        own_r = r is None
         r, sr = _out(r, "r", x, dt, dev)
     elif r is not None:
         raise ValueError("r is the sum with the residual: there is none")
     wp = _dense(weight, "weight", (C,), dt, dev)
     odt = torch.float8_e4m3fn if quant else dt
-    own = out is None
     out, yr = _out(out, "y", x, odt, dev)
     scales = None
     if quant:
         scales = _new_f32(x, *shape[:-1], -(-C // group) if group > 0 else 1)
     st = N.lib().winograd_rms_norm(
         _pack_norm(code, Nn, L, C, *xr, *rr, *sr, *yr, wp, 0 if scales is None else scales.data_ptr(), eps,
-                   _E4M3 if quant else code, group), _raw_stream(stream))
+                   _E4M3 if quant else code, group), _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
-    if stream is not None:
-        _keep(stream, dev, out if own else None, r if own_r else None, scales)
     return out, scales, r
 
 
@@ -274,7 +285,9 @@ def rms_norm(x, weight, residual=None, eps=1e-6, y=None, r=None, stream=None):
     """The norm of the rows of x + residual ([N][L][C] or [L][C]), times weight [C].
     Returns (y, r): r is the sum in the storage type (None without a residual); it
     may be given, and be x or the residual itself."""
-    out, _, r = _norm(x, weight, residual, eps, y, r, False, 0, stream)
+    if stream is not None:
+        return _on(stream, rms_norm, x, weight, residual, eps, y, r)
+    out, _, r = _norm(x, weight, residual, eps, y, r, False, 0)
     return out, r
 
 
@@ -282,7 +295,9 @@ def rms_norm_fp8(x, weight, residual=None, eps=1e-6, group=0, y=None, r=None, st
     """``rms_norm`` into 8 bits.  Returns (q, scales, r): q float8_e4m3fn shaped as
     x, scales fp32 [..., G], one for every ``group`` channels (32, 64 or 128) or for
     the row (0); q times its scale is the norm's output."""
-    return _norm(x, weight, residual, eps, y, r, True, group, stream)
+    if stream is not None:
+        return _on(stream, rms_norm_fp8, x, weight, residual, eps, group, y, r)
+    return _norm(x, weight, residual, eps, y, r, True, group)
 
 
 def rms_norm_backward(dy, r, weight, dr=None, eps=1e-6, dx=None, stream=None):
@@ -290,6 +305,8 @@ def rms_norm_backward(dy, r, weight, dr=None, eps=1e-6, dx=None, stream=None):
     gradient that reaches r from elsewhere.  Returns (dx, dweight): dx is the
     gradient of r, and so of x and of the residual; dweight is fp32 [C].  dx may be
     given, and be dy or dr itself."""
+    if stream is not None:
+        return _on(stream, rms_norm_backward, dy, r, weight, dr, eps, dx)
     dev = _first(r, "r", (2, 3))
     dt, shape = r.dtype, r.shape
     code = _code(r, "r")
@@ -299,18 +316,15 @@ def rms_norm_backward(dy, r, weight, dr=None, eps=1e-6, dx=None, stream=None):
     rr = _rows(r, "r", shape, dt, dev)
     dd = _NO_ROWS if dr is None else _rows(dr, "dr", shape, dt, dev)
     wp = _dense(weight, "weight", (C,), dt, dev)
-    own = dx is None
     dx, xr = _out(dx, "dx", r, dt, dev)
     dweight = torch.empty_like(weight, dtype=torch.float32)
     need = _size("winograd_rms_norm_workspace", code, Nn, L, C)
     ws = _workspace(need, r)
     st = N.lib().winograd_rms_norm_backward(
         _pack_norm_backward(code, Nn, L, C, *d, *rr, *dd, *xr, wp, dweight.data_ptr(), eps,
-                            0 if ws is None else ws.data_ptr(), need), _raw_stream(stream))
+                            0 if ws is None else ws.data_ptr(), need), _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
-    if stream is not None:
-        _keep(stream, dev, dx if own else None, dweight, ws)
     return dx, dweight
 
 
@@ -344,12 +358,13 @@ class W4Matrix:
     def quantize(cls, m, group=128, stream=None):
         """m [rows][cols] rounded to the nearest multiples -7 .. 7 of each group's
         scale, bf16(max |m| / 7)."""
+        if stream is not None:
+            return _on(stream, cls.quantize, m, group)
         dev = _first(m, "m", (2,))
         mp, _, ld = _rows(m, "m", m.shape, m.dtype, dev)
         code = _code(m, "m")
         w = cls._empty(m.shape[0], m.shape[1], group, m.device)
-        N.check(N.lib().winograd_quantize_w4(_pack_w4(*w._packed), code, mp, ld, _raw_stream(stream)))
-        _keep(stream, dev, w.tiles, w.scales)
+        N.check(N.lib().winograd_quantize_w4(_pack_w4(*w._packed), code, mp, ld, _raw_stream(None)))
         return w
 
     @classmethod
@@ -357,6 +372,8 @@ class W4Matrix:
         """From codes 0 .. 15 (value code - 8) as checkpoints hold them: uint8
         [rows][ceil(cols/2)], the even column in the lower half, and scales bf16
         [rows][ceil(cols/group)]; the group follows from their number."""
+        if stream is not None:
+            return _on(stream, cls.from_nibbles, nibbles, scales, cols)
         dev = _first(nibbles, "nibbles", (2,))
         rows = nibbles.shape[0]
         np_ = _dense(nibbles, "nibbles", (rows, -(-cols // 2)), torch.uint8, dev)
@@ -367,18 +384,18 @@ class W4Matrix:
             raise ValueError("scales must be [rows][ceil(cols/group)] for a group of 32, 64 or 128")
         sp = _dense(scales, "scales", (rows, scales.shape[1]), torch.bfloat16, dev)
         w = cls._empty(rows, cols, fits[0], nibbles.device)
-        N.check(N.lib().winograd_pack_w4(_pack_w4(*w._packed), np_, sp, _raw_stream(stream)))
-        _keep(stream, dev, w.tiles, w.scales)
+        N.check(N.lib().winograd_pack_w4(_pack_w4(*w._packed), np_, sp, _raw_stream(None)))
         return w
 
     def dequantize(self, dtype=torch.bfloat16, stream=None):
         """The matrix [rows][cols] that the codes and scales stand for."""
+        if stream is not None:
+            return _on(stream, W4Matrix.dequantize, self, dtype)
         m = torch.empty((self.rows, self.cols), dtype=dtype, device=self.tiles.device)
         code = _code(m, "m")
         _first(self.tiles, "tiles", (5,))
         N.check(N.lib().winograd_dequantize_w4(_pack_w4(*self._packed), code, m.data_ptr(), self.cols,
-                                               _raw_stream(stream)))
-        _keep(stream, self.tiles.get_device(), m)
+                                               _raw_stream(None)))
         return m
 
 
@@ -386,6 +403,8 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
     """y [M][rows] = x [M][cols] times the transpose of the ``W4Matrix`` w, for a few
     rows x in f32, f16, bf16 or, with x_scales fp32 [M][1] or [M][groups of w],
     float8_e4m3fn.  y has ``dtype``, by default x's (bf16 for 8 bits)."""
+    if stream is not None:
+        return _on(stream, matvec_w4, x, w, x_scales, y, dtype)
     dev = _first(x, "x", (2,))
     xdt = x.dtype
     x8 = xdt == torch.float8_e4m3fn
@@ -402,8 +421,7 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
         sp = _dense(x_scales, "x_scales", (M, groups), torch.float32, dev)
     elif x_scales is not None:
         raise ValueError("x_scales are for rows in 8 bits")
-    own = y is None
-    if own:
+    if y is None:
         if dtype is None:
             dtype = torch.bfloat16 if x8 else xdt
         y = torch.empty_strided((M, w.rows), (w.rows, 1), dtype=dtype, device=x.device)
@@ -413,9 +431,7 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
             raise TypeError("dtype is that of y")
         yp, _, ldy = _rows(y, "y", (M, w.rows), y.dtype, dev)
     st = N.lib().winograd_matvec_w4(
-        _pack_matvec(*w._packed, M, xcode, _code(y, "y"), xp, ldx, sp, groups, yp, ldy), _raw_stream(stream))
+        _pack_matvec(*w._packed, M, xcode, _code(y, "y"), xp, ldx, sp, groups, yp, ldy), _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
-    if stream is not None and own:
-        _keep(stream, dev, y)
     return y
