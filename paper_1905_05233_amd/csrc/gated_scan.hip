@@ -199,11 +199,11 @@ __device__ __forceinline__ float reach_chunk(const float2* maps, int64_t stride,
     return fmaf(of_last_part<P, true>(A), state, of_last_part<P, true>(B));
 }
 
-// blockIdx.x -> group: workgroups go to the eight XCDs in turn, and the two halves
-// of a 128-byte line (groups of 64 bytes) go to the same one.
-template <int LANES> __device__ __forceinline__ uint32_t group_of_block(uint32_t b) {
-    if (LANES == 8) return b;
-    return (b / 16) * 16 + (b % 8) * 2 + b % 16 / 8;
+// blockIdx.x -> group: workgroups go to the eight XCDs in turn, and each XCD takes
+// adjacent groups, so that lines that two groups share (halves of one, for groups of
+// 64 bytes; any, where rows are no multiple of a line) are fetched into one L2.
+__device__ __forceinline__ uint32_t group_of_block() {
+    return blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
 }
 
 // A thread's place as the owner of steps: its column (a run of V channels) of a
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(T) void scan_kernel(ScanArgs<Elem> a) {
     const int64_t blocks = (static_cast<int64_t>(L) + kScanBlock - 1) / kScanBlock;
     auto start_of = [&](int32_t tile) { return tile * TILE; };
 
-    const uint32_t group = group_of_block<LANES>(blockIdx.x);
+    const uint32_t group = group_of_block();
     if (group >= a.split.groups) return;
     const int chunk = blockIdx.y, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
     Place at = place_of<Elem, LANES>(a.split, a.lengths, L, a.C, group, start_of(chunk * a.split.chunk));
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(T) void scan_grad_kernel(GradArgs<Elem> a) {
     // tiles in the scan's order: 0 is the last one of the sequence
     auto start_of = [&](int32_t tile) { return (a.split.tiles - 1 - tile) * TILE; };
 
-    const uint32_t group = group_of_block<LANES>(blockIdx.x);
+    const uint32_t group = group_of_block();
     if (group >= a.split.groups) return;
     const int chunk = blockIdx.y, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
     Place at = place_of<Elem, LANES>(a.split, a.lengths, L, a.C, group, start_of(chunk * a.split.chunk));
@@ -667,7 +667,7 @@ Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
 }
 
 template <typename F> hipError_t launch_chunks(const Plan& p, F&& launch) {
-    const int64_t x = p.lanes == 8 ? p.split.groups : (static_cast<int64_t>(p.split.groups) + 15) / 16 * 16;
+    const int64_t x = (static_cast<int64_t>(p.split.groups) + 7) / 8 * 8;
     if (x * p.threads > 0xffffffffLL) return hipErrorInvalidValue;
     const unsigned y = static_cast<unsigned>(p.split.chunks);
     // nothing reads the last chunk's map; chunks are of groups of 8 LANES (fewer than kFull groups)

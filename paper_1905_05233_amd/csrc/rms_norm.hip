@@ -5,7 +5,7 @@
 //   dweight = sum over the rows of dy r rstd.
 // Sums and statistics in fp32.
 //
-// Memory bounds all of it, so a row is read once: TPR threads (8 to 1024, by the
+// Memory bounds all of it, so a row is read once: TPR threads (2 to 1024, by the
 // row's length) hold it in registers, NV runs of 16 bytes each, reduce over lanes
 // (and LDS, over waves), and write.  Workgroups walk rows with the weights in
 // registers; the gradients' workgroups also keep their share of dweight there and
@@ -99,7 +99,7 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
 template <typename Elem, bool FULL> __device__ __forceinline__ u32x4 load_one(const Elem* p, const RunShape& shape, int C) {
     u32x4 bits[1]{};
     const Elem* const at[1] = {p};
-    if (!FULL || shape.valid) load_runs<Elem, FULL, 1>(at, shape, C, bits);
+    if (shape.valid) load_runs<Elem, FULL, 1>(at, shape, C, bits);
     return bits[0];
 }
 
@@ -480,6 +480,8 @@ struct Shape {
 };
 Shape shape_of(int dtype, int64_t C) {
     const int64_t runs = (C + 16 / dtype_bytes(dtype) - 1) / (16 / dtype_bytes(dtype));
+    if (runs <= 2) return {2, 1};
+    if (runs <= 4) return {4, 1};
     if (runs <= 8) return {8, 1};
     if (runs <= 16) return {16, 1};
     if (runs <= 32) return {32, 1};
@@ -492,22 +494,27 @@ Shape shape_of(int dtype, int64_t C) {
     if (runs <= 4096) return {1024, 4};
     return {0, 0};
 }
-#define WG_NORM_SHAPES(X) X(8, 1) X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 4) X(256, 2) X(256, 4) X(1024, 2) X(1024, 4)
+#define WG_NORM_SHAPES(X) X(2, 1) X(4, 1) X(8, 1) X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 4) X(256, 2) X(256, 4) X(1024, 2) X(1024, 4)
 
-// Workgroups that walk the rows, as many as compute units hold at a time: eight of 256
-// threads with the norm's registers, four with the gradients'.
+// Workgroups that walk the rows: as many as are resident at a time, by the registers
+// that NV runs a thread take (the norm at most 64, 102 and 170 of them, its gradients
+// 102, 170 and 256).  More would leave a second, mostly empty round: gradients of 38759
+// rows of 516 bf16, 138 registers, take 83 us with four workgroups a compute unit and
+// 64 with three; of 4882 rows of 4096, 51 and 44.
 int64_t walkers(int64_t rows, int tpr, int per_cu) {
     const int block = block_of(tpr), per = block / tpr;
-    return std::max<int64_t>(1, std::min<int64_t>((rows + per - 1) / per, int64_t(device_cu_count()) * per_cu * 256 / block));
+    const int64_t resident = int64_t(device_cu_count()) * std::max(1, per_cu * 256 / block);
+    return std::max<int64_t>(1, std::min<int64_t>((rows + per - 1) / per, resident));
 }
+constexpr int norm_per_cu(int nv) { return nv == 1 ? 8 : nv == 2 ? 5 : 3; }
+constexpr int grad_per_cu(int nv) { return nv == 1 ? 5 : nv == 2 ? 3 : 2; }
 
-constexpr int kNormPerCu = 8, kGradPerCu = 4;
 // The gradients' workgroups.  A few rows are one workgroup's, whose dweight is the
 // whole of it: a round of rows takes some 1 us there, the second launch and its
 // workspace 5 us of the host's time.
 constexpr int64_t kOneRounds = 4;
-int64_t grad_walkers(int64_t rows, int tpr) {
-    return rows <= kOneRounds * (block_of(tpr) / tpr) ? 1 : walkers(rows, tpr, kGradPerCu);
+int64_t grad_walkers(int64_t rows, const Shape& s) {
+    return rows <= kOneRounds * (block_of(s.tpr) / s.tpr) ? 1 : walkers(rows, s.tpr, grad_per_cu(s.nv));
 }
 constexpr int64_t kLongBlocks = 4096, kColumnParts = 64;
 
@@ -518,7 +525,7 @@ size_t rms_norm_workspace(int dtype, int64_t N, int64_t L, int64_t C) {
     const Shape s = shape_of(dtype, C);
     const int64_t rows = N * L;
     if (s.tpr) {
-        const int64_t parts = grad_walkers(rows, s.tpr);
+        const int64_t parts = grad_walkers(rows, s);
         return parts == 1 ? 0 : static_cast<size_t>((parts * C * 4 + 15) / 16 * 16);
     }
     return static_cast<size_t>(((std::min(rows, kColumnParts) * C + rows) * 4 + 15) / 16 * 16 + 16);
@@ -532,7 +539,7 @@ template <int D> hipError_t launch_rms_norm_t(const wg_rms_norm& a, hipStream_t 
                            a.group && a.group < a.C ? a.group : a.C};
     const bool quant = a.y_dtype == WG_E4M3, full = a.C % Vec<Elem>::V == 0;
     const Shape s = shape_of(D, a.C);
-    const unsigned blocks = static_cast<unsigned>(s.tpr ? walkers(rows, s.tpr, kNormPerCu) : std::min(rows, kLongBlocks));
+    const unsigned blocks = static_cast<unsigned>(s.tpr ? walkers(rows, s.tpr, norm_per_cu(s.nv)) : std::min(rows, kLongBlocks));
 #define WG_NORM_CASE(TPR, NV)                                                                     \
     if (s.tpr == TPR && s.nv == NV) {                                                             \
         const unsigned threads = block_of(TPR);                                                   \
@@ -558,7 +565,7 @@ template <int D> hipError_t launch_rms_norm_backward_t(const wg_rms_norm_backwar
     const Shape s = shape_of(D, a.C);
     const unsigned column_blocks = static_cast<unsigned>((a.C + 15) / 16);
     if (s.tpr && rows > 0) {
-        k.parts = grad_walkers(rows, s.tpr);
+        k.parts = grad_walkers(rows, s);
         if (k.parts == 1) k.partial = a.dweight;
         const unsigned blocks = static_cast<unsigned>(k.parts);
 #define WG_NORM_CASE(TPR, NV) \
