@@ -199,11 +199,21 @@ __device__ __forceinline__ float reach_chunk(const float2* maps, int64_t stride,
     return fmaf(of_last_part<P, true>(A), state, of_last_part<P, true>(B));
 }
 
-// blockIdx.x -> group: workgroups go to the eight XCDs in turn, and each XCD takes
-// adjacent groups, so that lines that two groups share (halves of one, for groups of
-// 64 bytes; any, where rows are no multiple of a line) are fetched into one L2.
-__device__ __forceinline__ uint32_t group_of_block() {
-    return blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+// Which (chunk, group) a workgroup takes, all groups of chunk 0 first.  Workgroups go
+// to the eight XCDs in turn.  Where groups share lines (halves of one, for groups of 64
+// bytes; any, where a row is no whole number of groups), each XCD takes a run of the
+// order instead, so that a line is fetched into one L2: 12 x 4000 x 136 bf16 24 us, in
+// turn 32; 16 x 4096 x 512 in groups of 64 bytes 74 and 87.  Where they do not, in turn
+// is better (16381 x 512: 23.4 us, in runs 25.3).
+struct Share {
+    uint32_t group;
+    int chunk;   // from `chunks` on: none
+};
+template <int LANES> __device__ __forceinline__ Share share_of_block(const Split& split, int chunks) {
+    const bool apart = LANES == 8 && split.runs % LANES == 0;
+    const uint32_t id = apart ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+    const uint32_t chunk = id / split.groups;
+    return {id - chunk * split.groups, chunk < static_cast<uint32_t>(chunks) ? static_cast<int>(chunk) : chunks};
 }
 
 // A thread's place as the owner of steps: its column (a run of V channels) of a
@@ -280,9 +290,11 @@ __global__ __launch_bounds__(T) void scan_kernel(ScanArgs<Elem> a) {
     const int64_t blocks = (static_cast<int64_t>(L) + kScanBlock - 1) / kScanBlock;
     auto start_of = [&](int32_t tile) { return tile * TILE; };
 
-    const uint32_t group = group_of_block();
-    if (group >= a.split.groups) return;
-    const int chunk = blockIdx.y, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
+    const int chunks = a.split.chunks - (MAPS ? 1 : 0);   // nothing reads the last chunk's map
+    const Share share = share_of_block<LANES>(a.split, chunks);
+    if (share.chunk == chunks) return;
+    const uint32_t group = share.group;
+    const int chunk = share.chunk, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
     Place at = place_of<Elem, LANES>(a.split, a.lengths, L, a.C, group, start_of(chunk * a.split.chunk));
     const Scanner sc = scanner_of<Elem, LANES>(a.split, a.C, group, channel);
     const int64_t map_stride = static_cast<int64_t>(a.split.groups) * CH;
@@ -437,9 +449,11 @@ __global__ __launch_bounds__(T) void scan_grad_kernel(GradArgs<Elem> a) {
     // tiles in the scan's order: 0 is the last one of the sequence
     auto start_of = [&](int32_t tile) { return (a.split.tiles - 1 - tile) * TILE; };
 
-    const uint32_t group = group_of_block();
-    if (group >= a.split.groups) return;
-    const int chunk = blockIdx.y, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
+    const int chunks = a.split.chunks - (MAPS ? 1 : 0);   // nothing reads the last chunk's map
+    const Share share = share_of_block<LANES>(a.split, chunks);
+    if (share.chunk == chunks) return;
+    const uint32_t group = share.group;
+    const int chunk = share.chunk, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
     Place at = place_of<Elem, LANES>(a.split, a.lengths, L, a.C, group, start_of(chunk * a.split.chunk));
     const Scanner sc = scanner_of<Elem, LANES>(a.split, a.C, group, channel);
     const int64_t map_stride = static_cast<int64_t>(a.split.groups) * CH;
@@ -667,11 +681,10 @@ Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
 }
 
 template <typename F> hipError_t launch_chunks(const Plan& p, F&& launch) {
-    const int64_t x = (static_cast<int64_t>(p.split.groups) + 7) / 8 * 8;
-    if (x * p.threads > 0xffffffffLL) return hipErrorInvalidValue;
-    const unsigned y = static_cast<unsigned>(p.split.chunks);
-    // nothing reads the last chunk's map; chunks are of groups of 8 LANES (fewer than kFull groups)
-    launch(dim3(static_cast<unsigned>(x), y - 1), dim3(static_cast<unsigned>(x), y));
+    const int64_t groups = p.split.groups, chunks = p.split.chunks;
+    const int64_t blocks = (groups * chunks + 7) / 8 * 8, ahead = (groups * (chunks - 1) + 7) / 8 * 8;
+    if (blocks * p.threads > 0xffffffffLL) return hipErrorInvalidValue;
+    launch(static_cast<unsigned>(ahead), static_cast<unsigned>(blocks));
     return hipGetLastError();
 }
 
@@ -695,12 +708,12 @@ template <int D> hipError_t launch_gated_scan_t(const wg_gated_scan& a, hipStrea
                            rows_of<const Elem>(a.value), rows_of<const Elem>(a.out_gate), rows_of<Elem>(a.y), a.h0,
                            a.lengths, a.h_last, a.states, static_cast<float2*>(a.workspace), p.split};
     const bool out = a.out_gate.data != nullptr, full = a.C % Vec<Elem>::V == 0;
-    return launch_chunks(p, [&](dim3 ahead, dim3 grid) {
+    return launch_chunks(p, [&](unsigned ahead, unsigned grid) {
 #define WG_SCAN_CASE(LANES, OUT, FULL)                                                                               \
     if constexpr (LANES == 8 || D != kF32)                                                                           \
         if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
             constexpr int T = kThreads;                                                                              \
-            if (LANES == 8 && ahead.y > 0) scan_kernel<Elem, T, 8, false, FULL, true><<<ahead, T, 0, stream>>>(k);   \
+            if (LANES == 8 && ahead > 0) scan_kernel<Elem, T, 8, false, FULL, true><<<ahead, T, 0, stream>>>(k);   \
             if (LANES == 8 && p.threads == SHORT) scan_kernel<Elem, SHORT, 8, OUT, FULL, false><<<grid, SHORT, 0, stream>>>(k); \
             else scan_kernel<Elem, T, LANES, OUT, FULL, false><<<grid, T, 0, stream>>>(k);                           \
         }
@@ -718,12 +731,12 @@ template <int D> hipError_t launch_gated_scan_backward_t(const wg_gated_scan_bac
                            rows_of<Elem>(a.dgate), rows_of<Elem>(a.dvalue), rows_of<Elem>(a.dout_gate), a.states,
                            a.dh_last, a.lengths, a.dh0, static_cast<float2*>(a.workspace), p.split};
     const bool out = a.out_gate.data != nullptr, full = a.C % Vec<Elem>::V == 0;
-    return launch_chunks(p, [&](dim3 ahead, dim3 grid) {
+    return launch_chunks(p, [&](unsigned ahead, unsigned grid) {
 #define WG_SCAN_CASE(LANES, OUT, FULL)                                                                               \
     if constexpr (LANES == 8 || D != kF32)                                                                           \
         if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
             constexpr int T = kThreads, PAIRS = kGradPairs;                                                          \
-            if (LANES == 8 && ahead.y > 0) scan_grad_kernel<Elem, PAIRS, 8, OUT, FULL, true><<<ahead, PAIRS, 0, stream>>>(k); \
+            if (LANES == 8 && ahead > 0) scan_grad_kernel<Elem, PAIRS, 8, OUT, FULL, true><<<ahead, PAIRS, 0, stream>>>(k); \
             if (LANES == 8 && p.threads == SHORT)                                                                    \
                 scan_grad_kernel<Elem, SHORT, 8, OUT, FULL, false><<<grid, SHORT, 0, stream>>>(k);                   \
             else if (LANES == 8 && p.threads == PAIRS)                                                               \
