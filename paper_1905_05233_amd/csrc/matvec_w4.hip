@@ -46,8 +46,8 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
     return static_cast<int>(v >> (4 * (j / 2) + 16 * (j % 2)) & 15u);
 }
 
-// The product on the matrix cores.  A workgroup multiplies a tile of 16 rows of the
-// matrix with up to 16 rows of x (v_mfma_f32_16x16x32: 32 columns an instruction);
+// The product on the matrix cores.  A workgroup multiplies one or two tiles of 16 rows
+// of the matrix with up to 16 rows of x (v_mfma_f32_16x16x32: 32 columns an instruction);
 // a lane's 16 bytes of a tile of 128 columns are its fragments for four of them.
 //
 // A code becomes a 16-bit float without arithmetic: four bits at bit 3 of the
@@ -64,19 +64,21 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
 // The waves of a workgroup take the tiles of columns in turn, each wave's next tile
 // in flight (two or more ahead are no faster: 25088 -> 4096 14.2 us with one, 15.8
 // with two), and their sums are added in a fixed order at the end; how many
-// waves depends on the matrix alone, so that an output does not depend on the
-// other rows of x.
+// waves depends on the matrix alone, and the order of an output's sums not on the
+// tiles of its workgroup, so that an output does not depend on the other rows of x.
 //
 // Measured: 25088 -> 4096 for one bf16 row, 53 MB, 12.7 us a call: 4.2 TB/s; it is
 // bound by memory and the waves' start and end (a copy moves as much in 10.2).  4096 ->
 // 1000 for five fp32 rows 8 us, 1536 -> 1536 for sixteen 8-bit rows 5 us: latency, 63 and
-// 96 workgroups.  Sixteen rows take twice as long as one where the matrix is large
-// (30 against 14 us): every workgroup reads all of x through its L1.
+// 96 workgroups.  Sixteen rows of 25088 take twice as long as one (30 against 14 us):
+// every workgroup reads all of x through its L1.  4096 -> 32768 takes 20.4 us on the GPU
+// for one row and 26.9 for sixteen, 69 MB: 3.4 and 2.6 TB/s.
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kTokens = 16;     // rows of x that a wave takes
+constexpr int kUnits = 256;     // compute units of the chip
 
 template <bool F16> __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, const f32x4& c) {
     if constexpr (F16)
@@ -164,31 +166,39 @@ struct MatvecArgs {
     int y_dtype;
 };
 
-// GPT: groups of a tile of 128 columns; XG: x's scales go by groups.
-template <int XD, int GPT, bool XG>
+// GPT: groups of a tile of 128 columns; XG: x's scales go by groups; RT: tiles of 16
+// rows of the matrix that a workgroup multiplies with the same x.
+template <int XD, int GPT, bool XG, int RT>
 __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
     using X = typename XTypeOf<XD>::type;
     constexpr bool F16 = XD == 1;
     constexpr int SPG = 4 / GPT;   // instructions of a group
-    extern __shared__ float sums[];   // [wave][lane][4]
+    extern __shared__ float sums[];   // [wave][tile of rows][lane][4]
     const W4& w = a.w;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     const int quarter = lane / 16;
-    const int64_t rt = blockIdx.x;
     const int ktiles = static_cast<int>(w.ktiles);
-    const u32x4* codes = reinterpret_cast<const u32x4*>(w.codes) + rt * w.ktiles * 64 + lane;
-    const u32x2* scales = reinterpret_cast<const u32x2*>(w.scales + rt * w.groups * 16) + quarter;
+    const u32x4* codes[RT];
+    const u32x2* scales[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        // past the last tile of rows that one is taken again, and not stored
+        const int64_t rt = min(static_cast<int64_t>(blockIdx.x) * RT + r, (w.rows - 1) / 16);
+        codes[r] = reinterpret_cast<const u32x4*>(w.codes) + rt * w.ktiles * 64 + lane;
+        scales[r] = reinterpret_cast<const u32x2*>(w.scales + rt * w.groups * 16) + quarter;
+    }
     // past the last row of x the last one is taken again: outputs do not mix, and none is stored
     const int64_t row = min(static_cast<int64_t>(blockIdx.y) * kTokens + lane % 16, a.M - 1);
     const X* x = static_cast<const X*>(a.x) + row * a.ldx + 8 * quarter;
     const float* xs = XG ? a.x_scales + row * a.x_groups : nullptr;
 
     struct Tile {
-        u32x4 codes;
+        u32x4 codes[RT];
         XRun<X> x[4];
     };
     auto load = [&](int kt, Tile& tile) {
-        tile.codes = codes[static_cast<int64_t>(kt) * 64];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) tile.codes[r] = codes[r][static_cast<int64_t>(kt) * 64];
         const X* xk = x + static_cast<int64_t>(kt) * 128;
         const int64_t left = w.cols - static_cast<int64_t>(kt) * 128;
         if (left >= 128) {
@@ -199,11 +209,13 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
             for (int s = 0; s < 4; ++s) tile.x[s] = load_x(xk + 32 * s, left - 32 * s - 8 * quarter);
         }
     };
-    f32x4 acc{0, 0, 0, 0};
+    f32x4 acc[RT] = {};
     Tile tile;
     load(wave, tile);   // there are at least as many tiles as waves
     for (int kt = wave; kt < ktiles; kt += waves) {
-        const u32x4 cur = tile.codes;
+        u32x4 cur[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) cur[r] = tile.codes[r];
         u32x4 xp[4][kPlanes<XD>];
 #pragma unroll
         for (int s = 0; s < 4; ++s) widen_x<XD>(tile.x[s], xp[s]);
@@ -212,37 +224,42 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
         for (int g = 0; g < GPT; ++g) {
             // groups past the matrix's last one have no columns
             const int64_t group = min(static_cast<int64_t>(kt) * GPT + g, w.groups - 1);
-            const u32x2 sc = scales[group * 4];
             const u32x4 offset{kOffset<F16>, kOffset<F16>, kOffset<F16>, kOffset<F16>};
-            f32x4 sum{0, 0, 0, 0};
+            f32x4 start{0, 0, 0, 0};
             if constexpr (XD != 0) {
 #pragma unroll
-                for (int s = g * SPG; s < (g + 1) * SPG; ++s) sum = mma<F16>(offset, xp[s][0], sum);
-            }
-#pragma unroll
-            for (int s = g * SPG; s < (g + 1) * SPG; ++s) {
-                const u32x4 frag = XD == 0 ? exact_codes(cur[s]) : widen_codes<F16>(cur[s]);
-#pragma unroll
-                for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(frag, xp[s][part], sum);
+                for (int s = g * SPG; s < (g + 1) * SPG; ++s) start = mma<F16>(offset, xp[s][0], start);
             }
             const float by = XG ? xs[group] : 1.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float f = __uint_as_float(i % 2 ? sc[i / 2] & 0xffff0000u : sc[i / 2] << 16);
-                if (XG) f *= by;
-                acc[i] = fmaf(f, sum[i], acc[i]);
+            for (int r = 0; r < RT; ++r) {
+                const u32x2 sc = scales[r][group * 4];
+                f32x4 sum = start;
+#pragma unroll
+                for (int s = g * SPG; s < (g + 1) * SPG; ++s) {
+                    const u32x4 frag = XD == 0 ? exact_codes(cur[r][s]) : widen_codes<F16>(cur[r][s]);
+#pragma unroll
+                    for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(frag, xp[s][part], sum);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float f = __uint_as_float(i % 2 ? sc[i / 2] & 0xffff0000u : sc[i / 2] << 16);
+                    if (XG) f *= by;
+                    acc[r][i] = fmaf(f, sum[i], acc[r][i]);
+                }
             }
         }
     }
-    *reinterpret_cast<f32x4*>(sums + (wave * 64 + lane) * 4) = acc;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(sums + ((wave * RT + r) * 64 + lane) * 4) = acc[r];
     __syncthreads();
-    // an output a thread: [quarter][row of x][row in the quarter]
-    for (int id = threadIdx.x; id < 256; id += blockDim.x) {
-        const int64_t j = rt * 16 + id / 64 * 4 + id % 4;
+    // an output a thread: [tile of rows][quarter][row of x][row in the quarter]
+    for (int id = threadIdx.x; id < RT * 256; id += blockDim.x) {
+        const int64_t j = (static_cast<int64_t>(blockIdx.x) * RT + id / 256) * 16 + id % 256 / 64 * 4 + id % 4;
         const int64_t m = static_cast<int64_t>(blockIdx.y) * kTokens + id % 64 / 4;
         if (m >= a.M || j >= w.rows) continue;
         float s = 0.0f;
-        for (int k = 0; k < waves; ++k) s += sums[k * 256 + id];
+        for (int k = 0; k < waves; ++k) s += sums[k * RT * 256 + id];
         if (XD == 3 && !XG) s *= a.x_scales[m];
         const int64_t at = m * a.ldy + j;
         if (a.y_dtype == 0) static_cast<float*>(a.y)[at] = s;
@@ -316,13 +333,27 @@ hipError_t blocks_for(int64_t threads, unsigned* blocks) {
     return hipSuccess;
 }
 
-template <int XD, int GPT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hipStream_t stream) {
-    const int64_t x = (k.w.rows + 15) / 16, y = (k.M + kTokens - 1) / kTokens;
+template <int XD, int GPT, bool XG, int RT> hipError_t matvec_r(const MatvecArgs& k, hipStream_t stream) {
+    const int64_t x = (k.w.rows + 16 * RT - 1) / (16 * RT), y = (k.M + kTokens - 1) / kTokens;
     const int waves = static_cast<int>(k.w.ktiles < 16 ? k.w.ktiles : 16);
     if (x * waves * 64 > 0xffffffffLL || y > 0xffff) return hipErrorInvalidValue;
-    matvec_kernel<XD, GPT, XG><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), waves * 64,
-                                 waves * 256 * sizeof(float), stream>>>(k);
+    matvec_kernel<XD, GPT, XG, RT><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), waves * 64,
+                                 waves * RT * 256 * sizeof(float), stream>>>(k);
     return hipGetLastError();
+}
+template <int XD, int GPT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hipStream_t stream) {
+    // Two tiles of rows a workgroup where one each would be more workgroups than the
+    // chip has units, of which one holds one workgroup of sixteen waves at these
+    // registers: the second round of them is gone, and x is read half as often.
+    // One, then two: 4096 -> 5000 for one bf16 row 7.4, 6.1 us, for sixteen 12.1, 8.4;
+    // 4096 -> 32768 24.1, 20.4 and 41.1, 26.9; 1000 -> 12000 5.9, 4.9.  With fewer workgroups
+    // units are left idle (4096 -> 4096 4.8, 6.0); with fewer than eight waves more
+    // workgroups share a unit (512 -> 8192 3.6, 3.9); fp32 rows with groups of 32 spill
+    // 28 registers (4096 -> 5000 15.2, 16.6).
+    if constexpr (XD != 0 || GPT != 4)
+        if (k.w.ktiles >= 8 && (k.w.rows + 15) / 16 * ((k.M + kTokens - 1) / kTokens) > kUnits)
+            return matvec_r<XD, GPT, XG, 2>(k, stream);
+    return matvec_r<XD, GPT, XG, 1>(k, stream);
 }
 template <int XD, bool XG> hipError_t matvec_x(const MatvecArgs& k, hipStream_t stream) {
     return k.w.group == 32 ? matvec_t<XD, 4, XG>(k, stream)

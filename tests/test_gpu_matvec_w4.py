@@ -77,6 +77,38 @@ def test_matvec(shape, dtype):
                 R.assert_close(_np(y), xv @ ref.T, _bound(xv, 32 * scale_max, K), od, (shape, dtype, group, od))
 
 
+# more tiles of 16 rows (with those of 16 rows of x) than the chip has units, odd and even
+# in number, by few and many columns
+MANY_TILES = [(1, 1000, 4111), (16, 1409, 4097), (3, 900, 4112), (33, 1030, 1400), (5, 512, 4500), (100, 1100, 601)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "fp8"])
+@pytest.mark.parametrize("shape", MANY_TILES, ids=str)
+def test_matvec_of_many_tiles(shape, dtype):
+    """Against the reference, and bit for bit what the same rows of the matrix give
+    in a smaller one for one row of x."""
+    from paper_1905_05233_amd import sequence_ops as S
+    M, K, rows = shape
+    for group in (32, 64, 128):
+        print(f"[w4 many] {shape} {dtype} {group}", flush=True)
+        w, ref = _matrix(rows, K, group, seed=K + group)
+        groups = -(-K // group)
+        scale_max = np.repeat(_np(w.scales).transpose(0, 2, 1).reshape(-1, groups)[:rows], group, 1)[:, :K]
+        for xg in ((1, groups) if dtype == "fp8" else (1,)):
+            x, xs, xv = _x(M, K, dtype, seed=M, groups=xg)
+            if dtype == "fp8":
+                xv = xv[0] * (xv[1] if xg == 1 else np.repeat(xv[1], group, 1)[:, :K])
+            y = S.matvec_w4(x, w, x_scales=xs, dtype=torch.float32)
+            R.assert_close(_np(y), xv @ ref.T, _bound(xv, 32 * scale_max, K), "f32", (shape, dtype, group, xg))
+            first = max(0, rows // 16 - 2) * 16
+            part = S.W4Matrix._empty(rows - first, K, group, "cuda")
+            part.tiles.copy_(w.tiles[first // 16:])
+            part.scales.copy_(w.scales[first // 16:])
+            for m in {0, M - 1}:
+                one = S.matvec_w4(x[m:m + 1], part, x_scales=None if xs is None else xs[m:m + 1], dtype=torch.float32)
+                assert torch.equal(one[0], y[m, first:]), (shape, dtype, group, m)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_matvec_exact_on_small_integers(dtype):
     """Codes, scales that are powers of two and small whole numbers: every sum is
