@@ -95,6 +95,19 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
     return (m < kFp8Least ? kFp8Least : m) / kFp8Max;
 }
 
+// Quotients by a scale: the product with 1 / s, corrected by what it leaves of y.
+// Alone the product is up to 1.5 units of the last place off, which moves quotients at the
+// ties of the 8-bit rounding; corrected they are exact there.  (65536 rows of 512: 45 us
+// with the product alone, 46 with this, 48 with the compiler's division.)
+struct ByScale {
+    float inv, s;   // s 0 where it is infinite: finite values are 0 then
+    __device__ __forceinline__ explicit ByScale(float scale) : inv(1.0f / scale), s(inv == 0.0f ? 0.0f : scale) {}
+    __device__ __forceinline__ float operator()(float y) const {
+        const float q = y * inv;
+        return fmaf(-fmaf(q, s, -y), inv, q);   // in these signs -0 stays -0
+    }
+};
+
 // FULL: the row's channels are whole runs.
 template <typename Elem, bool FULL> __device__ __forceinline__ u32x4 load_one(const Elem* p, const RunShape& shape, int C) {
     u32x4 bits[1]{};
@@ -211,12 +224,13 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
 #pragma unroll
                 for (int j = 1; j < NV; ++j) m = top[j] > m ? top[j] : m;
                 m = RowReduce<TPR>::max(m, lds, slot + 1);
-                const float scale = scale_of(m), inv = 1.0f / scale;
+                const float scale = scale_of(m);
+                const ByScale code(scale);
                 if (lane == 0) a.scales[row] = scale;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
 #pragma unroll
-                    for (int q = 0; q < V; ++q) r[j][q] *= inv;
+                    for (int q = 0; q < V; ++q) r[j][q] = code(r[j][q]);
                     if (shape[j].valid) store_e4m3<V>(y + (j * TPR + lane) * V, shape[j].valid, r[j]);
                 }
             } else {
@@ -229,11 +243,12 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs<Elem> a) {
                     if (per > 4) o = other_half<8>(m), m = o > m ? o : m;
                     if (per > 8) o = other_half<16>(m), m = o > m ? o : m;
                     if (per > 16) o = other_half<32>(m), m = o > m ? o : m;
-                    const float scale = scale_of(m), inv = 1.0f / scale;
+                    const float scale = scale_of(m);
+                    const ByScale code(scale);
                     const int c = (j * TPR + lane) * V;
                     if (lane % per == 0 && shape[j].valid) a.scales[row * groups + c / static_cast<int>(a.group)] = scale;
 #pragma unroll
-                    for (int q = 0; q < V; ++q) r[j][q] *= inv;
+                    for (int q = 0; q < V; ++q) r[j][q] = code(r[j][q]);
                     if (shape[j].valid) store_e4m3<V>(y + c, shape[j].valid, r[j]);
                 }
             }
@@ -282,10 +297,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_long_kernel(NormArgs<Elem> 
                 top = lanes_max<64>(top);
                 if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
                 __syncthreads();
-                const float scale = scale_of(max(max(tops[0], tops[1]), max(tops[2], tops[3]))), inv = 1.0f / scale;
+                const float scale = scale_of(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+                const ByScale code(scale);
                 __syncthreads();
                 for (int64_t c = g * a.group + threadIdx.x; c < end; c += kNormThreads)
-                    y[c] = e4m3_of(sum_at(c) * rstd * S::to_f32(a.weight[c]) * inv);
+                    y[c] = e4m3_of(code(sum_at(c) * rstd * S::to_f32(a.weight[c])));
                 if (threadIdx.x == 0) a.scales[row * groups + g] = scale;
             }
         }
