@@ -75,7 +75,7 @@ class GatedConv:
         dn = self.plan.conv1d(rows, flipped)[:, 1:]
         dx, dnorm = S.rms_norm_backward(dn, r, self.norm_weight, dr=dr, eps=self.eps)
         dweight = torch.zeros((3 * C, 3, C), dtype=torch.float32, device=dy.device)
-        for j in range(min(3, L)):   # tap j meets the token 2 - j steps back
+        for j in range(3):   # tap j meets the token 2 - j steps back
             back = 2 - j
             if back >= L:
                 continue
