@@ -111,14 +111,16 @@ class GatedConv:
         return S.W4Matrix.quantize(self.weight.view(3 * self.C, 3 * self.C), group)
 
     def step(self, x, state, w4, residual=None):
-        """One token x [N][C] of each sequence; the state is updated in place."""
+        """One token x [N][C] of each sequence; the state is updated in its own memory,
+        so that a captured step can be replayed."""
         N, C = x.shape
         if state.scales is not None:
             bits = state.window.view(torch.uint8)
             bits[:, :2] = bits[:, 1:].clone()
             _, scales, r = S.rms_norm_fp8(x, self.norm_weight, residual=residual, eps=self.eps, group=w4.group,
                                           y=state.window[:, 2])
-            state.scales = torch.cat((state.scales[:, 1:], scales[:, None]), 1)
+            state.scales[:, :2] = state.scales[:, 1:].clone()
+            state.scales[:, 2] = scales
             u = S.matvec_w4(state.window.view(N, 3 * C), w4, x_scales=state.scales.view(N, -1), dtype=self.tdt)
         else:
             state.window[:, :2] = state.window[:, 1:].clone()

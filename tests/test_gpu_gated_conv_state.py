@@ -1,0 +1,64 @@
+"""The state that the example layer's single tokens keep: updated in its own
+memory, so that a captured step replays."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1)
+
+
+def _layer(C, eight_bit):
+    from paper_1905_05233_amd.gated_conv import GatedConv
+    layer = GatedConv(C, dtype="bf16", seed=3)
+    w4 = layer.quantize(group=64)
+    prompt = torch.randn((3, 5, C), device="cuda").bfloat16()
+    return layer, w4, lambda: layer.prompt(prompt, eight_bit=eight_bit)[2]
+
+
+def _parts(state):
+    return [state.window.view(torch.uint8), state.h] + ([] if state.scales is None else [state.scales])
+
+
+@pytest.mark.parametrize("eight_bit", [False, True])
+def test_step_keeps_the_states_memory(eight_bit):
+    layer, w4, start = _layer(64, eight_bit)
+    state = start()
+    held = [state.window, state.h, state.scales]
+    at = [t.data_ptr() for t in _parts(state)]
+    for _ in range(3):
+        layer.step(torch.randn((3, 64), device="cuda").bfloat16(), state, w4)
+    assert [t.data_ptr() for t in _parts(state)] == at
+    assert all(a is b for a, b in zip(held, (state.window, state.h, state.scales)))
+
+
+@pytest.mark.parametrize("eight_bit", [False, True])
+def test_captured_step(eight_bit):
+    """Tokens through replays of one captured step are those of eager steps, bit for bit."""
+    C = 64
+    layer, w4, start = _layer(C, eight_bit)
+    tokens = torch.randn((6, 3, C), device="cuda").bfloat16()
+    residuals = torch.randn((6, 3, C), device="cuda").bfloat16()
+    eager, want = start(), []
+    for x, res in zip(tokens, residuals):
+        y, r = layer.step(x, eager, w4, residual=res)
+        want.append((y.clone(), r.clone()))
+
+    state = start()
+    x, res = tokens[0].clone(), residuals[0].clone()
+    layer.step(x, start(), w4, residual=res)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, r = layer.step(x, state, w4, residual=res)
+    for k in range(6):
+        x.copy_(tokens[k])
+        res.copy_(residuals[k])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[k][0]) and torch.equal(r, want[k][1]), k
+    for a, b in zip(_parts(state), _parts(eager)):
+        assert torch.equal(a, b)
