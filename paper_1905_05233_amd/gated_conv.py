@@ -110,9 +110,21 @@ class GatedConv:
         """The convolution's weights in 4 bits, as the matrix of the last three tokens."""
         return S.W4Matrix.quantize(self.weight.view(3 * self.C, 3 * self.C), group)
 
+    def _check_step(self, x, state, w4, residual):
+        """What the calls of a step would refuse, before any of them changes the state."""
+        dev, shape = S._first(x, "x", (2,)), state.h.shape
+        S._rows(x, "x", shape, self.tdt, dev)
+        if residual is not None:
+            S._rows(residual, "residual", shape, self.tdt, dev)
+        if (w4.rows, w4.cols) != (3 * self.C, 3 * self.C) or w4.tiles.get_device() != dev:
+            raise ValueError("w4 must be the layer's matrix, on the GPU of the tokens")
+        if state.scales is not None and state.scales.shape[2] * w4.group != self.C:
+            raise ValueError("the state's scales must go by the groups of w4")
+
     def step(self, x, state, w4, residual=None):
         """One token x [N][C] of each sequence; the state is updated in its own memory,
         so that a captured step can be replayed."""
+        self._check_step(x, state, w4, residual)
         N, C = x.shape
         if state.scales is not None:
             bits = state.window.view(torch.uint8)

@@ -62,3 +62,25 @@ def test_captured_step(eight_bit):
         assert torch.equal(y, want[k][0]) and torch.equal(r, want[k][1]), k
     for a, b in zip(_parts(state), _parts(eager)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("what", ["group", "layer", "x", "tokens", "residual"])
+def test_refused_step_leaves_the_state(what):
+    layer, w4, start = _layer(128, True)
+    state = start()
+    x, res = torch.randn((3, 128), device="cuda").bfloat16(), None
+    if what == "group":
+        w4 = layer.quantize(group=32)
+    elif what == "layer":
+        w4 = _layer(64, True)[1]
+    elif what == "x":
+        x = x.float()
+    elif what == "tokens":
+        x = x[:2]
+    else:
+        res = torch.randn((3, 64), device="cuda").bfloat16()
+    before = [t.clone() for t in _parts(state)]
+    with pytest.raises((ValueError, TypeError)):
+        layer.step(x, state, w4, residual=res)
+    for a, b in zip(_parts(state), before):
+        assert torch.equal(a, b)
