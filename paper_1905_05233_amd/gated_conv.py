@@ -35,6 +35,11 @@ class State:
         self.window, self.scales, self.h = window, scales, h
 
 
+def _live(lengths, L):
+    """Which steps [N][L][1] are none of the padding."""
+    return (torch.arange(L, device=lengths.device)[None] < lengths[:, None])[:, :, None]
+
+
 class GatedConv:
     def __init__(self, C, dtype="bf16", moduli=F2_LINEAR, m=2, eps=1e-6, seed=0, device="cuda"):
         self.C, self.eps, self.tdt = C, eps, TORCH_DTYPES[dtype]
@@ -46,6 +51,13 @@ class GatedConv:
 
     def _forward(self, x, residual, lengths, h0, save):
         N, L, C = x.shape
+        if lengths is not None:
+            # the convolution's tiles of steps mix live ones with padding behind them, where
+            # a product with zero would not remove NaN or infinities
+            S._dense(lengths, "lengths", (N,), torch.int32, x.get_device())
+            live = _live(lengths, L)
+            x = torch.where(live, x, 0)
+            residual = None if residual is None else torch.where(live, residual, 0)
         rows = x.new_empty((N, L + 1, C))
         rows[:, 0].zero_()
         n, r = S.rms_norm(x, self.norm_weight, residual=residual, eps=self.eps, y=rows[:, 1:])
@@ -56,13 +68,14 @@ class GatedConv:
 
     def forward(self, x, residual=None, lengths=None):
         """y [N][L][C] and r, which the next layer takes as its residual, and what
-        ``backward`` needs."""
+        ``backward`` needs.  lengths int32 [N]: steps from there on are padding; nothing
+        there is used, and y and r are 0."""
         n, r, gates, (y, _, states) = self._forward(x, residual, lengths, None, True)
         return y, r, (n, r, gates, states, lengths)
 
     def backward(self, dy, saved, dr=None):
         """Gradients from dy (and dr, what reaches r from later layers): (dx, of x and
-        of the residual; dweight fp32 [3C][3][C]; dnorm_weight fp32 [C])."""
+        of the residual, 0 at padding; dweight fp32 [3C][3][C]; dnorm_weight fp32 [C])."""
         n, r, (gate, value, out_gate), states, lengths = saved
         N, L, C = dy.shape
         # the convolution's gradient by its input is a convolution with the taps in
@@ -73,6 +86,10 @@ class GatedConv:
         S.gated_scan_backward(dy, gate, value, states, out_gate=out_gate, lengths=lengths, out=du.split(C, dim=2))
         flipped = self.weight.flip(1).permute(2, 1, 0).contiguous()   # [C][3][3C]
         dn = self.plan.conv1d(rows, flipped)[:, 1:]
+        if lengths is not None:
+            live = _live(lengths, L)
+            dn = torch.where(live, dn, 0)
+            dr = None if dr is None else torch.where(live, dr, 0)
         dx, dnorm = S.rms_norm_backward(dn, r, self.norm_weight, dr=dr, eps=self.eps)
         dweight = torch.zeros((3 * C, 3, C), dtype=torch.float32, device=dy.device)
         for j in range(3):   # tap j meets the token 2 - j steps back
