@@ -279,10 +279,12 @@ __global__ __launch_bounds__(kW4Threads) void quantize_kernel(W4 w, const Elem* 
     auto value = [&](int64_t c) {
         return j < w.rows && c < w.cols ? Storage<Elem>::to_f32(m[j * ldm + c]) : 0.0f;
     };
-    float top = 0.0f;
-    for (int64_t c = g * w.group; c < (g + 1) * w.group; ++c) top = fmaxf(top, fabsf(value(c)));
-    const bf16_t scale = Storage<bf16_t>::from_f32(top / 7.0f);
-    const float s = Storage<bf16_t>::to_f32(scale);
+    uint32_t top = 0;   // the largest |value|'s bits: ascending with it, NaN last
+    for (int64_t c = g * w.group; c < (g + 1) * w.group; ++c) top = max(top, __float_as_uint(value(c)) & 0x7fffffffu);
+    // a group with NaN or an infinity has no scale, and stays recognisable: all of it is NaN
+    const bool finite = top < 0x7f800000u;
+    const bf16_t scale = finite ? Storage<bf16_t>::from_f32(__uint_as_float(top) / 7.0f) : bf16_t{0x7fc0};
+    const float s = finite ? Storage<bf16_t>::to_f32(scale) : 0.0f;
     if (g < w.groups) w.scales[scale_at(w, j, g)] = scale;
     for (int64_t c = g * w.group; c < (g + 1) * w.group; c += 8) {
         int code[8];

@@ -357,7 +357,7 @@ class W4Matrix:
     @classmethod
     def quantize(cls, m, group=128, stream=None):
         """m [rows][cols] rounded to the nearest multiples -7 .. 7 of each group's
-        scale, bf16(max |m| / 7)."""
+        scale, bf16(max |m| / 7).  A group with NaN or an infinity becomes NaN."""
         if stream is not None:
             return _on(stream, cls.quantize, m, group)
         dev = _first(m, "m", (2,))

@@ -1,0 +1,29 @@
+"""Making 4-bit matrices from values that are no ordinary numbers."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import TORCH
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_groups_that_are_not_finite_stay_so(bad, dtype):
+    """NaN or an infinity in a group makes its scale not finite and all its weights
+    NaN, here and in the outputs of products; other groups keep their bits."""
+    from paper_1905_05233_amd import sequence_ops as S
+    m = torch.randn((20, 300), generator=torch.Generator().manual_seed(1)).to(TORCH[dtype]).cuda()
+    clean = S.W4Matrix.quantize(m, 64).dequantize(torch.float32)
+    m[3, 70], m[17, 299] = bad, bad
+    w = S.W4Matrix.quantize(m, 64)
+    back = w.dequantize(torch.float32)
+    hit = torch.zeros_like(back, dtype=torch.bool)
+    hit[3, 64:128] = hit[17, 256:300] = True
+    assert bool(torch.isnan(back[hit]).all()) and torch.equal(back[~hit], clean[~hit])
+    y = S.matvec_w4(torch.ones((2, 300), device="cuda"), w)
+    rows = torch.tensor([3, 17], device="cuda")
+    assert bool(torch.isnan(y[:, rows]).all()) and int(torch.isnan(y).sum()) == 4
+    zero = S.matvec_w4(torch.zeros((1, 300), device="cuda"), w)
+    assert bool(torch.isnan(zero[0, rows]).all()) and not zero[0, :3].any()
