@@ -526,8 +526,9 @@ wg_status winograd_matvec_w4(const wg_matvec_w4* args, hipStream_t stream);
 
 /* Codes and scales of a matrix m [rows][cols] (dtype, rows ldm elements apart)
  * by rounding to the nearest: scale = bf16 of the group's max |m| / 7, codes
- * round(m / scale) + 8 (a group of zeros has scale 0 and codes 8).  A group with
- * NaN or an infinity has scale NaN and codes 8: all its weights are NaN. */
+ * round(m / scale) + 8, from 1 to 15 (a group of zeros has scale 0 and codes 8).
+ * A group with NaN or an infinity has scale NaN and codes 8: all its weights are
+ * NaN. */
 wg_status winograd_quantize_w4(const wg_w4* w, wg_dtype dtype, const void* m, int64_t ldm, hipStream_t stream);
 /* Codes and scales from a matrix of codes in plain order: nibbles [rows]
  * [ceil(cols/2)] bytes, the even column in the lower half, and scales bf16

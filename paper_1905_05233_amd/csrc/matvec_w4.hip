@@ -291,7 +291,7 @@ __global__ __launch_bounds__(kW4Threads) void quantize_kernel(W4 w, const Elem* 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float q = s > 0.0f ? rintf(value(c + e) / s) : 0.0f;
-            code[e] = static_cast<int>(fminf(fmaxf(q, -8.0f), 7.0f)) + 8;
+            code[e] = static_cast<int>(fminf(fmaxf(q, -7.0f), 7.0f)) + 8;
         }
         w.codes[word_at(w, j, c)] = pack8(code);
     }

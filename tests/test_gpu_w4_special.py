@@ -27,3 +27,14 @@ def test_groups_that_are_not_finite_stay_so(bad, dtype):
     assert bool(torch.isnan(y[:, rows]).all()) and int(torch.isnan(y).sum()) == 4
     zero = S.matvec_w4(torch.zeros((1, 300), device="cuda"), w)
     assert bool(torch.isnan(zero[0, rows]).all()) and not zero[0, :3].any()
+
+
+def test_scales_below_the_normal_range():
+    """There a scale has few bits: codes are clipped at 7 scales to either side."""
+    from paper_1905_05233_amd import sequence_ops as S
+    tiny = 2.0 ** -133                       # bf16's smallest value
+    m = torch.zeros((2, 32))
+    m[0, :4] = torch.tensor([9.8, -9.8, 2.0, -1.0]) * tiny     # a scale of 1.4 tiny becomes 1
+    w = S.W4Matrix.quantize(m.cuda(), 32)
+    back = w.dequantize(torch.float32).cpu().numpy() / tiny
+    assert np.array_equal(back[0, :4], [7.0, -7.0, 2.0, -1.0]) and not back[0, 4:].any() and not back[1].any()
