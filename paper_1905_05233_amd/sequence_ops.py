@@ -331,8 +331,14 @@ def rms_norm_backward(dy, r, weight, dr=None, eps=1e-6, dx=None, stream=None):
 class W4Matrix:
     """A matrix [rows][cols] in 4 bits with a bf16 scale for every ``group`` (32, 64
     or 128) columns of a row: tiles int32 [ceil(rows/16)][ceil(cols/128)][4][16][4]
-    and scales bf16 [ceil(rows/16)][ceil(cols/group)][16] in the library's layout."""
-    __slots__ = ("tiles", "scales", "rows", "cols", "group", "_packed")
+    and scales bf16 [ceil(rows/16)][ceil(cols/group)][16] in the library's layout.
+    Its attributes are what it was made of and cannot be set."""
+    __slots__ = ("_tiles", "_scales", "_rows", "_cols", "_group", "_packed")
+    tiles = property(lambda self: self._tiles)
+    scales = property(lambda self: self._scales)
+    rows = property(lambda self: self._rows)
+    cols = property(lambda self: self._cols)
+    group = property(lambda self: self._group)
 
     def __init__(self, tiles, scales, rows, cols, group):
         if group not in (32, 64, 128):
@@ -340,11 +346,22 @@ class W4Matrix:
         if rows < 1 or cols < 1:
             raise ValueError("rows and cols must be positive")
         dev = _first(tiles, "tiles", (5,))
-        rt = -(-rows // 16)
-        tp = _dense(tiles, "tiles", (rt, -(-cols // 128), 4, 16, 4), torch.int32, dev)
-        sp = _dense(scales, "scales", (rt, -(-cols // group), 16), torch.bfloat16, dev)
-        self.tiles, self.scales, self.rows, self.cols, self.group = tiles, scales, rows, cols, group
-        self._packed = (tp, sp, rows, cols, group)
+        self._tiles, self._scales, self._rows, self._cols, self._group = tiles, scales, rows, cols, group
+        self._check(dev)
+
+    def _check(self, dev):
+        rt = -(-self._rows // 16)
+        tp = _dense(self._tiles, "tiles", (rt, -(-self._cols // 128), 4, 16, 4), torch.int32, dev)
+        sp = _dense(self._scales, "scales", (rt, -(-self._cols // self._group), 16), torch.bfloat16, dev)
+        self._packed = (tp, sp, self._rows, self._cols, self._group)
+
+    def _words(self, dev):
+        """The argument's words.  Tensors that were given other memory since they were
+        last checked are checked again."""
+        packed = self._packed
+        if self._tiles.data_ptr() != packed[0] or self._scales.data_ptr() != packed[1]:
+            self._check(dev)
+        return self._packed
 
     @classmethod
     def _empty(cls, rows, cols, group, device):
@@ -364,7 +381,7 @@ class W4Matrix:
         mp, _, ld = _rows(m, "m", m.shape, m.dtype, dev)
         code = _code(m, "m")
         w = cls._empty(m.shape[0], m.shape[1], group, m.device)
-        N.check(N.lib().winograd_quantize_w4(_pack_w4(*w._packed), code, mp, ld, _raw_stream(None)))
+        N.check(N.lib().winograd_quantize_w4(_pack_w4(*w._words(dev)), code, mp, ld, _raw_stream(None)))
         return w
 
     @classmethod
@@ -384,7 +401,7 @@ class W4Matrix:
             raise ValueError("scales must be [rows][ceil(cols/group)] for a group of 32, 64 or 128")
         sp = _dense(scales, "scales", (rows, scales.shape[1]), torch.bfloat16, dev)
         w = cls._empty(rows, cols, fits[0], nibbles.device)
-        N.check(N.lib().winograd_pack_w4(_pack_w4(*w._packed), np_, sp, _raw_stream(None)))
+        N.check(N.lib().winograd_pack_w4(_pack_w4(*w._words(dev)), np_, sp, _raw_stream(None)))
         return w
 
     def dequantize(self, dtype=torch.bfloat16, stream=None):
@@ -393,8 +410,8 @@ class W4Matrix:
             return _on(stream, W4Matrix.dequantize, self, dtype)
         m = torch.empty((self.rows, self.cols), dtype=dtype, device=self.tiles.device)
         code = _code(m, "m")
-        _first(self.tiles, "tiles", (5,))
-        N.check(N.lib().winograd_dequantize_w4(_pack_w4(*self._packed), code, m.data_ptr(), self.cols,
+        dev = _first(self.tiles, "tiles", (5,))
+        N.check(N.lib().winograd_dequantize_w4(_pack_w4(*self._words(dev)), code, m.data_ptr(), self.cols,
                                                _raw_stream(None)))
         return m
 
@@ -408,10 +425,10 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
     dev = _first(x, "x", (2,))
     xdt = x.dtype
     x8 = xdt == torch.float8_e4m3fn
-    M = x.shape[0]
-    xp, _, ldx = _rows(x, "x", (M, w.cols), xdt, dev)
+    M, rows = x.shape[0], w._rows
+    xp, _, ldx = _rows(x, "x", (M, w._cols), xdt, dev)
     xcode = _E4M3 if x8 else _code(x, "x")
-    if w.tiles.get_device() != dev:
+    if w._tiles.get_device() != dev:
         raise ValueError("w must be on the GPU of the other tensors")
     sp, groups = 0, 0
     if x8:
@@ -424,14 +441,14 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
     if y is None:
         if dtype is None:
             dtype = torch.bfloat16 if x8 else xdt
-        y = torch.empty_strided((M, w.rows), (w.rows, 1), dtype=dtype, device=x.device)
-        yp, ldy = y.data_ptr(), w.rows
+        y = torch.empty_strided((M, rows), (rows, 1), dtype=dtype, device=x.device)
+        yp, ldy = y.data_ptr(), rows
     else:
         if dtype is not None and dtype != y.dtype:
             raise TypeError("dtype is that of y")
-        yp, _, ldy = _rows(y, "y", (M, w.rows), y.dtype, dev)
+        yp, _, ldy = _rows(y, "y", (M, rows), y.dtype, dev)
     st = N.lib().winograd_matvec_w4(
-        _pack_matvec(*w._packed, M, xcode, _code(y, "y"), xp, ldx, sp, groups, yp, ldy), _raw_stream(None))
+        _pack_matvec(*w._words(dev), M, xcode, _code(y, "y"), xp, ldx, sp, groups, yp, ldy), _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
     return y

@@ -38,3 +38,22 @@ def test_scales_below_the_normal_range():
     w = S.W4Matrix.quantize(m.cuda(), 32)
     back = w.dequantize(torch.float32).cpu().numpy() / tiny
     assert np.array_equal(back[0, :4], [7.0, -7.0, 2.0, -1.0]) and not back[0, 4:].any() and not back[1].any()
+
+
+def test_the_tensors_memory_is_read_where_it_is():
+    """A tensor of a matrix that is given other memory is read there, and checked again."""
+    from paper_1905_05233_amd import sequence_ops as S
+    m = torch.randn((40, 200), generator=torch.Generator().manual_seed(2)).cuda()
+    w, other = S.W4Matrix.quantize(m, 64), S.W4Matrix.quantize(m * 2 - 1, 64)
+    x = torch.randn((2, 200), generator=torch.Generator().manual_seed(3)).cuda()
+    first, want = S.matvec_w4(x, w), S.matvec_w4(x, other)
+    held = w.tiles.detach(), w.scales.detach()
+    w.tiles.data, w.scales.data = other.tiles, other.scales
+    assert torch.equal(S.matvec_w4(x, w), want) and not torch.equal(first, want)
+    w.tiles.data = other.tiles[:2].clone()
+    with pytest.raises(ValueError):
+        S.matvec_w4(x, w)
+    with pytest.raises(ValueError):
+        w.dequantize()
+    w.tiles.data, w.scales.data = held
+    assert torch.equal(S.matvec_w4(x, w), first)
