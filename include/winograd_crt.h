@@ -510,8 +510,8 @@ typedef struct {
  * x_scales is fp32 [M][G] (contiguous), G = 1 (a scale a row) or ceil(K/group)
  * with the weights' group; NULL otherwise.  y [M][R] in y_dtype (WG_F32, WG_F16,
  * WG_BF16).  x and y rows start ldx and ldy elements apart.  A row of x with NaN or
- * infinity, or with sums of 32 |x| (280 |x| in WG_F16) beyond fp32's range, gives
- * NaN or infinity in its own outputs alone. */
+ * infinity, or with sums of 32 |x| beyond fp32's range, gives NaN or infinity in its
+ * own outputs alone. */
 typedef struct {
     wg_w4 w;
     int64_t M, x_dtype, y_dtype;

@@ -53,13 +53,14 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
 // A code becomes a 16-bit float without arithmetic: four bits at bit 3 of the
 // fraction of a number whose ones there count 1 (16 in bf16, 128 in fp16), so that
 // a word gives its eight weights, plus 16 or 128, in seven and/or/shift
-// instructions.  What was added, and the codes' 8, leaves through the accumulator,
-// which starts each group from another product, of a constant matrix (-24 or -136)
-// with the same x, and so exactly up to the accumulator's fp32.
+// instructions.  For rows in bf16 and fp8 what was added, and the codes' 8, leaves
+// through the accumulator, which starts each group from another product, of a constant
+// matrix (-24) with the same x, and so exactly up to the accumulator's fp32.
 // The group's sum times its scale goes to the running fp32 sum of the output.
 //
-// Rows of x in fp32 are cut into three bf16 parts of 8 bits each, which hold all 24
-// bits, and meet the weights themselves; fp8 becomes bf16 exactly.
+// Rows of x in fp16 meet the weights themselves (four subtractions a word in place of
+// that product); so do rows in fp32, cut into three bf16 parts of 8 bits each, which hold
+// all 24 bits.  fp8 becomes bf16 exactly.
 //
 // The waves of a workgroup take the tiles of columns in turn, each wave's next tile
 // in flight (two or more ahead are no faster: 25088 -> 4096 14.2 us with one, 15.8
@@ -77,6 +78,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr int kTokens = 16;     // rows of x that a wave takes
 constexpr int kUnits = 256;     // compute units of the chip
 
@@ -94,18 +96,26 @@ template <bool F16> __device__ __forceinline__ u32x4 widen_codes(uint32_t w) {
     return u32x4{(w & kMask) | kOne, (w >> 4 & kMask) | kOne, (w >> 8 & kMask) | kOne,
                  (__builtin_amdgcn_alignbit(w, w, 12) & kMask) | kOne};
 }
-// What must go again: -24 in bf16, -136 in fp16.
-template <bool F16> constexpr uint32_t kOffset = F16 ? 0xd840d840u : 0xc1c0c1c0u;
+// What must go again: -24 in bf16.
+constexpr uint32_t kOffset = 0xc1c0c1c0u;
 
-// The weights themselves, codes less 8, for fp32: what is added above would cost
-// fp32 rows three of their bits (over 4096 columns 1.0e-6 off, and 1.2e-7 without).
+// The weights themselves, codes less 8, for fp32 and fp16 rows: what is added above
+// would cost their sums three and four bits (fp32 outputs over 4096 columns from fp32
+// rows 1.0e-6 off, and 1.2e-7 without; from fp16 rows 0.8 to 2.2e-6 and 0.9e-7, where 4096
+// -> 5000 takes 6.5 us instead of 6.3 and 25088 -> 4096 the same).  bf16 and fp8 rows lose
+// nothing: their products have few bits, 1.0e-7 either way.
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
-__device__ __forceinline__ u32x4 exact_codes(uint32_t w) {
-    u32x4 f = widen_codes<false>(w);
+template <bool F16> __device__ __forceinline__ u32x4 exact_codes(uint32_t w) {
+    u32x4 f = widen_codes<F16>(w);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        f[j] = upper_halves(__float_as_uint(__uint_as_float(f[j] << 16) - 24.0f),
-                            __float_as_uint(__uint_as_float(f[j] & 0xffff0000u) - 24.0f));
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t pair = f[j];
+        if constexpr (F16)
+            f[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) - f16x2{136, 136});
+        else
+            f[j] = upper_halves(__float_as_uint(__uint_as_float(pair << 16) - 24.0f),
+                                __float_as_uint(__uint_as_float(pair & 0xffff0000u) - 24.0f));
+    }
     return f;
 }
 
@@ -171,7 +181,7 @@ struct MatvecArgs {
 template <int XD, int GPT, bool XG, int RT>
 __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
     using X = typename XTypeOf<XD>::type;
-    constexpr bool F16 = XD == 1;
+    constexpr bool F16 = XD == 1, EXACT = XD < 2;   // the weights themselves, or plus an offset
     constexpr int SPG = 4 / GPT;   // instructions of a group
     extern __shared__ float sums[];   // [wave][tile of rows][lane][4]
     const W4& w = a.w;
@@ -224,9 +234,9 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
         for (int g = 0; g < GPT; ++g) {
             // groups past the matrix's last one have no columns
             const int64_t group = min(static_cast<int64_t>(kt) * GPT + g, w.groups - 1);
-            const u32x4 offset{kOffset<F16>, kOffset<F16>, kOffset<F16>, kOffset<F16>};
+            const u32x4 offset{kOffset, kOffset, kOffset, kOffset};
             f32x4 start{0, 0, 0, 0};
-            if constexpr (XD != 0) {
+            if constexpr (!EXACT) {
 #pragma unroll
                 for (int s = g * SPG; s < (g + 1) * SPG; ++s) start = mma<F16>(offset, xp[s][0], start);
             }
@@ -237,7 +247,7 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
                 f32x4 sum = start;
 #pragma unroll
                 for (int s = g * SPG; s < (g + 1) * SPG; ++s) {
-                    const u32x4 frag = XD == 0 ? exact_codes(cur[r][s]) : widen_codes<F16>(cur[r][s]);
+                    const u32x4 frag = EXACT ? exact_codes<F16>(cur[r][s]) : widen_codes<F16>(cur[r][s]);
 #pragma unroll
                     for (int part = 0; part < kPlanes<XD>; ++part) sum = mma<F16>(frag, xp[s][part], sum);
                 }
