@@ -4,6 +4,7 @@
 // The layout of codes and scales is winograd_crt.h's (wg_w4).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "device_common.hpp"
@@ -345,12 +346,26 @@ hipError_t blocks_for(int64_t threads, unsigned* blocks) {
     return hipSuccess;
 }
 
+// HIP takes fewer than 2^32 threads along x and 2^16 workgroups along y: larger products
+// go in several launches, of rows of the matrix and of x.
 template <int XD, int GPT, bool XG, int RT> hipError_t matvec_r(const MatvecArgs& k, hipStream_t stream) {
-    const int64_t x = (k.w.rows + 16 * RT - 1) / (16 * RT), y = (k.M + kTokens - 1) / kTokens;
     const int waves = static_cast<int>(k.w.ktiles < 16 ? k.w.ktiles : 16);
-    if (x * waves * 64 > 0xffffffffLL || y > 0xffff) return hipErrorInvalidValue;
-    matvec_kernel<XD, GPT, XG, RT><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), waves * 64,
-                                 waves * RT * 256 * sizeof(float), stream>>>(k);
+    const int64_t rows = int64_t(0xffffffff) / (waves * 64) * (16 * RT), tokens = int64_t(0xffff) * kTokens;
+    const int64_t xs = sizeof(typename XTypeOf<XD>::type), ys = dtype_bytes(k.y_dtype);
+    for (int64_t m = 0; m < k.M; m += tokens)
+        for (int64_t j = 0; j < k.w.rows; j += rows) {
+            MatvecArgs a = k;
+            a.M = std::min(k.M - m, tokens);
+            a.x = static_cast<const char*>(k.x) + m * k.ldx * xs;
+            if (k.x_scales) a.x_scales = k.x_scales + m * k.x_groups;
+            a.y = static_cast<char*>(k.y) + (m * k.ldy + j) * ys;
+            a.w.rows = std::min(k.w.rows - j, rows);
+            a.w.codes = k.w.codes + j * k.w.ktiles * 16;   // 16 words a row of a tile
+            a.w.scales = k.w.scales + j * k.w.groups;
+            const dim3 grid(static_cast<unsigned>((a.w.rows + 16 * RT - 1) / (16 * RT)),
+                            static_cast<unsigned>((a.M + kTokens - 1) / kTokens));
+            matvec_kernel<XD, GPT, XG, RT><<<grid, waves * 64, waves * RT * 256 * sizeof(float), stream>>>(a);
+        }
     return hipGetLastError();
 }
 template <int XD, int GPT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hipStream_t stream) {

@@ -1,0 +1,49 @@
+"""More rows, channels or weights than one launch takes threads."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1)
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_products_of_many_rows():
+    """More than 2^20 rows of x."""
+    from paper_1905_05233_amd import sequence_ops as S
+    w = S.W4Matrix.quantize(torch.randn((5, 40), device="cuda"), 32)
+    some = torch.randn((1000, 40), device="cuda").bfloat16()
+    M = 2 ** 20 + 1003
+    x = some.repeat(-(-M // 1000), 1)[:M]
+    y, want = S.matvec_w4(x, w), S.matvec_w4(some, w)
+    assert torch.equal(y, want.repeat(-(-M // 1000), 1)[:M])
+    scales = torch.rand((M, 1), device="cuda") + 0.5
+    q = x.to(torch.float8_e4m3fn)
+    y = S.matvec_w4(q, w, x_scales=scales)
+    for at in (0, 2 ** 20 - 20, M - 100):
+        assert torch.equal(y[at:at + 100], S.matvec_w4(q[at:at + 100], w, x_scales=scales[at:at + 100]))
+
+
+def test_products_with_many_outputs():
+    """2^30 rows of the matrix and some more: one column, as its tiles are 64 bytes a row."""
+    from paper_1905_05233_amd import sequence_ops as S
+    rows = 2 ** 30 + 40
+    w = S.W4Matrix._empty(rows, 1, 32, "cuda")
+    small = S.W4Matrix.quantize(torch.randn((1600, 1), device="cuda"), 32)
+    tiles = w.tiles.shape[0]
+    for at in range(0, tiles, 100):
+        if at >= 3200 and at + 3200 < tiles and at % 1000000:
+            continue                        # the rest holds whatever it holds
+        n = min(100, tiles - at)
+        w.tiles[at:at + n] = small.tiles[:n]
+        w.scales[at:at + n] = small.scales[:n]
+    x = torch.randn((3, 1), device="cuda").bfloat16()
+    y, want = S.matvec_w4(x, w), S.matvec_w4(x, small)
+    for at in (0, 1000000, tiles // 100 * 100 - 1000, tiles // 100 * 100):
+        n = min(100, tiles - at) * 16
+        n = min(n, rows - at * 16)
+        assert torch.equal(y[:, at * 16:at * 16 + n], want[:, :n]), at
