@@ -640,18 +640,20 @@ template <typename Elem> struct StepArgs {
 template <typename Elem>
 __global__ __launch_bounds__(kStepThreads) void step_kernel(StepArgs<Elem> a) {
     using S = Storage<Elem>;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * kStepThreads + threadIdx.x;
-    if (id >= a.N * a.C) return;
-    const int64_t n = id / a.C, c = id % a.C;
-    const Gate g = gate_of(S::to_f32(a.gate.at(n, 0)[c]));
-    const float h = g.f * a.h[id] + g.i * S::to_f32(a.value.at(n, 0)[c]);
-    float y = h;
-    if (a.out_gate.p) {
-        const float o = S::to_f32(a.out_gate.at(n, 0)[c]);
-        y = h * (o * sigmoid_of(o));
+    // more states than a launch has threads: in turns
+    const int64_t all = a.N * a.C, stride = static_cast<int64_t>(gridDim.x) * kStepThreads;
+    for (int64_t id = static_cast<int64_t>(blockIdx.x) * kStepThreads + threadIdx.x; id < all; id += stride) {
+        const int64_t n = id / a.C, c = id % a.C;
+        const Gate g = gate_of(S::to_f32(a.gate.at(n, 0)[c]));
+        const float h = g.f * a.h[id] + g.i * S::to_f32(a.value.at(n, 0)[c]);
+        float y = h;
+        if (a.out_gate.p) {
+            const float o = S::to_f32(a.out_gate.at(n, 0)[c]);
+            y = h * (o * sigmoid_of(o));
+        }
+        a.h_new[id] = h;
+        a.y.at(n, 0)[c] = S::from_f32(y);
     }
-    a.h_new[id] = h;
-    a.y.at(n, 0)[c] = S::from_f32(y);
 }
 
 // How a call is cut.
@@ -752,8 +754,7 @@ template <int D> hipError_t launch_gated_step_t(const wg_gated_step& a, hipStrea
     using Elem = typename DTypeOf<D>::type;
     const StepArgs<Elem> k{a.N, a.C, rows_of<const Elem>(a.gate), rows_of<const Elem>(a.value),
                            rows_of<const Elem>(a.out_gate), rows_of<Elem>(a.y), a.h, a.h_new};
-    const int64_t blocks = (a.N * a.C + kStepThreads - 1) / kStepThreads;
-    if (blocks * kStepThreads > 0xffffffffLL) return hipErrorInvalidValue;
+    const int64_t blocks = std::min<int64_t>((a.N * a.C + kStepThreads - 1) / kStepThreads, 0xffffffffLL / kStepThreads);
     step_kernel<Elem><<<static_cast<unsigned>(blocks), kStepThreads, 0, stream>>>(k);
     return hipGetLastError();
 }

@@ -47,3 +47,16 @@ def test_products_with_many_outputs():
         n = min(100, tiles - at) * 16
         n = min(n, rows - at * 16)
         assert torch.equal(y[:, at * 16:at * 16 + n], want[:, :n]), at
+
+
+def test_step_of_many_channels():
+    """More than 2^32 states."""
+    from paper_1905_05233_amd import sequence_ops as S
+    N, C = 4099, 2 ** 20
+    z, v, o = (torch.randn((1, C), device="cuda").bfloat16() for _ in range(3))
+    h = torch.randn((1, C), device="cuda")
+    wy, wh = S.gated_step(z, v, h, out_gate=o)
+    big = h.repeat(N, 1)
+    y, new = S.gated_step(z.expand(N, C), v.expand(N, C), big, out_gate=o.expand(N, C), h_new=big)
+    for at in range(0, N, 500):
+        assert bool((new[at:at + 500] == wh).all()) and bool((y[at:at + 500] == wy).all()), at
