@@ -279,71 +279,78 @@ __global__ __launch_bounds__(1024) void matvec_kernel(MatvecArgs a) {
     }
 }
 
+// Each thread's first item of all the launch's and the number of its threads: more items
+// than HIP takes threads are taken in turns.
+struct Turns {
+    int64_t first, stride;
+};
+__device__ __forceinline__ Turns turns() {
+    return {static_cast<int64_t>(blockIdx.x) * kW4Threads + threadIdx.x, static_cast<int64_t>(gridDim.x) * kW4Threads};
+}
+unsigned blocks_for(int64_t items) {
+    return static_cast<unsigned>(std::min<int64_t>((items + kW4Threads - 1) / kW4Threads, 0xffffffffLL / kW4Threads));
+}
+
 // One thread per group of a row (padding rows too).
 template <typename Elem>
-__global__ __launch_bounds__(kW4Threads) void quantize_kernel(W4 w, const Elem* m, int64_t ldm) {
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * kW4Threads + threadIdx.x;
-    const int64_t rows = (w.rows + 15) / 16 * 16, padded = w.ktiles * 128;
-    const int64_t groups = padded / w.group;
-    if (id >= rows * groups) return;
-    const int64_t j = id / groups, g = id % groups;
-    auto value = [&](int64_t c) {
-        return j < w.rows && c < w.cols ? Storage<Elem>::to_f32(m[j * ldm + c]) : 0.0f;
-    };
-    uint32_t top = 0;   // the largest |value|'s bits: ascending with it, NaN last
-    for (int64_t c = g * w.group; c < (g + 1) * w.group; ++c) top = max(top, __float_as_uint(value(c)) & 0x7fffffffu);
-    // a group with NaN or an infinity has no scale, and stays recognisable: all of it is NaN
-    const bool finite = top < 0x7f800000u;
-    const bf16_t scale = finite ? Storage<bf16_t>::from_f32(__uint_as_float(top) / 7.0f) : bf16_t{0x7fc0};
-    const float s = finite ? Storage<bf16_t>::to_f32(scale) : 0.0f;
-    if (g < w.groups) w.scales[scale_at(w, j, g)] = scale;
-    for (int64_t c = g * w.group; c < (g + 1) * w.group; c += 8) {
-        int code[8];
+__global__ __launch_bounds__(kW4Threads) void quantize_kernel(W4 w, const Elem* m, int64_t ldm, int64_t items) {
+    const int64_t groups = w.ktiles * 128 / w.group;
+    const Turns t = turns();
+    for (int64_t id = t.first; id < items; id += t.stride) {
+        const int64_t j = id / groups, g = id % groups;
+        auto value = [&](int64_t c) {
+            return j < w.rows && c < w.cols ? Storage<Elem>::to_f32(m[j * ldm + c]) : 0.0f;
+        };
+        uint32_t top = 0;   // the largest |value|'s bits: ascending with it, NaN last
+        for (int64_t c = g * w.group; c < (g + 1) * w.group; ++c) top = max(top, __float_as_uint(value(c)) & 0x7fffffffu);
+        // a group with NaN or an infinity has no scale, and stays recognisable: all of it is NaN
+        const bool finite = top < 0x7f800000u;
+        const bf16_t scale = finite ? Storage<bf16_t>::from_f32(__uint_as_float(top) / 7.0f) : bf16_t{0x7fc0};
+        const float s = finite ? Storage<bf16_t>::to_f32(scale) : 0.0f;
+        if (g < w.groups) w.scales[scale_at(w, j, g)] = scale;
+        for (int64_t c = g * w.group; c < (g + 1) * w.group; c += 8) {
+            int code[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float q = s > 0.0f ? rintf(value(c + e) / s) : 0.0f;
-            code[e] = static_cast<int>(fminf(fmaxf(q, -7.0f), 7.0f)) + 8;
+            for (int e = 0; e < 8; ++e) {
+                const float q = s > 0.0f ? rintf(value(c + e) / s) : 0.0f;
+                code[e] = static_cast<int>(fminf(fmaxf(q, -7.0f), 7.0f)) + 8;
+            }
+            w.codes[word_at(w, j, c)] = pack8(code);
         }
-        w.codes[word_at(w, j, c)] = pack8(code);
     }
 }
 
 // One thread per word (of padding rows and columns too).
-__global__ __launch_bounds__(kW4Threads) void pack_kernel(W4 w, const uint8_t* nibbles, const bf16_t* scales) {
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * kW4Threads + threadIdx.x;
-    const int64_t rows = (w.rows + 15) / 16 * 16, words = w.ktiles * 16;
-    if (id >= rows * words) return;
-    const int64_t j = id / words, c = id % words * 8, ld = (w.cols + 1) / 2;
-    int code[8];
+__global__ __launch_bounds__(kW4Threads) void pack_kernel(W4 w, const uint8_t* nibbles, const bf16_t* scales, int64_t items) {
+    const int64_t words = w.ktiles * 16, ld = (w.cols + 1) / 2;
+    const Turns t = turns();
+    for (int64_t id = t.first; id < items; id += t.stride) {
+        const int64_t j = id / words, c = id % words * 8;
+        int code[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int64_t at = c + e;
-        code[e] = j < w.rows && at < w.cols ? nibbles[j * ld + at / 2] >> (at % 2 * 4) & 15 : 8;
-    }
-    w.codes[word_at(w, j, c)] = pack8(code);
-    if (c % w.group == 0 && c / w.group < w.groups) {
-        const int64_t g = c / w.group;
-        w.scales[scale_at(w, j, g)] = j < w.rows ? scales[j * w.groups + g] : bf16_t{0};
+        for (int e = 0; e < 8; ++e) {
+            const int64_t at = c + e;
+            code[e] = j < w.rows && at < w.cols ? nibbles[j * ld + at / 2] >> (at % 2 * 4) & 15 : 8;
+        }
+        w.codes[word_at(w, j, c)] = pack8(code);
+        if (c % w.group == 0 && c / w.group < w.groups) {
+            const int64_t g = c / w.group;
+            w.scales[scale_at(w, j, g)] = j < w.rows ? scales[j * w.groups + g] : bf16_t{0};
+        }
     }
 }
 
 template <typename Elem>
-__global__ __launch_bounds__(kW4Threads) void dequantize_kernel(W4 w, Elem* m, int64_t ldm) {
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * kW4Threads + threadIdx.x;
+__global__ __launch_bounds__(kW4Threads) void dequantize_kernel(W4 w, Elem* m, int64_t ldm, int64_t items) {
     const int64_t words = (w.cols + 7) / 8;
-    if (id >= w.rows * words) return;
-    const int64_t j = id / words, c = id % words * 8;
-    const uint32_t word = w.codes[word_at(w, j, c)];
-    const float s = Storage<bf16_t>::to_f32(w.scales[scale_at(w, j, c / w.group)]);
-    for (int e = 0; e < 8 && c + e < w.cols; ++e)
-        m[j * ldm + c + e] = Storage<Elem>::from_f32(static_cast<float>(code_of(word, e) - 8) * s);
-}
-
-hipError_t blocks_for(int64_t threads, unsigned* blocks) {
-    const int64_t b = (threads + kW4Threads - 1) / kW4Threads;
-    if (b * kW4Threads > 0xffffffffLL) return hipErrorInvalidValue;
-    *blocks = static_cast<unsigned>(b);
-    return hipSuccess;
+    const Turns t = turns();
+    for (int64_t id = t.first; id < items; id += t.stride) {
+        const int64_t j = id / words, c = id % words * 8;
+        const uint32_t word = w.codes[word_at(w, j, c)];
+        const float s = Storage<bf16_t>::to_f32(w.scales[scale_at(w, j, c / w.group)]);
+        for (int e = 0; e < 8 && c + e < w.cols; ++e)
+            m[j * ldm + c + e] = Storage<Elem>::from_f32(static_cast<float>(code_of(word, e) - 8) * s);
+    }
 }
 
 // HIP takes fewer than 2^32 threads along x and 2^16 workgroups along y: larger products
@@ -403,29 +410,23 @@ hipError_t launch_matvec_w4(const wg_matvec_w4& a, hipStream_t stream) {
 template <int D> hipError_t launch_quantize_w4_t(const wg_w4& w, const void* m, int64_t ldm, hipStream_t stream) {
     using Elem = typename DTypeOf<D>::type;
     const W4 k = w4_of(w);
-    unsigned blocks;
-    const hipError_t e = blocks_for((w.rows + 15) / 16 * 16 * (k.ktiles * 128 / w.group), &blocks);
-    if (e != hipSuccess) return e;
-    quantize_kernel<Elem><<<blocks, kW4Threads, 0, stream>>>(k, static_cast<const Elem*>(m), ldm);
+    const int64_t items = (w.rows + 15) / 16 * 16 * (k.ktiles * 128 / w.group);
+    quantize_kernel<Elem><<<blocks_for(items), kW4Threads, 0, stream>>>(k, static_cast<const Elem*>(m), ldm, items);
     return hipGetLastError();
 }
 
 template <int D> hipError_t launch_dequantize_w4_t(const wg_w4& w, void* m, int64_t ldm, hipStream_t stream) {
     using Elem = typename DTypeOf<D>::type;
-    unsigned blocks;
-    const hipError_t e = blocks_for(w.rows * ((w.cols + 7) / 8), &blocks);
-    if (e != hipSuccess) return e;
-    dequantize_kernel<Elem><<<blocks, kW4Threads, 0, stream>>>(w4_of(w), static_cast<Elem*>(m), ldm);
+    const int64_t items = w.rows * ((w.cols + 7) / 8);
+    dequantize_kernel<Elem><<<blocks_for(items), kW4Threads, 0, stream>>>(w4_of(w), static_cast<Elem*>(m), ldm, items);
     return hipGetLastError();
 }
 
 hipError_t launch_pack_w4(const wg_w4& w, const void* nibbles, const void* scales, hipStream_t stream) {
     const W4 k = w4_of(w);
-    unsigned blocks;
-    const hipError_t e = blocks_for((w.rows + 15) / 16 * 16 * (k.ktiles * 16), &blocks);
-    if (e != hipSuccess) return e;
-    pack_kernel<<<blocks, kW4Threads, 0, stream>>>(k, static_cast<const uint8_t*>(nibbles),
-                                                   static_cast<const bf16_t*>(scales));
+    const int64_t items = (w.rows + 15) / 16 * 16 * (k.ktiles * 16);
+    pack_kernel<<<blocks_for(items), kW4Threads, 0, stream>>>(k, static_cast<const uint8_t*>(nibbles),
+                                                              static_cast<const bf16_t*>(scales), items);
     return hipGetLastError();
 }
 

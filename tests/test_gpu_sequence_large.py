@@ -60,3 +60,37 @@ def test_step_of_many_channels():
     y, new = S.gated_step(z.expand(N, C), v.expand(N, C), big, out_gate=o.expand(N, C), h_new=big)
     for at in range(0, N, 500):
         assert bool((new[at:at + 500] == wh).all()) and bool((y[at:at + 500] == wy).all()), at
+
+
+def test_making_large_matrices():
+    """Matrices of more groups, words or runs of columns than 2^32."""
+    from paper_1905_05233_amd import sequence_ops as S
+    rows = 2 ** 30 + 48
+    some = torch.randn((1600, 1), device="cuda").bfloat16()
+    small = S.W4Matrix.quantize(some, 32)
+    w = S.W4Matrix.quantize(some.repeat(-(-rows // 1600), 1)[:rows], 32)
+    for at in (0, 10 ** 7, rows // 1600 * 100 - 100):
+        assert torch.equal(w.tiles[at:at + 100], small.tiles) and torch.equal(w.scales[at:at + 100], small.scales)
+    n = w.tiles.shape[0] % 100
+    assert torch.equal(w.tiles[-n:], small.tiles[:n]) and torch.equal(w.scales[-n:], small.scales[:n])
+    del w
+    torch.cuda.empty_cache()
+
+    rows = 2 ** 28 + 48
+    codes = torch.randint(0, 256, (1600, 1), device="cuda").to(torch.uint8)
+    scales = torch.rand((1600, 1), device="cuda").bfloat16()
+    small = S.W4Matrix.from_nibbles(codes, scales, 1)
+    w = S.W4Matrix.from_nibbles(codes.repeat(-(-rows // 1600), 1)[:rows], scales.repeat(-(-rows // 1600), 1)[:rows], 1)
+    for at in (0, 10 ** 7, rows // 1600 * 100 - 100):
+        assert torch.equal(w.tiles[at:at + 100], small.tiles) and torch.equal(w.scales[at:at + 100], small.scales)
+    del w
+    torch.cuda.empty_cache()
+
+    rows, cols = 2 ** 22 + 16, 8192
+    small = S.W4Matrix.quantize(torch.randn((16, cols), device="cuda"), 128)
+    w = S.W4Matrix._empty(rows, cols, 128, "cuda")
+    w.tiles.copy_(small.tiles.expand_as(w.tiles))
+    w.scales.copy_(small.scales.expand_as(w.scales))
+    m, want = w.dequantize().view(-1, 16, cols), small.dequantize()
+    for at in range(0, rows // 16, 2 ** 14):
+        assert bool((m[at:at + 2 ** 14] == want).all()), at
