@@ -112,7 +112,8 @@ __device__ __forceinline__ int32_t steps_of(const int32_t* lengths, int64_t n, i
 struct Split {
     int64_t columns;      // N * runs
     int32_t runs;         // runs of V channels in a row, the last one maybe short
-    uint32_t groups;      // of LANES columns
+    int64_t first;        // group of this launch
+    uint32_t groups;      // of LANES columns, of this launch
     int32_t tiles;        // of a sequence
     int32_t chunk;        // tiles of a chunk
     int32_t chunks;
@@ -206,14 +207,14 @@ __device__ __forceinline__ float reach_chunk(const float2* maps, int64_t stride,
 // turn 32; 16 x 4096 x 512 in groups of 64 bytes 74 and 87.  Where they do not, in turn
 // is better (16381 x 512: 23.4 us, in runs 25.3).
 struct Share {
-    uint32_t group;
+    int64_t group;
     int chunk;   // from `chunks` on: none
 };
 template <int LANES> __device__ __forceinline__ Share share_of_block(const Split& split, int chunks) {
     const bool apart = LANES == 8 && split.runs % LANES == 0;
     const uint32_t id = apart ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
     const uint32_t chunk = id / split.groups;
-    return {id - chunk * split.groups, chunk < static_cast<uint32_t>(chunks) ? static_cast<int>(chunk) : chunks};
+    return {split.first + (id - chunk * split.groups), chunk < static_cast<uint32_t>(chunks) ? static_cast<int>(chunk) : chunks};
 }
 
 // A thread's place as the owner of steps: its column (a run of V channels) of a
@@ -224,10 +225,10 @@ struct Place {
     RunShape shape;   // no channels: no column
 };
 template <typename Elem, int LANES>
-__device__ __forceinline__ Place place_of(const Split& split, const int32_t* lengths, int32_t L, int32_t C, uint32_t group,
+__device__ __forceinline__ Place place_of(const Split& split, const int32_t* lengths, int32_t L, int32_t C, int64_t group,
                                           int32_t t) {
     constexpr int V = Vec<Elem>::V, S = kHeld / V;
-    const int64_t column = static_cast<int64_t>(group) * LANES + threadIdx.x % LANES;
+    const int64_t column = group * LANES + threadIdx.x % LANES;
     const bool has = column < split.columns;
     Place p;
     if (split.columns >> 31 == 0) {   // 32-bit division
@@ -250,9 +251,9 @@ struct Scanner {
     bool scans;
 };
 template <typename Elem, int LANES>
-__device__ __forceinline__ Scanner scanner_of(const Split& split, int32_t C, uint32_t group, int channel) {
+__device__ __forceinline__ Scanner scanner_of(const Split& split, int32_t C, int64_t group, int channel) {
     constexpr int V = Vec<Elem>::V;
-    const int64_t column = static_cast<int64_t>(group) * LANES + channel / V;
+    const int64_t column = group * LANES + channel / V;
     Scanner s;
     if (split.columns >> 31 == 0) {
         const uint32_t q = static_cast<uint32_t>(column) / static_cast<uint32_t>(split.runs);
@@ -293,12 +294,12 @@ __global__ __launch_bounds__(T) void scan_kernel(ScanArgs<Elem> a) {
     const int chunks = a.split.chunks - (MAPS ? 1 : 0);   // nothing reads the last chunk's map
     const Share share = share_of_block<LANES>(a.split, chunks);
     if (share.chunk == chunks) return;
-    const uint32_t group = share.group;
+    const int64_t group = share.group;
     const int chunk = share.chunk, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
     Place at = place_of<Elem, LANES>(a.split, a.lengths, L, a.C, group, start_of(chunk * a.split.chunk));
     const Scanner sc = scanner_of<Elem, LANES>(a.split, a.C, group, channel);
     const int64_t map_stride = static_cast<int64_t>(a.split.groups) * CH;
-    float2* maps = a.maps + static_cast<int64_t>(group) * CH + channel;
+    float2* maps = a.maps + group * CH + channel;
     // the state ahead of the tile at hand, or the map of the chunk's tiles so far
     float carry = !MAPS && sc.scans && a.h0 ? a.h0[sc.n * a.C + sc.c] : 0.0f;
     float product = 1.0f;
@@ -452,12 +453,12 @@ __global__ __launch_bounds__(T) void scan_grad_kernel(GradArgs<Elem> a) {
     const int chunks = a.split.chunks - (MAPS ? 1 : 0);   // nothing reads the last chunk's map
     const Share share = share_of_block<LANES>(a.split, chunks);
     if (share.chunk == chunks) return;
-    const uint32_t group = share.group;
+    const int64_t group = share.group;
     const int chunk = share.chunk, end = min((chunk + 1) * a.split.chunk, a.split.tiles);
     Place at = place_of<Elem, LANES>(a.split, a.lengths, L, a.C, group, start_of(chunk * a.split.chunk));
     const Scanner sc = scanner_of<Elem, LANES>(a.split, a.C, group, channel);
     const int64_t map_stride = static_cast<int64_t>(a.split.groups) * CH;
-    float2* maps = a.maps + static_cast<int64_t>(group) * CH + channel;
+    float2* maps = a.maps + group * CH + channel;
     // the gradient behind the tile at hand, or the map of the chunk's tiles so far
     float carry = !MAPS && sc.scans && a.dh_last ? a.dh_last[sc.n * a.C + sc.c] : 0.0f;
     float product = 1.0f;
@@ -659,6 +660,7 @@ __global__ __launch_bounds__(kStepThreads) void step_kernel(StepArgs<Elem> a) {
 // How a call is cut.
 struct Plan {
     Split split;
+    int64_t groups;
     int lanes, threads;
 };
 Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
@@ -667,8 +669,7 @@ Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
     p.split.runs = static_cast<int32_t>((C + V - 1) / V);
     p.split.columns = N * p.split.runs;
     p.lanes = dtype == kF32 || L <= kShort || p.split.columns >= 8 * kFull || p.split.columns < 4 * kFull ? 8 : 4;
-    const int64_t groups = (p.split.columns + p.lanes - 1) / p.lanes;
-    p.split.groups = static_cast<uint32_t>(std::min<int64_t>(groups, 0xffffffffLL));
+    const int64_t groups = p.groups = (p.split.columns + p.lanes - 1) / p.lanes;
     p.threads = L <= kShort ? short_threads(V) : kThreads;
     const bool one_launch = C % V == 0 && L <= kWalked * (kThreads / (8 * V) * kHeld);
     if (backward && L > kShort && p.lanes == 8 && (groups >= kFull || !one_launch)) p.threads = kGradPairs;
@@ -682,11 +683,17 @@ Plan plan_scan(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
     return p;
 }
 
+// launch(split, workgroups of the chunks' maps, workgroups).  HIP takes fewer than 2^32
+// threads: more groups than that go in several launches (they have one chunk).
 template <typename F> hipError_t launch_chunks(const Plan& p, F&& launch) {
-    const int64_t groups = p.split.groups, chunks = p.split.chunks;
-    const int64_t blocks = (groups * chunks + 7) / 8 * 8, ahead = (groups * (chunks - 1) + 7) / 8 * 8;
-    if (blocks * p.threads > 0xffffffffLL) return hipErrorInvalidValue;
-    launch(static_cast<unsigned>(ahead), static_cast<unsigned>(blocks));
+    const int64_t chunks = p.split.chunks, most = chunks > 1 ? p.groups : int64_t(0xffffffff) / p.threads / 8 * 8;
+    for (int64_t first = 0; first < p.groups; first += most) {
+        Split split = p.split;
+        const int64_t groups = std::min(p.groups - first, most);
+        split.first = first;
+        split.groups = static_cast<uint32_t>(groups);
+        launch(split, static_cast<unsigned>((groups * (chunks - 1) + 7) / 8 * 8), static_cast<unsigned>((groups * chunks + 7) / 8 * 8));
+    }
     return hipGetLastError();
 }
 
@@ -699,18 +706,19 @@ template <typename F> hipError_t launch_chunks(const Plan& p, F&& launch) {
 size_t gated_scan_workspace(int dtype, int64_t N, int64_t L, int64_t C, bool backward) {
     const Plan p = plan_scan(dtype, N, L, C, backward);
     if (p.split.chunks == 1) return 0;
-    return static_cast<size_t>(p.split.chunks - 1) * p.split.groups * p.lanes * (16 / dtype_bytes(dtype)) * sizeof(float2);
+    return static_cast<size_t>(p.split.chunks - 1) * p.groups * p.lanes * (16 / dtype_bytes(dtype)) * sizeof(float2);
 }
 
 template <int D> hipError_t launch_gated_scan_t(const wg_gated_scan& a, hipStream_t stream) {
     using Elem = typename DTypeOf<D>::type;
     constexpr int SHORT = short_threads(Vec<Elem>::V);
     const Plan p = plan_scan(D, a.N, a.L, a.C, false);
-    const ScanArgs<Elem> k{a.N, static_cast<int32_t>(a.L), static_cast<int32_t>(a.C), rows_of<const Elem>(a.gate),
-                           rows_of<const Elem>(a.value), rows_of<const Elem>(a.out_gate), rows_of<Elem>(a.y), a.h0,
-                           a.lengths, a.h_last, a.states, static_cast<float2*>(a.workspace), p.split};
+    ScanArgs<Elem> k{a.N, static_cast<int32_t>(a.L), static_cast<int32_t>(a.C), rows_of<const Elem>(a.gate),
+                     rows_of<const Elem>(a.value), rows_of<const Elem>(a.out_gate), rows_of<Elem>(a.y), a.h0,
+                     a.lengths, a.h_last, a.states, static_cast<float2*>(a.workspace), p.split};
     const bool out = a.out_gate.data != nullptr, full = a.C % Vec<Elem>::V == 0;
-    return launch_chunks(p, [&](unsigned ahead, unsigned grid) {
+    return launch_chunks(p, [&](const Split& split, unsigned ahead, unsigned grid) {
+        k.split = split;
 #define WG_SCAN_CASE(LANES, OUT, FULL)                                                                               \
     if constexpr (LANES == 8 || D != kF32)                                                                           \
         if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \
@@ -728,12 +736,13 @@ template <int D> hipError_t launch_gated_scan_backward_t(const wg_gated_scan_bac
     using Elem = typename DTypeOf<D>::type;
     constexpr int SHORT = short_threads(Vec<Elem>::V);
     const Plan p = plan_scan(D, a.N, a.L, a.C, true);
-    const GradArgs<Elem> k{a.N, static_cast<int32_t>(a.L), static_cast<int32_t>(a.C), rows_of<const Elem>(a.dy),
-                           rows_of<const Elem>(a.gate), rows_of<const Elem>(a.value), rows_of<const Elem>(a.out_gate),
-                           rows_of<Elem>(a.dgate), rows_of<Elem>(a.dvalue), rows_of<Elem>(a.dout_gate), a.states,
-                           a.dh_last, a.lengths, a.dh0, static_cast<float2*>(a.workspace), p.split};
+    GradArgs<Elem> k{a.N, static_cast<int32_t>(a.L), static_cast<int32_t>(a.C), rows_of<const Elem>(a.dy),
+                     rows_of<const Elem>(a.gate), rows_of<const Elem>(a.value), rows_of<const Elem>(a.out_gate),
+                     rows_of<Elem>(a.dgate), rows_of<Elem>(a.dvalue), rows_of<Elem>(a.dout_gate), a.states,
+                     a.dh_last, a.lengths, a.dh0, static_cast<float2*>(a.workspace), p.split};
     const bool out = a.out_gate.data != nullptr, full = a.C % Vec<Elem>::V == 0;
-    return launch_chunks(p, [&](unsigned ahead, unsigned grid) {
+    return launch_chunks(p, [&](const Split& split, unsigned ahead, unsigned grid) {
+        k.split = split;
 #define WG_SCAN_CASE(LANES, OUT, FULL)                                                                               \
     if constexpr (LANES == 8 || D != kF32)                                                                           \
         if (p.lanes == LANES && out == OUT && full == FULL) {                                                        \

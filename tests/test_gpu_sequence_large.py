@@ -94,3 +94,38 @@ def test_making_large_matrices():
     m, want = w.dequantize().view(-1, 16, cols), small.dequantize()
     for at in range(0, rows // 16, 2 ** 14):
         assert bool((m[at:at + 2 ** 14] == want).all()), at
+
+
+@pytest.mark.parametrize("shape", [(2 ** 21 + 3, 1, 1024), (1, 35, 2 ** 29 + 64)], ids=str)
+def test_scan_of_many_channels(shape):
+    """More channels than one launch has threads: many sequences of a step, and one
+    wide one."""
+    from paper_1905_05233_amd import sequence_ops as S
+    N, L, C = shape
+    some = 1024
+    parts = [torch.randn((1, L, some), device="cuda").bfloat16() for _ in range(3)]
+    want = S.gated_scan(*parts[:2], save_states=True)
+    grads = S.gated_scan_backward(parts[2], *parts[:2], want[2])
+    if N > 1:
+        wide = [p.expand(N, L, some) for p in parts]
+    else:   # every input row is the same memory, with the channels repeated
+        parts = [p[:, :1].expand(1, L, some) for p in parts]
+        want = S.gated_scan(*parts[:2], save_states=True)
+        grads = S.gated_scan_backward(parts[2], *parts[:2], want[2])
+        wide = [p[:, :1].repeat(1, 1, -(-C // some))[:, :, :C].expand(1, L, C) for p in parts]
+    y, h, s = S.gated_scan(*wide[:2], save_states=True)
+
+    def same(got, ref):   # [N or 1][..][C] against [1][..][some]
+        if N > 1:
+            return all(bool((got[at:at + 2 ** 18] == ref).all()) for at in range(0, N, 2 ** 18))
+        whole = C // some * some
+        ok = torch.equal(got[..., whole:], ref[..., :C - whole])
+        for l in range(0, whole, 2 ** 24):
+            part = got[..., l:min(l + 2 ** 24, whole)]
+            ok = ok and bool((part.unflatten(-1, (-1, some)) == ref.unsqueeze(-2)).all())
+        return ok
+
+    assert same(y, want[0]) and same(h, want[1]) and same(s, want[2])
+    del y, h
+    dz, dv, _, dh = S.gated_scan_backward(wide[2], *wide[:2], s)
+    assert same(dz, grads[0]) and same(dv, grads[1]) and same(dh, grads[3])
