@@ -178,6 +178,8 @@ def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_s
     states = None
     if save_states:
         states = _new_f32(gate, Nn, -(-L // SCAN_BLOCK), C)
+    if Nn == 0:   # the library takes one sequence and more
+        return (y, h_last, states) if save_states else (y, h_last)
     need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 0)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan(
@@ -216,6 +218,8 @@ def gated_scan_backward(dy, gate, value, states, out_gate=None, dh_last=None, le
     dvalue, vr = _out(out[1], "dvalue", gate, dt, dev)
     dout_gate, outr = (None, _NO_ROWS) if out_gate is None else _out(out[2], "dout_gate", gate, dt, dev)
     dh0 = _new_f32(gate, Nn, C)
+    if Nn == 0:
+        return dgate, dvalue, dout_gate, dh0
     need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 1)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan_backward(
