@@ -463,7 +463,8 @@ wg_status winograd_gated_step(const wg_gated_step* args, hipStream_t stream);
  *   s = max(max |y|, 2^-100) / 448 of each group of `group` channels (32, 64 or
  *   128; 0: the whole row; the last group may be short), y = e4m3(y / s),
  * scales fp32 [N][L][ceil(C / group)] (one a row for group 0), contiguous.
- * r may be x or residual itself (the same rows).  N, L >= 0, 1 <= C <= 2^25. */
+ * r may be x or residual itself (the same rows).  eps is used in fp32, and finite and
+ * not negative there.  N, L >= 0, 1 <= C <= 2^25. */
 typedef struct {
     int64_t dtype, N, L, C;
     wg_rows x, residual, r, y;

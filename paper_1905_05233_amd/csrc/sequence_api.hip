@@ -196,7 +196,8 @@ wg_status winograd_rms_norm(const wg_rms_norm* a, hipStream_t stream) {
         const int64_t N = a->N, L = a->L, C = a->C, es = wg::dtype_bytes(static_cast<int>(a->dtype));
         WG_TRY(check_sizes(N, L, C, 0, 0));
         WG_TRY(check_row(C));
-        if (!std::isfinite(a->eps) || a->eps < 0) return fail(WG_ERR_ARG, "eps must be finite and not negative");
+        if (!std::isfinite(static_cast<float>(a->eps)) || a->eps < 0)
+            return fail(WG_ERR_ARG, "eps must be finite in fp32 and not negative");
         if (N == 0 || L == 0) return WG_OK;
         WG_TRY(check_rows(a->x, "x", N, L, C, es, false));
         if (a->residual.data) WG_TRY(check_rows(a->residual, "residual", N, L, C, es, false));
@@ -227,7 +228,8 @@ wg_status winograd_rms_norm_backward(const wg_rms_norm_backward* a, hipStream_t 
         const int64_t N = a->N, L = a->L, C = a->C, es = wg::dtype_bytes(static_cast<int>(a->dtype));
         WG_TRY(check_sizes(N, L, C, 0, 0));
         WG_TRY(check_row(C));
-        if (!std::isfinite(a->eps) || a->eps < 0) return fail(WG_ERR_ARG, "eps must be finite and not negative");
+        if (!std::isfinite(static_cast<float>(a->eps)) || a->eps < 0)
+            return fail(WG_ERR_ARG, "eps must be finite in fp32 and not negative");
         WG_TRY(check_rows(a->dy, "dy", N, L, C, es, false));
         WG_TRY(check_rows(a->r, "r", N, L, C, es, false));
         if (a->dr.data) WG_TRY(check_rows(a->dr, "dr", N, L, C, es, false));
