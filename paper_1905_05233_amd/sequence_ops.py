@@ -111,9 +111,10 @@ def _new_f32(like, *shape):
     return torch.empty_strided(shape, strides, dtype=torch.float32, device=like.device)
 
 
-def _size(query, *args):
-    """Bytes of workspace, asked of the library once for given sizes."""
-    key = (query, args)
+def _size(query, dev, *args):
+    """Bytes of workspace on the current device, dev, asked of the library once for given
+    sizes: they go by the device's compute units too."""
+    key = (query, dev, args)
     need = _sizes.get(key)
     if need is None:
         out = ctypes.c_size_t()
@@ -180,7 +181,7 @@ def gated_scan(gate, value, out_gate=None, h0=None, lengths=None, y=None, save_s
         states = _new_f32(gate, Nn, -(-L // SCAN_BLOCK), C)
     if Nn == 0:   # the library takes one sequence and more
         return (y, h_last, states) if save_states else (y, h_last)
-    need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 0)
+    need = _size("winograd_gated_scan_workspace", dev, code, Nn, L, C, 0)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan(
         _pack_scan(code, Nn, L, C, *g, *v, *o, *yr, h0p, lp, h_last.data_ptr(),
@@ -220,7 +221,7 @@ def gated_scan_backward(dy, gate, value, states, out_gate=None, dh_last=None, le
     dh0 = _new_f32(gate, Nn, C)
     if Nn == 0:
         return dgate, dvalue, dout_gate, dh0
-    need = _size("winograd_gated_scan_workspace", code, Nn, L, C, 1)
+    need = _size("winograd_gated_scan_workspace", dev, code, Nn, L, C, 1)
     ws = _workspace(need, gate)
     st = N.lib().winograd_gated_scan_backward(
         _pack_scan_backward(code, Nn, L, C, *d, *g, *v, *o, *zr, *vr, *outr, sp, dhp, lp, dh0.data_ptr(),
@@ -322,7 +323,7 @@ def rms_norm_backward(dy, r, weight, dr=None, eps=1e-6, dx=None, stream=None):
     wp = _dense(weight, "weight", (C,), dt, dev)
     dx, xr = _out(dx, "dx", r, dt, dev)
     dweight = torch.empty_like(weight, dtype=torch.float32)
-    need = _size("winograd_rms_norm_workspace", code, Nn, L, C)
+    need = _size("winograd_rms_norm_workspace", dev, code, Nn, L, C)
     ws = _workspace(need, r)
     st = N.lib().winograd_rms_norm_backward(
         _pack_norm_backward(code, Nn, L, C, *d, *rr, *dd, *xr, wp, dweight.data_ptr(), eps,
