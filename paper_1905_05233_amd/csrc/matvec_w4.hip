@@ -81,7 +81,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr int kTokens = 16;     // rows of x that a wave takes
-constexpr int kUnits = 256;     // compute units of the chip
 
 template <bool F16> __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, const f32x4& c) {
     if constexpr (F16)
@@ -385,7 +384,7 @@ template <int XD, int GPT, bool XG> hipError_t matvec_t(const MatvecArgs& k, hip
     // workgroups share a unit (512 -> 8192 3.6, 3.9); fp32 rows with groups of 32 spill
     // 28 registers (4096 -> 5000 15.2, 16.6).
     if constexpr (XD != 0 || GPT != 4)
-        if (k.w.ktiles >= 8 && (k.w.rows + 15) / 16 * ((k.M + kTokens - 1) / kTokens) > kUnits)
+        if (k.w.ktiles >= 8 && (k.w.rows + 15) / 16 * ((k.M + kTokens - 1) / kTokens) > device_cu_count())
             return matvec_r<XD, GPT, XG, 2>(k, stream);
     return matvec_r<XD, GPT, XG, 1>(k, stream);
 }
