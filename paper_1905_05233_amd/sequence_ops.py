@@ -338,7 +338,7 @@ class W4Matrix:
     or 128) columns of a row: tiles int32 [ceil(rows/16)][ceil(cols/128)][4][16][4]
     and scales bf16 [ceil(rows/16)][ceil(cols/group)][16] in the library's layout.
     Its attributes are what it was made of and cannot be set."""
-    __slots__ = ("_tiles", "_scales", "_rows", "_cols", "_group", "_packed")
+    __slots__ = ("_tiles", "_scales", "_rows", "_cols", "_group", "_dev", "_packed")
     tiles = property(lambda self: self._tiles)
     scales = property(lambda self: self._scales)
     rows = property(lambda self: self._rows)
@@ -358,14 +358,16 @@ class W4Matrix:
         rt = -(-self._rows // 16)
         tp = _dense(self._tiles, "tiles", (rt, -(-self._cols // 128), 4, 16, 4), torch.int32, dev)
         sp = _dense(self._scales, "scales", (rt, -(-self._cols // self._group), 16), torch.bfloat16, dev)
-        self._packed = (tp, sp, self._rows, self._cols, self._group)
+        self._dev, self._packed = dev, (tp, sp, self._rows, self._cols, self._group)
 
     def _words(self, dev):
-        """The argument's words.  Tensors that were given other memory since they were
-        last checked are checked again."""
+        """The argument's words for a call on dev.  Tensors that were given other memory
+        since they were last checked are checked again."""
         packed = self._packed
         if self._tiles.data_ptr() != packed[0] or self._scales.data_ptr() != packed[1]:
             self._check(dev)
+        elif self._dev != dev:
+            raise ValueError("w must be on the GPU of the other tensors")
         return self._packed
 
     @classmethod
@@ -433,8 +435,7 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
     M, rows = x.shape[0], w._rows
     xp, _, ldx = _rows(x, "x", (M, w._cols), xdt, dev)
     xcode = _E4M3 if x8 else _code(x, "x")
-    if w._tiles.get_device() != dev:
-        raise ValueError("w must be on the GPU of the other tensors")
+    words = w._words(dev)
     sp, groups = 0, 0
     if x8:
         if not isinstance(x_scales, torch.Tensor) or x_scales.dim() != 2:
@@ -453,7 +454,7 @@ def matvec_w4(x, w, x_scales=None, y=None, dtype=None, stream=None):
             raise TypeError("dtype is that of y")
         yp, _, ldy = _rows(y, "y", (M, rows), y.dtype, dev)
     st = N.lib().winograd_matvec_w4(
-        _pack_matvec(*w._words(dev), M, xcode, _code(y, "y"), xp, ldx, sp, groups, yp, ldy), _raw_stream(None))
+        _pack_matvec(*words, M, xcode, _code(y, "y"), xp, ldx, sp, groups, yp, ldy), _raw_stream(None))
     if st != N.WG_OK:
         N.check(st)
     return y
