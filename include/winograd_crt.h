@@ -464,7 +464,8 @@ wg_status winograd_gated_step(const wg_gated_step* args, hipStream_t stream);
  *   128; 0: the whole row; the last group may be short), y = e4m3(y / s),
  * scales fp32 [N][L][ceil(C / group)] (one a row for group 0), contiguous.
  * r may be x or residual itself (the same rows).  eps is used in fp32, and finite and
- * not negative there.  N, L >= 0, 1 <= C <= 2^25. */
+ * not negative there.  The sum of squares is fp32's too: a row that exceeds its range
+ * (values of some 1e19) gives 0.  N, L >= 0, 1 <= C <= 2^25. */
 typedef struct {
     int64_t dtype, N, L, C;
     wg_rows x, residual, r, y;

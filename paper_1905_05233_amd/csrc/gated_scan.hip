@@ -21,12 +21,14 @@
 // workgroup each: a first kernel composes each chunk's map (reading the gates a
 // second time), the second one starts each chunk from the maps ahead of it.
 //
-// What bounds it: memory, for many channels (64 x 512 x 2048 in bf16: 118 us
-// forward, 4.6 TB/s; 204 us backward, 4.6 TB/s), held back where a workgroup's runs
+// What bounds it: memory, for many channels (64 x 512 x 2048 in bf16: 117 us
+// forward, 4.6 TB/s; 203 us backward, 4.6 TB/s), held back where a workgroup's runs
 // are 64 bytes long: a card copies those at 3.8 TB/s, runs of 128 bytes at 4.8.
-// 16 x 4096 x 512, of 64-byte runs: 74 us forward (3.6 TB/s), 114 us backward (4.1).
+// 16 x 4096 x 512, of 64-byte runs: 69 us forward (3.9 TB/s), 122 us backward (3.9).
 // One sequence of 16381 x 512 reads its gates twice: 10 + 15 us, 67 MB of inputs and
-// outputs (2.9 TB/s for the call).  A few short sequences take one tile's latency.
+// outputs (2.7 TB/s).  A few short sequences take one tile's latency.
+// Times here and below are the kernels' own in replayed graphs over several sets of
+// inputs, both launches of a call in chunks together.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -44,28 +46,29 @@ namespace {
 constexpr int kStepThreads = 256;
 constexpr int kScanBlock = WG_SCAN_BLOCK;
 // Gates that a thread holds of a tile: with 32 the gradients spill registers, and the
-// forward pass of 64 x 512 x 2048 bf16 takes 132 us instead of 118.
+// forward pass of 64 x 512 x 2048 bf16 takes an eighth longer.
 constexpr int kHeld = 16;
 
 // Which form a call takes.  LANES, 16-byte runs of a group: 8 make a 128-byte run of
 // channels, 4 a 64-byte one with twice as many groups.  8 where that still gives
-// kFull groups (three quarters of the compute units; 64 x 512 x 2048 bf16: 118 us
-// against 139 forward, 204 against 237 backward), and where the length is cut into
-// chunks anyway (16381 x 512 backward: 43 against 50 us).  4 in between
-// (16 x 4096 x 512, 128 groups of 128 bytes or 256 of 64: 74 against 101 us forward,
-// 127 against 161 backward).  fp32 has one form.
+// kFull groups (three quarters of the compute units; 64 x 512 x 2048 bf16: 117 us
+// against 134 forward, 203 against 245 backward), and where the length is cut into
+// chunks anyway, to as many workgroups with either.  4 in between
+// (16 x 4096 x 512, 256 groups of 64 bytes, or 128 of 128 in chunks: 69 against 81 us
+// forward, 122 against 138 backward; without chunks 100 and 186).  fp32 has one form.
 constexpr int64_t kFull = 192;
 // Chunks, where there are fewer groups than kFull: so many that there are kChunked
-// workgroups (16381 x 512 forward: 25.2 us; with 256 28.0, with 1024 26.4), and at
-// most kMostChunks, whose maps each chunk composes (32768 x 64: 16.9 us forward, with
-// 64 chunks 22.0).  Sequences of kWalked tiles or fewer are walked (3 to 4 us a tile,
-// against a second launch and its workspace, 5 us of the host's time); 8 tiles of the
-// gradients of 4 x 1000 x 96 fp32 cost 22.6 us walked, 4 + 6 in chunks.
+// workgroups (16381 x 512: 26.9 us forward and 43.7 backward; with 256 27.3 and 47.7,
+// with 1024 32.8 and 47.7), and at most kMostChunks, whose maps each chunk composes
+// (32768 x 64: 18.0 and 23.0 us, with 64 chunks 22.9 and 37.4, with 128 17.8 and 25.6).
+// Sequences of kWalked tiles or fewer are walked: a second launch and its workspace
+// cost the host 5 us.  Four tiles of 4 x 1000 x 96 fp32 take 12.9 us forward and 17.5
+// backward, in chunks 10.2 and 11.2; eight tiles of the gradients cost 22.6.
 constexpr int64_t kChunked = 512, kMostChunks = 256, kWalked = 4;
 // Threads of a workgroup.  The gradients hold twice the values: with kGradPairs of them
-// two workgroups share a compute unit (64 x 512 x 2048: 204 us, with 512 threads 225).
+// two workgroups share a compute unit (64 x 512 x 2048: 203 us, with 512 threads 211).
 // More threads are better where there is one group a compute unit, for the loads in
-// flight (16 x 4096 x 512: 127 us with 512, 137 with 256), and where their longer tiles
+// flight (16 x 4096 x 512: 122 us with 512, 132 with 256), and where their longer tiles
 // save the second launch: training 8 x 400 x 256 bf16 takes 27 us a pass instead of 32,
 // but 3 x 500 x 75 fp16, whose short runs make slow tiles, 39 instead of 32.
 constexpr int kThreads = 512, kGradPairs = 256;
@@ -76,9 +79,10 @@ constexpr int short_threads(int V) { return 2 * 8 * V; }
 // LANES: 16-byte runs of channels of a workgroup
 template <typename Elem, int LANES> constexpr int kChannels = LANES * (16 / static_cast<int>(sizeof(Elem)));
 
-// sigmoid(z) and sigmoid(-z), both to fp32 accuracy for any z (1 - f would lose
-// the small one): with e = exp(-z) they are 1 / (1 + e) and e / (1 + e), which is 1
-// where e is large (e may be infinite); NaN stays NaN.
+// sigmoid(z) and sigmoid(-z), each within some (|z| + 8) 2^-24 of its own size (|z| from
+// the exponent's rounding; 1 - f would lose the small one): with e = exp(-z) they are
+// 1 / (1 + e) and e / (1 + e), which is 1 where e is large (e may be infinite); NaN stays
+// NaN.
 struct Gate {
     float f, i;
 };
@@ -203,9 +207,10 @@ __device__ __forceinline__ float reach_chunk(const float2* maps, int64_t stride,
 // Which (chunk, group) a workgroup takes, all groups of chunk 0 first.  Workgroups go
 // to the eight XCDs in turn.  Where groups share lines (halves of one, for groups of 64
 // bytes; any, where a row is no whole number of groups), each XCD takes a run of the
-// order instead, so that a line is fetched into one L2: 12 x 4000 x 136 bf16 24 us, in
-// turn 32; 16 x 4096 x 512 in groups of 64 bytes 74 and 87.  Where they do not, in turn
-// is better (16381 x 512: 23.4 us, in runs 25.3).
+// order instead, so that a line is fetched into one L2: 12 x 4000 x 136 bf16 25 us forward
+// and 40 backward, in turn 34 and 56; 16 x 4096 x 512 in groups of 64 bytes 69 and 122, in
+// turn 87 and 143.  Where they do not, in turn is better (16381 x 512: 26.9 and 43.7, in
+// runs 28.3 and 45.5).
 struct Share {
     int64_t group;
     int chunk;   // from `chunks` on: none
@@ -637,7 +642,8 @@ template <typename Elem> struct StepArgs {
     float* h_new;
 };
 
-// One thread per channel of a sequence: 16 x 512 take 2.6 us, a launch's latency.
+// One thread per channel of a sequence: 16 x 512 take 2.4 us, a launch's latency;
+// 256 x 4096 bf16 4.8 us, of which 16.8 MB at a copy's rate are 3.2.
 template <typename Elem>
 __global__ __launch_bounds__(kStepThreads) void step_kernel(StepArgs<Elem> a) {
     using S = Storage<Elem>;

@@ -72,9 +72,11 @@ __device__ __forceinline__ int code_of(uint32_t word, int j) {
 // Measured: 25088 -> 4096 for one bf16 row, 53 MB, 12.7 us a call: 4.2 TB/s; it is
 // bound by memory and the waves' start and end (a copy moves as much in 10.2).  4096 ->
 // 1000 for five fp32 rows 8 us, 1536 -> 1536 for sixteen 8-bit rows 5 us: latency, 63 and
-// 96 workgroups.  Sixteen rows of 25088 take twice as long as one (30 against 14 us):
-// every workgroup reads all of x through its L1.  4096 -> 32768 takes 20.4 us on the GPU
-// for one row and 26.9 for sixteen, 69 MB: 3.4 and 2.6 TB/s.
+// 96 workgroups.  Sixteen rows of 25088 take twice as long as one (30 against 15.6 us):
+// every workgroup reads all of x through its L1.  4096 -> 32768 takes 21.4 us on the GPU
+// for one row and 28.5 for sixteen, 69 MB: 3.2 and 2.4 TB/s.  fp32 rows, three products a
+// fragment and rebuilt weights, are bound by that work: 25088 -> 4096 34 us for one row and
+// 53 for sixteen, 4096 -> 4096 8.1 for one (bf16 4.8).
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -290,7 +292,9 @@ unsigned blocks_for(int64_t items) {
     return static_cast<unsigned>(std::min<int64_t>((items + kW4Threads - 1) / kW4Threads, 0xffffffffLL / kW4Threads));
 }
 
-// One thread per group of a row (padding rows too).
+// One thread per group of a row (padding rows too).  Plain kernels, since matrices are made
+// once: 4096 x 25088 from bf16 3.2 ms, from codes 0.09 ms, back into bf16 0.13 ms (4096 x
+// 4096: 135, 20 and 26 us).
 template <typename Elem>
 __global__ __launch_bounds__(kW4Threads) void quantize_kernel(W4 w, const Elem* m, int64_t ldm, int64_t items) {
     const int64_t groups = w.ktiles * 128 / w.group;

@@ -13,10 +13,11 @@
 // order.  Rows too long for that are read twice (three times by the gradients).
 //
 // 65536 rows of 512 bf16 with the residual into 8 bits with scales for every 128
-// channels, 236 MB: 50 us, 4.7 TB/s (a copy of 1 GiB 5.2); their gradients, 268 MB:
-// 51 + 5 us, 4.8 TB/s.  Rows that are no whole runs of 16 bytes start at odd addresses:
-// 511 channels instead of 512 take 63 us instead of 50.  3001 rows of 1000 fp16, 24 MB:
-// 7 us.  A few rows take 3.5 us, a launch's latency and a row's.
+// channels, 236 MB: 46 us in replayed graphs, 5.1 TB/s (a copy of 1 GiB 5.2), 50 a call;
+// their gradients, 268 MB: 54 us for both kernels, 5.0 TB/s.  Rows that are no whole runs
+// of 16 bytes start at odd addresses: 511 channels instead of 512 take 57 us instead of
+// 46.  3001 rows of 1000 fp16, 24 MB: 6.3 us.  A few rows take 3.1 us, a launch's latency
+// and a row's.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -266,7 +267,10 @@ __device__ __forceinline__ float block_sum(float v, float* lds) {
     return v;
 }
 
-// Rows of any length, one workgroup each, read again for the output.
+// Rows of any length, one workgroup each, read again for the output.  A plain form for
+// what the registers do not hold: 300 rows of 40000 bf16 with the residual take 174 us,
+// into 8 bits with a scale a row 243, with scales for every 32 channels, two barriers
+// each, 1200 (a floor of 16 to 18); their gradients 275.
 template <typename Elem, bool QUANT>
 __global__ __launch_bounds__(kNormThreads) void norm_long_kernel(NormArgs<Elem> a) {
     using S = Storage<Elem>;
@@ -412,7 +416,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs<E
 }
 
 // dweight from its parts: 16 channels a workgroup, the parts over 64 threads a
-// channel, eight of them in flight (1024 parts of 512 channels: 3 us).
+// channel, eight of them in flight (1280 parts of 512 channels, 2.6 MB: 4.8 us).
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* partial, int64_t parts, int64_t C, float* dweight) {
     constexpr int kChannels = 16, kSlices = 64;
     __shared__ float lds[kSlices][kChannels + 1];

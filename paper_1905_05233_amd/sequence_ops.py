@@ -14,6 +14,10 @@ a buffer with a leading row); states, scales and weights are contiguous.  Calls
 are asynchronous on ``stream`` or the current stream; work that another stream
 has still to do on the inputs is the caller's to wait for.  Outputs must not overlap
 inputs, unless said otherwise.
+
+Autograd sees nothing of these calls: results carry no graph, also where inputs
+require gradients.  Gradients come from the ``_backward`` calls (the 4-bit products have
+none), from within a ``torch.autograd.Function`` where a graph is wanted.
 """
 import ctypes
 import struct
