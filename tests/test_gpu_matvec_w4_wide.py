@@ -54,8 +54,9 @@ def test_whole_numbers(K, group, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "fp8"])
 @pytest.mark.parametrize("shape", [(1, 25088, 64), (16, 25088, 48), (5, 4096, 1000), (3, 1000, 4500), (2, 1409, 4112)], ids=str)
 def test_within_the_order_of_the_sums(shape, dtype):
-    """fp32 outputs meet the weights themselves, whatever x's type: no bits are lost to
-    an offset.  Beside the bound, the size of the error: with a rounding of 0.6 2^-24 of the
+    """fp32 outputs within the bound of sums of the weights themselves, whatever x's type:
+    rows in bf16 and e4m3, which meet codes with an offset, must lose nothing to it (their
+    products have few bits).  Beside the bound, the size of the error: with a rounding of 0.6 2^-24 of the
     partial sum for each column, and partial sums that grow as the root of their columns,
     a group's sum of 128 is off by 8 * 0.6 2^-24 = 2.8e-7 of its size, and the output by
     as much; 50 sums of groups in a wave add 1.7e-7 and 16 waves 1e-7, together 3.5e-7.

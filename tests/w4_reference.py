@@ -3,8 +3,8 @@ in which the kernel adds.
 
 A group's columns are added in the matrix cores' fp32 accumulator, one rounding a
 column and part at most, of partial sums that are at most the sum of all terms'
-sizes; 16-bit outputs start from the product with the codes' offset, so that a term is
-|x| times offset + 8 + offset's own.  The group's sum times its scale is added to a
+sizes.  With codes that carry an offset, taken out by a product of its own, a term would be
+|x| times up to 2 offset + 15.  The group's sum times its scale is added to a
 wave's sum (two roundings a group of its tiles, with the row scale of 8 bits a third), and
 up to 16 waves' sums to the output's.  Products of two 16-bit numbers are exact in fp32.
 """
