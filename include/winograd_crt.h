@@ -539,6 +539,123 @@ wg_status winograd_pack_w4(const wg_w4* w, const void* nibbles, const void* scal
 /* The matrix m [rows][cols] (dtype, rows ldm elements apart) that w stands for. */
 wg_status winograd_dequantize_w4(const wg_w4* w, wg_dtype dtype, void* m, int64_t ldm, hipStream_t stream);
 
+/* Heads of contiguous channels of a tensor [N][L][H][D] in a storage dtype, at
+ * data + n * stride_n + l * stride_l + h * stride_h, as wg_rows. */
+typedef struct {
+    const void* data;
+    int64_t stride_n, stride_l, stride_h;
+} wg_heads;
+
+/* Linear attention with a decay for each head.  Of a sequence n and a head h, with a
+ * state S [Dk][Dv] that starts from s0 (NULL: zeros):
+ *   S[l] = exp(log_decay[h]) S[l-1] + k[l] v[l]^T,   y[l] = scale S[l]^T q[l].
+ * q [N][L][q_heads][Dk], k [N][L][k_heads][Dk], v [N][L][v_heads][Dv] and
+ * y [N][L][heads][Dv] are in dtype; q_heads, k_heads and v_heads divide heads, and
+ * head h reads q's head h / (heads / q_heads), and so on.  log_decay fp32 [heads],
+ * s0 and s_last (the state after the last step, NULL: not wanted) fp32
+ * [N][heads][Dk][Dv] and lengths [N] are contiguous; log_decay is 0 or less (minus
+ * infinity: nothing is kept).  lengths (NULL: every sequence has L steps; values are
+ * clipped to [0, L]): steps from lengths[n] on are padding; nothing there is used, y
+ * is 0 and the state stays.  An infinity or NaN at a step reaches no y ahead of it.
+ * workspace: of winograd_linear_attention_workspace bytes, 16-byte aligned (NULL if
+ * that is 0).  N >= 1, 0 <= L <= 2^31 - 2^16, heads <= 65536, 1 <= Dk, Dv <= 256. */
+typedef struct {
+    int64_t dtype, N, L, q_heads, k_heads, v_heads, heads, Dk, Dv;
+    wg_heads q, k, v, y;
+    const float* log_decay;
+    const float* s0;
+    const int32_t* lengths;
+    float* s_last;
+    double scale;
+    void* workspace;
+    int64_t workspace_bytes;
+} wg_linear_attention;
+wg_status winograd_linear_attention(const wg_linear_attention* args, hipStream_t stream);
+
+/* Its gradients, from dy [N][L][heads][Dv] and ds_last (fp32 [N][heads][Dk][Dv], NULL:
+ * zeros): dq, dk and dv, shaped as q, k and v, in dtype (0 at padding; where heads share
+ * an input, the sum over them, rounded once) and ds0 fp32 [N][heads][Dk][Dv] (NULL: not
+ * wanted).  q, k, v, log_decay, s0, lengths and scale are the forward call's.  The
+ * decays are constants here: they have no gradient. */
+typedef struct {
+    int64_t dtype, N, L, q_heads, k_heads, v_heads, heads, Dk, Dv;
+    wg_heads dy, q, k, v, dq, dk, dv;
+    const float* log_decay;
+    const float* s0;
+    const float* ds_last;
+    const int32_t* lengths;
+    float* ds0;
+    double scale;
+    void* workspace;
+    int64_t workspace_bytes;
+} wg_linear_attention_backward;
+wg_status winograd_linear_attention_backward(const wg_linear_attention_backward* args, hipStream_t stream);
+
+/* Bytes of workspace that the attention (backward = 0) or its gradients (1) need, by the
+ * sizes of args alone (of its tensors nothing is read). */
+wg_status winograd_linear_attention_workspace(const wg_linear_attention* args, int backward, size_t* bytes);
+
+/* One step for N sequences: q [N][q_heads][Dk], k, v and y likewise (stride_l is not
+ * used), s and s_new contiguous fp32 [N][heads][Dk][Dv] states ahead of and after the
+ * step; s_new may be s. */
+typedef struct {
+    int64_t dtype, N, q_heads, k_heads, v_heads, heads, Dk, Dv;
+    wg_heads q, k, v, y;
+    const float* log_decay;
+    const float* s;
+    float* s_new;
+    double scale;
+} wg_linear_attention_step;
+wg_status winograd_linear_attention_step(const wg_linear_attention_step* args, hipStream_t stream);
+
+/* The root-mean-square norm of each head of queries and keys, with the rotation by their
+ * position: of a head's D channels x at position p, with weight [D] in dtype,
+ *   u = x / sqrt(mean(x^2) + eps) * weight,
+ * and of each pair i < R / 2 of its first R channels, (i, i + R / 2) or, with adjacent,
+ * (2 i, 2 i + 1), turned by the angle a = p f_i:
+ *   (u_a cos a - u_b sin a, u_a sin a + u_b cos a).
+ * Channels from R on are u.  q and q_out are [N][L][q_heads][D], k and k_out
+ * [N][L][k_heads][D] in dtype; q_out may be q and k_out k (the same rows).  turns: R / 2
+ * 64-bit words, f_i / (2 pi) modulo 1 as a fraction of 2^64 (f_i radians a position).
+ * positions int32 [N][L], contiguous (NULL: start + l).  eps is used in fp32, and finite
+ * and not negative there; the sum of squares is fp32's.  N, L >= 0, q_heads + k_heads <=
+ * 65536, 2 <= R <= D <= 256, R even, -2^31 <= start < 2^31. */
+typedef struct {
+    int64_t dtype, N, L, q_heads, k_heads, D, R, adjacent;
+    wg_heads q, k, q_out, k_out;
+    const void* q_weight;
+    const void* k_weight;
+    const void* turns;
+    const int32_t* positions;
+    int64_t start;
+    double eps;
+} wg_head_norm_rotate;
+wg_status winograd_head_norm_rotate(const wg_head_norm_rotate* args, hipStream_t stream);
+
+/* Its gradients, from dq_out and dk_out, those of q_out and k_out: dq and dk in dtype
+ * (dq may be dq_out, dk dk_out) and dq_weight, dk_weight fp32 [D], summed in a fixed
+ * order.  The other arguments are the forward call's.  workspace: of
+ * winograd_head_norm_rotate_workspace bytes, 16-byte aligned. */
+typedef struct {
+    int64_t dtype, N, L, q_heads, k_heads, D, R, adjacent;
+    wg_heads dq_out, dk_out, q, k, dq, dk;
+    const void* q_weight;
+    const void* k_weight;
+    const void* turns;
+    const int32_t* positions;
+    int64_t start;
+    double eps;
+    float* dq_weight;
+    float* dk_weight;
+    void* workspace;
+    int64_t workspace_bytes;
+} wg_head_norm_rotate_backward;
+wg_status winograd_head_norm_rotate_backward(const wg_head_norm_rotate_backward* args, hipStream_t stream);
+
+/* Bytes of workspace of the gradients; heads = q_heads + k_heads. */
+wg_status winograd_head_norm_rotate_workspace(wg_dtype dtype, int64_t N, int64_t L, int64_t heads, int64_t D, int64_t R,
+                                              int adjacent, size_t* bytes);
+
 /* Message describing the last error of the calling thread ("" if none). */
 const char* winograd_last_error(void);
 

@@ -123,6 +123,14 @@ def lib():
         "winograd_quantize_w4": (ctypes.c_int, [ctypes.c_char_p, ctypes.c_int, P, i64, P]),
         "winograd_pack_w4": (ctypes.c_int, [ctypes.c_char_p, P, P, P]),
         "winograd_dequantize_w4": (ctypes.c_int, [ctypes.c_char_p, ctypes.c_int, P, i64, P]),
+        "winograd_linear_attention": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_linear_attention_backward": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_linear_attention_workspace": (ctypes.c_int, [ctypes.c_char_p, ctypes.c_int, ctypes.POINTER(sz)]),
+        "winograd_linear_attention_step": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_head_norm_rotate": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_head_norm_rotate_backward": (ctypes.c_int, [ctypes.c_char_p, P]),
+        "winograd_head_norm_rotate_workspace": (ctypes.c_int, [ctypes.c_int] + [i64] * 5 + [ctypes.c_int,
+                                                                                           ctypes.POINTER(sz)]),
         "winograd_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sigs.items():

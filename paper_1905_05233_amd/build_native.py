@@ -45,6 +45,10 @@ UNITS = [
     ("gated_scan.hip", DEVICE, "gated_scan.o"),
     ("rms_norm.hip", DEVICE, "rms_norm.o"),
     ("matvec_w4.hip", DEVICE, "matvec_w4.o"),
+    ("linear_attention.hip", DEVICE + ["-DWG_DTYPE=0"], "linear_attention_f32.o"),
+    ("linear_attention.hip", DEVICE + ["-DWG_DTYPE=1"], "linear_attention_f16.o"),
+    ("linear_attention.hip", DEVICE + ["-DWG_DTYPE=2"], "linear_attention_bf16.o"),
+    ("head_norm_rotate.hip", DEVICE, "head_norm_rotate.o"),
 ]
 
 

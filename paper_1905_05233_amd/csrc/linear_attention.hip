@@ -1,0 +1,690 @@
+// Linear attention with a decay for each head, its gradients and its single step on
+// gfx950.  With lambda = exp(log_decay) of a head and its state S [Dk][Dv],
+//   S[t] = lambda S[t-1] + k[t] v[t]^T,   y[t] = scale S[t]^T q[t].
+// Steps are taken in tiles of T.  Within a tile, counted from 0 and with S the state
+// ahead of it,
+//   y[i] = scale (lambda^(i+1) S^T q[i] + sum_(j<=i) lambda^(i-j) (q[i].k[j]) v[j])
+//   S'   = lambda^T S + sum_j lambda^(T-1-j) k[j] v[j]^T,
+// which are four matrix products.  The gradients are the same products again, in
+// other roles: dq is linear attention of (dy, v, k), and with the steps in reverse
+// dk that of (v, dy, q) and dv that of (k, q, dy), where the state of the reversed
+// ones is G, the gradient at the state, for which in a tile
+//   y[i] = lambda^(T-1-i) G^T q[i] + scale sum_(j>=i) lambda^(j-i) (q[i].k[j]) v[j]
+//   G'   = lambda^T G + scale sum_j lambda^(j+1) k[j] v[j]^T.
+// So one kernel makes all of them (a "pass"; its q, k, v are the roles above).
+//
+// All products are the matrix cores' bf16 ones, with sums in fp32.  A value that 8
+// bits do not hold goes in as the sum of two or three bf16 parts, each the rounding
+// of what the ones ahead of it leave: fp16 inputs are exact in two, fp32 ones in
+// three; the state, the weights q.k and the decayed v are held in fp32 and enter in
+// two parts (2^-16 of a value is left) or, for fp32 rows, three.  Products of parts
+// below that are left out.  bf16 has fp32's range, so no state overflows on the way.
+//
+// A workgroup takes a head of a sequence and a block of v's columns, whose state stays
+// in the registers of its four waves, a quarter of the columns each; q, k and v of a
+// tile stand in LDS, and the weights of the tile pass through it.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "device_common.hpp"
+#include "kernels.hpp"
+#include "rows.hpp"
+#include "sequence.hpp"
+
+namespace wg {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// bf16 parts of an input, and of a value computed in fp32
+template <typename Elem> constexpr int kParts = std::is_same_v<Elem, bf16_t> ? 1 : std::is_same_v<Elem, _Float16> ? 2 : 3;
+template <typename Elem> constexpr int kSums = std::is_same_v<Elem, float> ? 3 : 2;
+// steps of a tile
+template <typename Elem> constexpr int kTile = std::is_same_v<Elem, bf16_t> ? 64 : 32;
+
+// Heads of one tensor: [N][L][H][D] with the channels contiguous; `per` of the
+// attention's heads read each.
+struct HeadsIn {
+    const void* p;
+    int64_t sn, sl, sh;
+    int32_t per;
+};
+struct HeadsOut {
+    void* p;
+    int64_t sn, sl, sh;
+    int32_t f32;   // fp32 instead of the storage type
+};
+
+// Element (i, j) of a head's state at i row + j col.
+struct StateAt {
+    int32_t row, col;
+};
+
+struct Pass {
+    HeadsIn q, k, v;
+    HeadsOut y;
+    int32_t kd, vd, blocks;   // channels of q and k, of v and y; blocks of columns
+    const float* s_in;        // [N][H] states (or null: zeros), and the last ones (or null)
+    float* s_out;
+    StateAt at;
+    float in_scale, out_scale;
+    int32_t reverse;
+};
+
+struct Args {
+    Pass pass[3];
+    int32_t first[4];         // workgroups of a segment of each pass, added up
+    int64_t N;
+    int32_t L, H;
+    const float* log_decay;
+    const int32_t* lengths;
+    float scale;
+};
+
+__device__ __forceinline__ int32_t steps_of(const int32_t* lengths, int64_t n, int32_t L) {
+    if (!lengths) return L;
+    const int32_t v = lengths[n];
+    return v < 0 ? 0 : (v > L ? L : v);
+}
+
+// lambda^n from log2(lambda), also where lambda is 0
+__device__ __forceinline__ float power(float log2_decay, int n) {
+    return n == 0 ? 1.0f : __builtin_amdgcn_exp2f(log2_decay * static_cast<float>(n));
+}
+// lambda^n to fp32's last place: the state is multiplied by it once a tile, and its
+// errors would add up.
+__device__ __forceinline__ float exact_power(float log_decay, int n) {
+    return n == 0 ? 1.0f : static_cast<float>(exp(static_cast<double>(log_decay) * n));
+}
+
+// x as the sum of bf16 parts.  What is left of an infinity is made finite, so that
+// infinities stay infinities.
+template <int P, int V> struct Split {
+    typedef __bf16 Run __attribute__((ext_vector_type(V)));
+    Run part[P];
+    __device__ __forceinline__ void of(const float (&x)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float left = x[e];
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                part[p][e] = static_cast<__bf16>(left);
+                if (p + 1 < P) left = __builtin_amdgcn_fmed3f(left - static_cast<float>(part[p][e]), -0x1p120f, 0x1p120f);
+            }
+        }
+    }
+};
+
+// c += a b over the parts whose product is not below the last part's
+template <int PA, int PB, int P>
+__device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[PA], const bf16x8 (&b)[PB], f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+#pragma unroll
+        for (int j = 0; j < PB; ++j)
+            if (i + j < P) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// Rows of a tile in LDS, one plane a part; 16 bytes between rows keep the 16 rows that
+// a fragment reads on different banks.
+template <int PLANES, int ROWS, int WIDTH> struct TileLds {
+    static constexpr int kStride = WIDTH + 8;
+    uint16_t v[PLANES][ROWS][kStride];
+
+    // 8 channels from c of a row, as a matrix instruction takes them of its row (or
+    // column) `row`: lane m + 16 g holds 8 g .. 8 g + 7 of row m
+    __device__ __forceinline__ void across(int row, int c, bf16x8 (&f)[PLANES]) const {
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) f[p] = *reinterpret_cast<const bf16x8*>(&v[p][row][c]);
+    }
+    // 8 rows from `row` of a channel: the lanes of 16 hand in the places of four
+    // channels in each of four rows, and lane m gets the four rows of channel m
+    __device__ __forceinline__ void down(int row, int c, bf16x8 (&f)[PLANES]) const {
+        using At = __attribute__((address_space(3))) s16x4*;
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) {
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row][c]));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row + 4][c]));
+            f[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// A tile's rows on their way from memory: 16 bytes of U rows a thread.
+template <typename Elem, int ROWS, int WIDTH> struct TileLoad {
+    static constexpr int V = Vec<Elem>::V, kRuns = WIDTH / V, kPer = kThreads / kRuns, U = (ROWS + kPer - 1) / kPer;
+    static_assert(kRuns <= kThreads && (ROWS % kPer == 0 || U == 1), "threads cover whole rows");
+    u32x4 raw[U];
+
+    // rows 0 .. live - 1 from p, `stride` apart; channels c0 .. of D; zeros elsewhere
+    __device__ __forceinline__ void load(const Elem* p, int64_t stride, int live, int c0, int D) {
+        const int c = c0 + static_cast<int>(threadIdx.x) % kRuns * V, r0 = threadIdx.x / kRuns;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = r0 + u * kPer;
+            raw[u] = u32x4{0, 0, 0, 0};
+            if (row >= live) continue;
+            const Elem* at = p + row * stride + c;
+            if (c + V <= D) {
+                raw[u] = reinterpret_cast<const Bytes16*>(at)->v;
+            } else if (c < D) {
+                typename Vec<Elem>::Packed e{};
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (c + j < D) e.v[j] = at[j];
+                raw[u] = __builtin_bit_cast(u32x4, e);
+            }
+        }
+    }
+    template <int PLANES> __device__ __forceinline__ void store(TileLds<PLANES, ROWS, WIDTH>& to) const {
+        const int c = static_cast<int>(threadIdx.x) % kRuns * V, r0 = threadIdx.x / kRuns;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = r0 + u * kPer;
+            if (ROWS % kPer != 0 && row >= ROWS) continue;
+            if constexpr (PLANES == 1) {
+                *reinterpret_cast<u32x4*>(&to.v[0][row][c]) = raw[u];
+            } else {
+                float x[V];
+                Vec<Elem>::widen(raw[u], x);
+                Split<PLANES, V> s;
+                s.of(x);
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) *reinterpret_cast<typename Split<PLANES, V>::Run*>(&to.v[p][row][c]) = s.part[p];
+            }
+        }
+    }
+    __device__ __forceinline__ bool finite() const {
+        bool all = true;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[V];
+            Vec<Elem>::widen(raw[u], x);
+#pragma unroll
+            for (int e = 0; e < V; ++e) all &= fabsf(x[e]) < __builtin_inff();
+        }
+        return all;
+    }
+};
+
+// Where a pass's workgroup stands.
+struct Place {
+    int32_t pass, block, h;
+    int64_t n;
+};
+
+template <typename Elem> __device__ __forceinline__ const Elem* heads_at(const HeadsIn& t, int64_t n, int32_t h) {
+    return static_cast<const Elem*>(t.p) + n * t.sn + h / t.per * t.sh;
+}
+
+template <typename Elem, int KD, int CB> struct Shape {
+    static constexpr int T = kTile<Elem>, PI = kParts<Elem>, PS = kSums<Elem>;
+    static constexpr int VB = 64 * CB;          // columns of a workgroup
+    struct Lds {
+        TileLds<PI, T, KD> q, k;
+        TileLds<PI, T, VB> v;
+        TileLds<PS, T, T> p;
+        int32_t odd;                            // v holds an infinity or NaN
+    };
+};
+
+// A pass.  A wave's accumulators of the state: S[b][c], lane m + 16 g, register r holds
+// the state at (32 (b / 2) + 8 g + 4 (b % 2) + r, column(c, m)), so that those of two
+// blocks side by side are the 8 consecutive rows that a lane hands a matrix
+// instruction, without a move.  Outputs come transposed, O[i][c] with row 16 i + m and
+// columns column(c, 4 g + r): four or eight side by side.
+template <typename Elem, int KD, int CB>
+__global__ __launch_bounds__(kThreads) void attention_kernel(Args a) {
+    using Sh = Shape<Elem, KD, CB>;
+    constexpr int T = Sh::T, PI = Sh::PI, PS = Sh::PS, VB = Sh::VB, IB = T / 16, JS = T / 32, KS = KD / 32;
+    __shared__ __align__(16) typename Sh::Lds lds;
+    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, m = lane % 16, g = lane / 16;
+
+    int32_t which = 0;
+    const uint32_t id = blockIdx.x;
+    while (id >= static_cast<uint32_t>(a.first[which + 1])) ++which;
+    const Pass& pass = a.pass[which];
+    const uint32_t unit = id - a.first[which];
+    const int32_t block = unit % pass.blocks;
+    const int32_t h = unit / pass.blocks % a.H;
+    const int64_t n = unit / pass.blocks / a.H;
+    const int32_t steps = steps_of(a.lengths, n, a.L), kd = pass.kd, vd = pass.vd, v0 = block * VB;
+    const bool reverse = pass.reverse != 0;
+    const float log_decay = a.log_decay[h], log2_decay = log_decay * kLog2e;
+
+    auto column = [&](int c, int i) { return CB == 1 ? 16 * wave + i : 32 * wave + 8 * (i / 4) + 4 * c + i % 4; };
+    // channels that a lane hands to a transposing read, of the state's rows and columns
+    auto row_chunk = [&](int b) { return 32 * (b / 2) + 8 * (m % 4) + 4 * (b % 2); };
+    auto column_chunk = [&](int c) { return column(c, 4 * (m % 4)); };
+
+    f32x4 S[KD / 16][CB];
+    const int64_t state = (n * a.H + h) * static_cast<int64_t>(kd) * vd;
+#pragma unroll
+    for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + column(c, m);
+                S[b][c][r] = pass.s_in && i < kd && j < vd ? pass.s_in[state + i * pass.at.row + j * pass.at.col] : 0.0f;
+            }
+
+    const Elem* q = heads_at<Elem>(pass.q, n, h);
+    const Elem* k = heads_at<Elem>(pass.k, n, h);
+    const Elem* v = heads_at<Elem>(pass.v, n, h);
+    TileLoad<Elem, T, KD> lq, lk;
+    TileLoad<Elem, T, VB> lv;
+    const int32_t tiles = (steps + T - 1) / T;
+    auto first_of = [&](int32_t t) { return (reverse ? tiles - 1 - t : t) * T; };
+    auto load = [&](int32_t t) {
+        const int32_t t0 = first_of(t), live = min(T, steps - t0);
+        lq.load(q + t0 * pass.q.sl, pass.q.sl, live, 0, kd);
+        lk.load(k + t0 * pass.k.sl, pass.k.sl, live, 0, kd);
+        lv.load(v + t0 * pass.v.sl, pass.v.sl, live, v0, vd);
+    };
+    // weights above the diagonal are zeros that nothing writes
+    for (int i = tid; i < static_cast<int>(sizeof(lds.p) / 4); i += kThreads) reinterpret_cast<uint32_t*>(&lds.p)[i] = 0;
+    if (tid == 0) lds.odd = 0;
+    if (tiles > 0) load(0);
+    __syncthreads();
+
+    for (int32_t t = 0; t < tiles; ++t) {
+        const int32_t t0 = first_of(t), live = min(T, steps - t0);
+        lq.template store<PI>(lds.q);
+        lk.template store<PI>(lds.k);
+        lv.template store<PI>(lds.v);
+        if (!lv.finite()) lds.odd = t + 1;
+        if (t + 1 < tiles) load(t + 1);
+        __syncthreads();
+
+        // the weights of the tile, in blocks of 16 x 16 of the triangle
+        for (int blk = wave; blk < IB * (IB + 1) / 2; blk += kWaves) {
+            const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
+            const int ib = reverse ? near : far, jb = reverse ? far : near;
+            f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                bf16x8 fk[PI], fq[PI];
+                lds.k.across(16 * jb + m, 32 * s + 8 * g, fk);
+                lds.q.across(16 * ib + m, 32 * s + 8 * g, fq);
+                w = multiply<PI, PI, PS>(fk, fq, w);
+            }
+            float x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * ib + m, j = 16 * jb + 4 * g + r, d = reverse ? j - i : i - j;
+                x[r] = d < 0 ? 0.0f : w[r] * (a.scale * power(log2_decay, d));
+            }
+            Split<PS, 4> parts;
+            parts.of(x);
+#pragma unroll
+            for (int p = 0; p < PS; ++p) *reinterpret_cast<bf16x4*>(&lds.p.v[p][16 * ib + m][16 * jb + 4 * g]) = parts.part[p];
+        }
+
+        // what the state gives
+        f32x4 O[IB][CB];
+#pragma unroll
+        for (int i = 0; i < IB; ++i)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) O[i][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            Split<PS, 8> fs[CB];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][c][e % 4];
+                fs[c].of(x);
+            }
+#pragma unroll
+            for (int i = 0; i < IB; ++i) {
+                bf16x8 fq[PI];
+                lds.q.across(16 * i + m, 32 * s + 8 * g, fq);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) O[i][c] = multiply<PS, PI, PS>(fs[c].part, fq, O[i][c]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < IB; ++i) {
+            const int row = 16 * i + m;
+            const float f = pass.out_scale * power(log2_decay, reverse ? max(0, live - 1 - row) : row + 1);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) O[i][c] *= f;
+        }
+
+        // the state behind the tile
+        const float whole = exact_power(log_decay, live);
+#pragma unroll
+        for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) S[b][c] *= whole;
+        bf16x8 fv[JS][CB][PI];
+#pragma unroll
+        for (int s = 0; s < JS; ++s) {
+            Split<PS, 8> late[CB];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                lds.v.down(32 * s + 8 * g + m / 4, column_chunk(c), fv[s][c]);
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int j = 32 * s + 8 * g + e;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int p = PI - 1; p >= 0; --p) sum += static_cast<float>(fv[s][c][p][e]);
+                    x[e] = sum * (pass.in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j)));
+                }
+                late[c].of(x);
+            }
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b) {
+                bf16x8 fk[PI];
+                lds.k.down(32 * s + 8 * g + m / 4, row_chunk(b), fk);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) S[b][c] = multiply<PI, PS, PS>(fk, late[c].part, S[b][c]);
+            }
+        }
+        __syncthreads();
+
+        // what the tile's own steps give
+        if (lds.odd != t + 1) {
+#pragma unroll
+            for (int i = 0; i < IB; ++i)
+#pragma unroll
+                for (int s = 0; s < JS; ++s) {
+                    if (reverse ? 32 * s + 31 < 16 * i : 32 * s > 16 * i + 15) continue;
+                    bf16x8 fp[PS];
+                    lds.p.across(16 * i + m, 32 * s + 8 * g, fp);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) O[i][c] = multiply<PI, PS, PS>(fv[s][c], fp, O[i][c]);
+                }
+        } else {
+            // step by step: a weight of zero would not remove an infinity or NaN of a later v
+#pragma unroll
+            for (int i = 0; i < IB; ++i) {
+                const int row = 16 * i + m;
+                for (int j = reverse ? row : 0; j < (reverse ? T : row + 1); ++j) {
+                    float w = 0.0f;
+#pragma unroll
+                    for (int p = PS - 1; p >= 0; --p) w += __uint_as_float(static_cast<uint32_t>(lds.p.v[p][row][j]) << 16);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float x = 0.0f;
+#pragma unroll
+                            for (int p = PI - 1; p >= 0; --p)
+                                x += __uint_as_float(static_cast<uint32_t>(lds.v.v[p][j][column(c, 4 * g + r)]) << 16);
+                            O[i][c][r] += w * x;
+                        }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < IB; ++i) {
+            const int row = 16 * i + m, j = v0 + column(0, 4 * g);
+            if (row >= live || j >= vd) continue;
+            const int64_t at = n * pass.y.sn + (t0 + row) * pass.y.sl + h * pass.y.sh + j;
+            if (pass.y.f32) {
+                float* y = static_cast<float*>(pass.y.p) + at;
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (j + 4 * c + r < vd) y[4 * c + r] = O[i][c][r];
+            } else {
+                Elem* y = static_cast<Elem*>(pass.y.p) + at;
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (j + 4 * c + r < vd) y[4 * c + r] = Storage<Elem>::from_f32(O[i][c][r]);
+            }
+        }
+        __syncthreads();
+    }
+
+    // padding
+    const int width = min(VB, vd - v0);
+    for (int64_t i = tid; i < static_cast<int64_t>(a.L - steps) * width; i += kThreads) {
+        const int64_t row = steps + i / width;
+        const int64_t at = n * pass.y.sn + row * pass.y.sl + h * pass.y.sh + v0 + i % width;
+        if (pass.y.f32) static_cast<float*>(pass.y.p)[at] = 0.0f;
+        else static_cast<Elem*>(pass.y.p)[at] = Storage<Elem>::from_f32(0.0f);
+    }
+    if (!pass.s_out) return;
+#pragma unroll
+    for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + column(c, m);
+                if (i < kd && j < vd) pass.s_out[state + i * pass.at.row + j * pass.at.col] = S[b][c][r];
+            }
+}
+
+// Gradients of an input that heads share: the sum over them of their parts
+// [N][L][H][D] in fp32, in the order of the heads.
+template <typename Elem>
+__global__ __launch_bounds__(kThreads) void shared_kernel(const float* part, HeadsOut to, int64_t rows, int32_t L, int32_t heads,
+                                                          int32_t per, int32_t D) {
+    const int64_t all = rows * heads * D, stride = static_cast<int64_t>(gridDim.x) * kThreads;
+    for (int64_t id = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; id < all; id += stride) {
+        const int64_t row = id / (heads * static_cast<int64_t>(D));
+        const int32_t h = id / D % heads, d = id % D;
+        const float* p = part + (row * heads + h) * per * D + d;
+        float sum = 0.0f;
+        for (int32_t u = 0; u < per; ++u) sum += p[static_cast<int64_t>(u) * D];
+        static_cast<Elem*>(to.p)[row / L * to.sn + row % L * to.sl + h * to.sh + d] = Storage<Elem>::from_f32(sum);
+    }
+}
+
+struct StepArgs {
+    HeadsIn q, k, v;
+    HeadsOut y;
+    int64_t N;
+    int32_t H, kd, vd, blocks;
+    const float* log_decay;
+    const float* s;
+    float* s_new;
+    float scale;
+};
+
+// One step: a workgroup takes 64 columns of a head's state, a thread 4 of them in every
+// 16th row.  Bound by the states' memory.
+constexpr int kStepColumns = 64, kStepRows = kThreads / (kStepColumns / 4);
+template <typename Elem>
+__global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a) {
+    using St = Storage<Elem>;
+    __shared__ float lds[kStepRows][kStepColumns + 4];
+    const int64_t units = a.N * a.H * a.blocks;
+    const int c = threadIdx.x % (kStepColumns / 4) * 4, r0 = threadIdx.x / (kStepColumns / 4);
+    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const int32_t j = static_cast<int32_t>(unit % a.blocks) * kStepColumns + c, h = unit / a.blocks % a.H;
+        const int64_t n = unit / a.blocks / a.H;
+        const Elem* q = heads_at<Elem>(a.q, n, h);
+        const Elem* k = heads_at<Elem>(a.k, n, h);
+        const Elem* v = heads_at<Elem>(a.v, n, h);
+        const float keep = exact_power(a.log_decay[h], 1);
+        const int valid = min(4, a.vd - j);
+        float x[4], sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = e < valid ? St::to_f32(v[j + e]) : 0.0f;
+        const int64_t at = ((n * a.H + h) * a.kd) * static_cast<int64_t>(a.vd) + j;
+        for (int i = r0; i < a.kd; i += kStepRows) {
+            const float ki = St::to_f32(k[i]), qi = St::to_f32(q[i]);
+            const float* s = a.s + at + static_cast<int64_t>(i) * a.vd;
+            float* s_new = a.s_new + at + static_cast<int64_t>(i) * a.vd;
+            if (valid == 4) {
+                f32x4 w = __builtin_bit_cast(f32x4, reinterpret_cast<const Bytes16*>(s)->v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = fmaf(keep, w[e], ki * x[e]);
+                    sum[e] = fmaf(qi, w[e], sum[e]);
+                }
+                reinterpret_cast<Bytes16*>(s_new)->v = __builtin_bit_cast(u32x4, w);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (e >= valid) continue;
+                    const float w = fmaf(keep, s[e], ki * x[e]);
+                    sum[e] = fmaf(qi, w, sum[e]);
+                    s_new[e] = w;
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds[r0][c + e] = sum[e];
+        __syncthreads();
+        const int column = threadIdx.x, jj = j - c + column;
+        if (column < kStepColumns && jj < a.vd) {
+            float y = 0.0f;
+#pragma unroll
+            for (int r = 0; r < kStepRows; ++r) y += lds[r][column];
+            static_cast<Elem*>(a.y.p)[n * a.y.sn + h * a.y.sh + jj] = St::from_f32(a.scale * y);
+        }
+        __syncthreads();
+    }
+}
+
+HeadsIn heads_in(const wg_heads& t, int64_t heads, int64_t H) {
+    return {t.data, t.stride_n, t.stride_l, t.stride_h, static_cast<int32_t>(H / heads)};
+}
+HeadsOut heads_out(const wg_heads& t) { return {const_cast<void*>(t.data), t.stride_n, t.stride_l, t.stride_h, 0}; }
+
+// launch(args with first set, workgroups).  HIP takes fewer than 2^32 threads: more
+// sequences than that go in several launches.
+hipError_t over_sequences(const Args& a, int passes, int dtype, void (*kernel)(Args), hipStream_t stream) {
+    int64_t per = 0;   // workgroups of a sequence
+    for (int p = 0; p < passes; ++p) per += static_cast<int64_t>(a.H) * a.pass[p].blocks;
+    const int64_t most = std::max<int64_t>(1, 0xffffff / per);
+    for (int64_t n0 = 0; n0 < a.N; n0 += most) {
+        Args k = a;
+        k.N = std::min(a.N - n0, most);
+        if (a.lengths) k.lengths = a.lengths + n0;
+        auto from = [&](auto& t, int es) { t.p = const_cast<char*>(static_cast<const char*>(t.p)) + n0 * t.sn * es; };
+        k.first[0] = 0;
+        for (int p = 0; p < passes; ++p) {
+            Pass& s = k.pass[p];
+            for (HeadsIn* t : {&s.q, &s.k, &s.v}) from(*t, dtype_bytes(dtype));
+            from(s.y, s.y.f32 ? 4 : dtype_bytes(dtype));
+            const int64_t states = n0 * a.H * s.kd * s.vd;
+            if (s.s_in) s.s_in += states;
+            if (s.s_out) s.s_out += states;
+            k.first[p + 1] = k.first[p] + static_cast<int32_t>(k.N * a.H * s.blocks);
+        }
+        for (int p = passes; p < 3; ++p) k.first[p + 1] = k.first[p];
+        kernel<<<static_cast<unsigned>(k.first[passes]), kThreads, 0, stream>>>(k);
+    }
+    return hipGetLastError();
+}
+
+#define WG_ATTENTION_SHAPES(X) X(32, 1) X(32, 2) X(64, 1) X(64, 2) X(128, 1) X(128, 2) X(256, 1)
+
+template <typename Elem> hipError_t run_passes(Args& a, int passes, int dtype, hipStream_t stream) {
+    int kd = 0, vd = 0;
+    for (int p = 0; p < passes; ++p) kd = std::max(kd, a.pass[p].kd), vd = std::max(vd, a.pass[p].vd);
+    const int KD = kd <= 32 ? 32 : kd <= 64 ? 64 : kd <= 128 ? 128 : 256, CB = vd <= 64 || KD == 256 ? 1 : 2;
+    for (int p = 0; p < passes; ++p) a.pass[p].blocks = (a.pass[p].vd + 64 * CB - 1) / (64 * CB);
+#define WG_ATTENTION_CASE(K, C) \
+    if (KD == K && CB == C) return over_sequences(a, passes, dtype, attention_kernel<Elem, K, C>, stream);
+    WG_ATTENTION_SHAPES(WG_ATTENTION_CASE)
+#undef WG_ATTENTION_CASE
+    return hipErrorInvalidValue;
+}
+
+// Bytes of the parts that an input's gradient is summed from: none where no heads share it.
+size_t part_bytes(int64_t N, int64_t L, int64_t heads, int64_t H, int64_t D) {
+    return heads == H ? 0 : static_cast<size_t>((N * L * H * D * 4 + 15) / 16 * 16);
+}
+
+}  // namespace
+
+#if WG_DTYPE == 0
+size_t linear_attention_workspace(int, int64_t N, int64_t L, int64_t q_heads, int64_t k_heads, int64_t v_heads, int64_t H,
+                                  int64_t Dk, int64_t Dv, bool backward) {
+    if (!backward) return 0;
+    return part_bytes(N, L, q_heads, H, Dk) + part_bytes(N, L, k_heads, H, Dk) + part_bytes(N, L, v_heads, H, Dv);
+}
+#endif
+
+template <int D> hipError_t launch_linear_attention_t(const wg_linear_attention& a, hipStream_t stream) {
+    using Elem = typename DTypeOf<D>::type;
+    const int32_t Dk = static_cast<int32_t>(a.Dk), Dv = static_cast<int32_t>(a.Dv);
+    Args k{};
+    k.N = a.N, k.L = static_cast<int32_t>(a.L), k.H = static_cast<int32_t>(a.heads);
+    k.log_decay = a.log_decay, k.lengths = a.lengths, k.scale = static_cast<float>(a.scale);
+    k.pass[0] = Pass{heads_in(a.q, a.q_heads, a.heads), heads_in(a.k, a.k_heads, a.heads), heads_in(a.v, a.v_heads, a.heads),
+                     heads_out(a.y), Dk, Dv, 0, a.s0, a.s_last, {Dv, 1}, 1.0f, k.scale, 0};
+    return run_passes<Elem>(k, 1, D, stream);
+}
+
+template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_attention_backward& a, hipStream_t stream) {
+    using Elem = typename DTypeOf<D>::type;
+    const int64_t H = a.heads;
+    const int32_t Dk = static_cast<int32_t>(a.Dk), Dv = static_cast<int32_t>(a.Dv);
+    Args k{};
+    k.N = a.N, k.L = static_cast<int32_t>(a.L), k.H = static_cast<int32_t>(H);
+    k.log_decay = a.log_decay, k.lengths = a.lengths, k.scale = static_cast<float>(a.scale);
+    const HeadsIn q = heads_in(a.q, a.q_heads, H), kk = heads_in(a.k, a.k_heads, H), v = heads_in(a.v, a.v_heads, H),
+                  dy = heads_in(a.dy, H, H);
+    char* ws = static_cast<char*>(a.workspace);
+    HeadsOut out[3] = {heads_out(a.dq), heads_out(a.dk), heads_out(a.dv)};
+    const int64_t heads[3] = {a.q_heads, a.k_heads, a.v_heads};
+    const int32_t dims[3] = {Dk, Dk, Dv};
+    const float* parts[3] = {};
+    for (int p = 0; p < 3; ++p) {
+        if (heads[p] == H) continue;
+        parts[p] = reinterpret_cast<const float*>(ws);
+        ws += part_bytes(a.N, a.L, heads[p], H, dims[p]);
+    }
+    auto to = [&](int p) {
+        if (!parts[p]) return out[p];
+        return HeadsOut{const_cast<float*>(parts[p]), a.L * H * dims[p], H * dims[p], dims[p], 1};
+    };
+    k.pass[0] = Pass{dy, v, kk, to(0), Dv, Dk, 0, a.s0, nullptr, {1, Dv}, 1.0f, k.scale, 0};
+    k.pass[1] = Pass{v, dy, q, to(1), Dv, Dk, 0, a.ds_last, nullptr, {1, Dv}, k.scale, 1.0f, 1};
+    k.pass[2] = Pass{kk, q, dy, to(2), Dk, Dv, 0, a.ds_last, a.ds0, {Dv, 1}, k.scale, 1.0f, 1};
+    if (const hipError_t e = run_passes<Elem>(k, 3, D, stream)) return e;
+    for (int p = 0; p < 3; ++p) {
+        const int64_t all = a.N * a.L * heads[p] * dims[p];
+        if (!parts[p] || all == 0) continue;
+        const int64_t blocks = std::min<int64_t>((all + kThreads - 1) / kThreads, 0xffffffffLL / kThreads);
+        shared_kernel<Elem><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(
+            parts[p], out[p], a.N * a.L, k.L, static_cast<int32_t>(heads[p]), static_cast<int32_t>(H / heads[p]), dims[p]);
+    }
+    return hipGetLastError();
+}
+
+template <int D> hipError_t launch_linear_attention_step_t(const wg_linear_attention_step& a, hipStream_t stream) {
+    using Elem = typename DTypeOf<D>::type;
+    const int32_t blocks = static_cast<int32_t>((a.Dv + kStepColumns - 1) / kStepColumns);
+    const StepArgs k{heads_in(a.q, a.q_heads, a.heads), heads_in(a.k, a.k_heads, a.heads), heads_in(a.v, a.v_heads, a.heads),
+                     heads_out(a.y), a.N, static_cast<int32_t>(a.heads), static_cast<int32_t>(a.Dk), static_cast<int32_t>(a.Dv),
+                     blocks, a.log_decay, a.s, a.s_new, static_cast<float>(a.scale)};
+    const int64_t grid = std::min<int64_t>(a.N * a.heads * blocks, 0xffffffffLL / kThreads);
+    step_kernel<Elem><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(k);
+    return hipGetLastError();
+}
+
+#define WG_ATTENTION_INSTANCES(D)                                                                    \
+    template hipError_t launch_linear_attention_t<D>(const wg_linear_attention&, hipStream_t);       \
+    template hipError_t launch_linear_attention_backward_t<D>(const wg_linear_attention_backward&, hipStream_t); \
+    template hipError_t launch_linear_attention_step_t<D>(const wg_linear_attention_step&, hipStream_t);
+WG_ATTENTION_INSTANCES(WG_DTYPE)
+#undef WG_ATTENTION_INSTANCES
+
+}  // namespace wg

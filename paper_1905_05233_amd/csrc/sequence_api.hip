@@ -4,6 +4,7 @@
 // is launched.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <exception>
@@ -23,6 +24,8 @@ namespace {
 constexpr int64_t kMaxSize = int64_t(1) << 31;      // sizes are below this
 constexpr int64_t kMaxElements = int64_t(1) << 40;  // and the rows of one tensor together hold at most this
 constexpr int64_t kMaxReach = int64_t(1) << 58;     // elements between a tensor's first and last row
+
+#define WG_TRY(e) do { const wg_status s_ = (e); if (s_ != WG_OK) return s_; } while (0)
 
 template <typename F>
 wg_status guarded(F&& f) noexcept {
@@ -91,6 +94,72 @@ wg_status check_workspace(const void* ws, int64_t bytes, size_t need) {
     return WG_OK;
 }
 
+constexpr int64_t kMaxHeads = 65536, kMaxChannels = 256;
+
+// Heads [N][L][H][D] of elements of es bytes; `written`: they must not overlap.
+wg_status check_heads(const wg_heads& t, const char* name, int64_t N, int64_t L, int64_t H, int64_t D, int64_t es,
+                      bool written) {
+    if (N == 0 || L == 0) return WG_OK;   // nothing is touched
+    if (!t.data) return fail(WG_ERR_ARG, std::string("null tensor ") + name);
+    if (!aligned(t.data, static_cast<uintptr_t>(es)))
+        return fail(WG_ERR_ARG, std::string(name) + " is not aligned to its elements");
+    if (t.stride_n < 0 || t.stride_l < 0 || t.stride_h < 0 || t.stride_n > kMaxReach / N || t.stride_l > kMaxReach / L ||
+        t.stride_h > kMaxReach / H)
+        return fail(WG_ERR_ARG, std::string(name) + ": strides out of range");
+    if (!written) return WG_OK;
+    // the strides in ascending order: each spaces what the smaller ones reach
+    std::pair<int64_t, int64_t> dims[3] = {{t.stride_h, H}, {t.stride_l, L}, {t.stride_n, N}};
+    std::sort(dims, dims + 3);
+    int64_t reach = D;
+    for (const auto& [stride, count] : dims) {
+        if (count == 1) continue;
+        if (stride < reach) return fail(WG_ERR_ARG, std::string("rows of ") + name + " overlap");
+        reach += (count - 1) * stride;
+    }
+    return WG_OK;
+}
+
+// The sizes of a linear attention, of which wg_linear_attention and its kin begin with.
+template <typename A> wg_status check_attention(const A& a, int64_t N, int64_t L) {
+    if (!storage(a.dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
+    if (a.heads < 1 || a.heads > kMaxHeads) return fail(WG_ERR_ARG, "heads must be in [1, 65536]");
+    for (const int64_t h : {a.q_heads, a.k_heads, a.v_heads})
+        if (h < 1 || a.heads % h != 0) return fail(WG_ERR_ARG, "q_heads, k_heads and v_heads must divide heads");
+    if (a.Dk < 1 || a.Dv < 1) return fail(WG_ERR_ARG, "Dk and Dv must be positive");
+    if (a.Dk > kMaxChannels || a.Dv > kMaxChannels) return fail(WG_ERR_UNSUPPORTED, "heads of more than 256 channels");
+    const int64_t D = a.Dk > a.Dv ? a.Dk : a.Dv;
+    WG_TRY(check_sizes(N, L, a.heads * D, 0, 0));
+    WG_TRY(check_sizes(N, a.Dk, a.heads * a.Dv, 0, 0));
+    return check_steps(L, a.heads * D);
+}
+wg_status check_scale(double scale) {
+    return std::isfinite(static_cast<float>(scale)) ? WG_OK : fail(WG_ERR_ARG, "scale must be finite in fp32");
+}
+template <typename A> size_t attention_workspace(const A& a, bool backward) {
+    return wg::linear_attention_workspace(static_cast<int>(a.dtype), a.N, a.L, a.q_heads, a.k_heads, a.v_heads, a.heads, a.Dk,
+                                          a.Dv, backward);
+}
+
+template <typename A> wg_status check_rotation(const A& a) {
+    if (!storage(a.dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
+    if (a.q_heads < 1 || a.k_heads < 1 || a.q_heads > kMaxHeads || a.k_heads > kMaxHeads - a.q_heads)
+        return fail(WG_ERR_ARG, "q_heads and k_heads must be positive, and 65536 together at most");
+    if (a.D > kMaxChannels) return fail(WG_ERR_UNSUPPORTED, "heads of more than 256 channels");
+    if (a.R < 2 || a.R > a.D || a.R % 2 != 0) return fail(WG_ERR_ARG, "R must be even and in [2, D]");
+    WG_TRY(check_sizes(a.N, a.L, (a.q_heads + a.k_heads) * a.D, 0, 0));
+    if (a.start < -kMaxSize || a.start >= kMaxSize) return fail(WG_ERR_ARG, "start must be in [-2^31, 2^31)");
+    if (!std::isfinite(static_cast<float>(a.eps)) || a.eps < 0)
+        return fail(WG_ERR_ARG, "eps must be finite in fp32 and not negative");
+    return WG_OK;
+}
+template <typename A> wg_status check_rotation_pointers(const A& a) {
+    const uintptr_t es = static_cast<uintptr_t>(wg::dtype_bytes(static_cast<int>(a.dtype)));
+    if (!a.q_weight || !a.k_weight || !aligned(a.q_weight, es) || !aligned(a.k_weight, es))
+        return fail(WG_ERR_ARG, "q_weight or k_weight is null or not aligned to its elements");
+    if (!a.turns || !aligned(a.turns, 8)) return fail(WG_ERR_ARG, "turns is null or not 8-byte aligned");
+    return check_f32(a.positions, "positions");
+}
+
 wg_status check_w4(const wg_w4& w) {
     if (!w.codes || !w.scales) return fail(WG_ERR_ARG, "null codes or scales");
     if (!aligned(w.codes, 16) || !aligned(w.scales, 16)) return fail(WG_ERR_ARG, "codes and scales must be 16-byte aligned");
@@ -102,7 +171,6 @@ wg_status check_w4(const wg_w4& w) {
     return WG_OK;
 }
 
-#define WG_TRY(e) do { const wg_status s_ = (e); if (s_ != WG_OK) return s_; } while (0)
 #define WG_BY_DTYPE(dtype, call)                                      \
     ((dtype) == WG_F32 ? call<0> : (dtype) == WG_F16 ? call<1> : call<2>)
 
@@ -295,6 +363,128 @@ wg_status winograd_dequantize_w4(const wg_w4* w, wg_dtype dtype, void* m, int64_
         if (!storage(dtype)) return fail(WG_ERR_UNSUPPORTED, "unknown dtype");
         WG_TRY(check_rows(wg_rows{m, 0, ldm}, "m", 1, w->rows, w->cols, wg::dtype_bytes(dtype), true));
         return from_hip(WG_BY_DTYPE(dtype, wg::launch_dequantize_w4_t)(*w, m, ldm, stream), "4-bit weights");
+    });
+}
+
+wg_status winograd_linear_attention_workspace(const wg_linear_attention* a, int backward, size_t* bytes) {
+    return guarded([&]() -> wg_status {
+        if (!a || !bytes) return fail(WG_ERR_ARG, "null argument");
+        WG_TRY(check_attention(*a, a->N, a->L));
+        *bytes = attention_workspace(*a, backward != 0);
+        return WG_OK;
+    });
+}
+
+wg_status winograd_linear_attention(const wg_linear_attention* a, hipStream_t stream) {
+    return guarded([&]() -> wg_status {
+        if (!a) return fail(WG_ERR_ARG, "null argument");
+        const int64_t N = a->N, L = a->L;
+        WG_TRY(check_attention(*a, N, L));
+        WG_TRY(check_scale(a->scale));
+        if (N == 0) return WG_OK;
+        const int64_t es = wg::dtype_bytes(static_cast<int>(a->dtype));
+        WG_TRY(check_heads(a->q, "q", N, L, a->q_heads, a->Dk, es, false));
+        WG_TRY(check_heads(a->k, "k", N, L, a->k_heads, a->Dk, es, false));
+        WG_TRY(check_heads(a->v, "v", N, L, a->v_heads, a->Dv, es, false));
+        WG_TRY(check_heads(a->y, "y", N, L, a->heads, a->Dv, es, true));
+        WG_TRY(check_f32(a->log_decay, "log_decay", false));
+        WG_TRY(check_f32(a->s0, "s0"));
+        WG_TRY(check_f32(a->lengths, "lengths"));
+        WG_TRY(check_f32(a->s_last, "s_last"));
+        WG_TRY(check_workspace(a->workspace, a->workspace_bytes, attention_workspace(*a, false)));
+        return from_hip(WG_BY_DTYPE(a->dtype, wg::launch_linear_attention_t)(*a, stream), "linear attention");
+    });
+}
+
+wg_status winograd_linear_attention_backward(const wg_linear_attention_backward* a, hipStream_t stream) {
+    return guarded([&]() -> wg_status {
+        if (!a) return fail(WG_ERR_ARG, "null argument");
+        const int64_t N = a->N, L = a->L;
+        WG_TRY(check_attention(*a, N, L));
+        WG_TRY(check_scale(a->scale));
+        if (N == 0) return WG_OK;
+        const int64_t es = wg::dtype_bytes(static_cast<int>(a->dtype));
+        WG_TRY(check_heads(a->dy, "dy", N, L, a->heads, a->Dv, es, false));
+        WG_TRY(check_heads(a->q, "q", N, L, a->q_heads, a->Dk, es, false));
+        WG_TRY(check_heads(a->k, "k", N, L, a->k_heads, a->Dk, es, false));
+        WG_TRY(check_heads(a->v, "v", N, L, a->v_heads, a->Dv, es, false));
+        WG_TRY(check_heads(a->dq, "dq", N, L, a->q_heads, a->Dk, es, true));
+        WG_TRY(check_heads(a->dk, "dk", N, L, a->k_heads, a->Dk, es, true));
+        WG_TRY(check_heads(a->dv, "dv", N, L, a->v_heads, a->Dv, es, true));
+        WG_TRY(check_f32(a->log_decay, "log_decay", false));
+        WG_TRY(check_f32(a->s0, "s0"));
+        WG_TRY(check_f32(a->ds_last, "ds_last"));
+        WG_TRY(check_f32(a->lengths, "lengths"));
+        WG_TRY(check_f32(a->ds0, "ds0"));
+        WG_TRY(check_workspace(a->workspace, a->workspace_bytes, attention_workspace(*a, true)));
+        return from_hip(WG_BY_DTYPE(a->dtype, wg::launch_linear_attention_backward_t)(*a, stream), "linear attention's gradients");
+    });
+}
+
+wg_status winograd_linear_attention_step(const wg_linear_attention_step* a, hipStream_t stream) {
+    return guarded([&]() -> wg_status {
+        if (!a) return fail(WG_ERR_ARG, "null argument");
+        const int64_t N = a->N;
+        WG_TRY(check_attention(*a, N, 1));
+        WG_TRY(check_scale(a->scale));
+        if (N == 0) return WG_OK;
+        const int64_t es = wg::dtype_bytes(static_cast<int>(a->dtype));
+        WG_TRY(check_heads(a->q, "q", N, 1, a->q_heads, a->Dk, es, false));
+        WG_TRY(check_heads(a->k, "k", N, 1, a->k_heads, a->Dk, es, false));
+        WG_TRY(check_heads(a->v, "v", N, 1, a->v_heads, a->Dv, es, false));
+        WG_TRY(check_heads(a->y, "y", N, 1, a->heads, a->Dv, es, true));
+        WG_TRY(check_f32(a->log_decay, "log_decay", false));
+        WG_TRY(check_f32(a->s, "s", false));
+        WG_TRY(check_f32(a->s_new, "s_new", false));
+        return from_hip(WG_BY_DTYPE(a->dtype, wg::launch_linear_attention_step_t)(*a, stream), "linear attention's step");
+    });
+}
+
+wg_status winograd_head_norm_rotate(const wg_head_norm_rotate* a, hipStream_t stream) {
+    return guarded([&]() -> wg_status {
+        if (!a) return fail(WG_ERR_ARG, "null argument");
+        WG_TRY(check_rotation(*a));
+        const int64_t N = a->N, L = a->L, es = wg::dtype_bytes(static_cast<int>(a->dtype));
+        if (N == 0 || L == 0) return WG_OK;
+        WG_TRY(check_heads(a->q, "q", N, L, a->q_heads, a->D, es, false));
+        WG_TRY(check_heads(a->k, "k", N, L, a->k_heads, a->D, es, false));
+        WG_TRY(check_heads(a->q_out, "q_out", N, L, a->q_heads, a->D, es, true));
+        WG_TRY(check_heads(a->k_out, "k_out", N, L, a->k_heads, a->D, es, true));
+        WG_TRY(check_rotation_pointers(*a));
+        return from_hip(WG_BY_DTYPE(a->dtype, wg::launch_head_norm_rotate_t)(*a, stream), "norm of heads");
+    });
+}
+
+wg_status winograd_head_norm_rotate_workspace(wg_dtype dtype, int64_t N, int64_t L, int64_t heads, int64_t D, int64_t R,
+                                              int adjacent, size_t* bytes) {
+    return guarded([&]() -> wg_status {
+        if (!bytes) return fail(WG_ERR_ARG, "null argument");
+        wg_head_norm_rotate a{};
+        a.dtype = dtype, a.N = N, a.L = L, a.q_heads = heads - 1, a.k_heads = 1, a.D = D, a.R = R;
+        WG_TRY(check_rotation(a));
+        *bytes = wg::head_norm_rotate_workspace(dtype, N, L, heads, D, R, adjacent != 0);
+        return WG_OK;
+    });
+}
+
+wg_status winograd_head_norm_rotate_backward(const wg_head_norm_rotate_backward* a, hipStream_t stream) {
+    return guarded([&]() -> wg_status {
+        if (!a) return fail(WG_ERR_ARG, "null argument");
+        WG_TRY(check_rotation(*a));
+        const int64_t N = a->N, L = a->L, es = wg::dtype_bytes(static_cast<int>(a->dtype));
+        WG_TRY(check_heads(a->dq_out, "dq_out", N, L, a->q_heads, a->D, es, false));
+        WG_TRY(check_heads(a->dk_out, "dk_out", N, L, a->k_heads, a->D, es, false));
+        WG_TRY(check_heads(a->q, "q", N, L, a->q_heads, a->D, es, false));
+        WG_TRY(check_heads(a->k, "k", N, L, a->k_heads, a->D, es, false));
+        WG_TRY(check_heads(a->dq, "dq", N, L, a->q_heads, a->D, es, true));
+        WG_TRY(check_heads(a->dk, "dk", N, L, a->k_heads, a->D, es, true));
+        WG_TRY(check_rotation_pointers(*a));
+        WG_TRY(check_f32(a->dq_weight, "dq_weight", false));
+        WG_TRY(check_f32(a->dk_weight, "dk_weight", false));
+        WG_TRY(check_workspace(a->workspace, a->workspace_bytes,
+                               wg::head_norm_rotate_workspace(static_cast<int>(a->dtype), N, L, a->q_heads + a->k_heads, a->D,
+                                                              a->R, a->adjacent != 0)));
+        return from_hip(WG_BY_DTYPE(a->dtype, wg::launch_head_norm_rotate_backward_t)(*a, stream), "norm of heads' gradients");
     });
 }
 

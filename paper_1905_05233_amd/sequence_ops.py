@@ -1,16 +1,23 @@
 """Python binding of the sequence operators (argument marshalling only; the work
-runs in the gfx950 kernels of gated_scan.hip, rms_norm.hip and matvec_w4.hip):
-what stands around ``Plan.conv1d`` in a sequence model.
+runs in the gfx950 kernels of gated_scan.hip, linear_attention.hip,
+head_norm_rotate.hip, rms_norm.hip and matvec_w4.hip): what stands around
+``Plan.conv1d`` in a sequence model.
 
   * ``gated_scan``, ``gated_scan_backward``, ``gated_step``: the recurrence
     h = f h_before + (1 - f) value with f = sigmoid(gate), y = h or h silu(out_gate);
+  * ``linear_attention``, ``linear_attention_backward``, ``linear_attention_step``:
+    the recurrence S = exp(log_decay) S_before + k v^T of a matrix for each head,
+    y = scale S^T q;
+  * ``head_norm_rotate``, ``head_norm_rotate_backward`` and ``Rotary``: the norm of
+    each head of queries and keys with the rotation by their position;
   * ``rms_norm``, ``rms_norm_fp8``, ``rms_norm_backward``: the root-mean-square
     norm of rows with the residual's addition, into the storage type or 8 bits;
   * ``W4Matrix``, ``matvec_w4``: products with 4-bit weights with group scales.
 
-Tensors are f32, f16 or bf16 on the current GPU.  Rows [N][L][C] may have any
-strides as long as the channels are contiguous (slices of a projection's rows,
-a buffer with a leading row); states, scales and weights are contiguous.  Calls
+Tensors are f32, f16 or bf16 on the current GPU.  Rows [N][L][C] and heads
+[N][L][H][D] may have any strides as long as the channels are contiguous (slices of
+a projection's rows, a buffer with a leading row); states, scales and weights are
+contiguous.  Calls
 are asynchronous on ``stream`` or the current stream; work that another stream
 has still to do on the inputs is the caller's to wait for.  Outputs must not overlap
 inputs, unless said otherwise.
@@ -20,7 +27,9 @@ require gradients.  Gradients come from the ``_backward`` calls (the 4-bit produ
 none), from within a ``torch.autograd.Function`` where a graph is wanted.
 """
 import ctypes
+import math
 import struct
+from fractions import Fraction
 
 import torch
 
@@ -37,6 +46,11 @@ _pack_scan_backward = struct.Struct("4q" + "Pqq" * 7 + "4PPq").pack
 _pack_step = struct.Struct("3q" + "Pqq" * 4 + "2P").pack
 _pack_norm = struct.Struct("4q" + "Pqq" * 4 + "2Pd2q").pack
 _pack_norm_backward = struct.Struct("4q" + "Pqq" * 4 + "2PdPq").pack
+_pack_attention = struct.Struct("9q" + "Pqqq" * 4 + "4PdPq").pack
+_pack_attention_backward = struct.Struct("9q" + "Pqqq" * 7 + "5PdPq").pack
+_pack_attention_step = struct.Struct("8q" + "Pqqq" * 4 + "3Pd").pack
+_pack_rotate = struct.Struct("8q" + "Pqqq" * 4 + "4Pqd").pack
+_pack_rotate_backward = struct.Struct("8q" + "Pqqq" * 6 + "4Pqd3Pq").pack
 _pack_w4 = struct.Struct("2P3q").pack
 _pack_matvec = struct.Struct("2P3q" + "3q" + "PqPqPq").pack
 _SIZES_KEPT = 256
@@ -109,6 +123,30 @@ def _out(t, name, like, dtype, dev):
     return t, (t.data_ptr(), 0, shape[1])
 
 
+def _heads(t, name, shape, dtype, dev):
+    """(address, stride_n, stride_l, stride_h) of [N][L][H][D], or of [N][H][D] as one step."""
+    try:
+        s = t.stride()
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev and (s[-1] == 1 or shape[-1] <= 1):
+            return (t.data_ptr(), *s[:3]) if len(s) == 4 else (t.data_ptr(), s[0], 0, s[1])
+    except AttributeError:
+        pass
+    _check(t, name, shape, dtype, dev)   # raises, or the strides are at fault
+    raise ValueError(f"{name}: the channels of a head must be contiguous")
+
+
+def _out_heads(t, name, shape, like):
+    """(tensor, its heads): t, or if it is None a new contiguous one."""
+    if t is not None:
+        return t, _heads(t, name, shape, like.dtype, like.get_device())
+    t = torch.empty(shape, dtype=like.dtype, device=like.device)
+    if len(shape) == 3:
+        _, H, D = shape
+        return t, (t.data_ptr(), H * D, 0, D)
+    _, L, H, D = shape
+    return t, (t.data_ptr(), L * H * D, H * D, D)
+
+
 def _new_f32(like, *shape):
     """A contiguous fp32 tensor of two or three dimensions on like's GPU."""
     strides = (shape[1], 1) if len(shape) == 2 else (shape[1] * shape[2], shape[2], 1)
@@ -140,6 +178,8 @@ def _tensors(values):
             yield v
         elif isinstance(v, W4Matrix):
             yield from (v.tiles, v.scales)
+        elif isinstance(v, Rotary):
+            yield v.turns
         elif isinstance(v, (tuple, list)):
             yield from _tensors(v)
 
@@ -261,6 +301,226 @@ def gated_step(gate, value, h, out_gate=None, h_new=None, y=None, stream=None):
     if st != N.WG_OK:
         N.check(st)
     return y, h_new
+
+
+def _attention(q, k, v, log_decay, dims):
+    """(dev, dtype code, (q_heads, k_heads, v_heads, heads, Dk, Dv), addresses of q, k, v and log_decay)."""
+    dev = _first(q, "q", (dims,))
+    dt, lead = q.dtype, q.shape[:-2]
+    code = _code(q, "q")
+    for t, name in ((k, "k"), (v, "v")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch tensor")
+        if t.dim() != dims:
+            raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
+    if not isinstance(log_decay, torch.Tensor):
+        raise TypeError("log_decay must be a torch tensor")
+    if log_decay.dim() != 1:
+        raise ValueError("log_decay must be [heads]")
+    (Hq, Dk), (Hk, _), (Hv, Dv), H = q.shape[-2:], k.shape[-2:], v.shape[-2:], log_decay.shape[0]
+    qh = _heads(q, "q", q.shape, dt, dev)
+    kh = _heads(k, "k", (*lead, Hk, Dk), dt, dev)
+    vh = _heads(v, "v", (*lead, Hv, Dv), dt, dev)
+    return dev, code, (Hq, Hk, Hv, H, Dk, Dv), (qh, kh, vh), _dense(log_decay, "log_decay", (H,), torch.float32, dev)
+
+
+def _attention_size(dev, backward, code, Nn, L, sizes):
+    """Bytes of workspace, asked of the library once for given sizes."""
+    key = ("winograd_linear_attention_workspace", dev, backward, code, Nn, L, sizes)
+    need = _sizes.get(key)
+    if need is None:
+        out = ctypes.c_size_t()
+        args = _pack_attention(code, Nn, L, *sizes, *(0,) * 20, 0.0, 0, 0)
+        N.check(N.lib().winograd_linear_attention_workspace(args, backward, ctypes.byref(out)))
+        need = out.value
+        if len(_sizes) >= _SIZES_KEPT:
+            _sizes.clear()
+        _sizes[key] = need
+    return need
+
+
+def _scale(scale, Dk):
+    return float(Dk) ** -0.5 if scale is None and Dk > 0 else scale
+
+
+def linear_attention(q, k, v, log_decay, s0=None, lengths=None, scale=None, y=None, stream=None):
+    """Linear attention with a decay for each head, over sequences: q [N][L][Hq][Dk],
+    k [N][L][Hk][Dk], v [N][L][Hv][Dv] (one dtype), log_decay fp32 [H], the logarithms
+    of the decays (0 or less).  Hq, Hk and Hv divide H: neighbouring heads share an input.
+    s0 fp32 [N][H][Dk][Dv] (zeros if absent), lengths int32 [N] (steps from there on are
+    padding: y is 0 and the state stays), scale of the outputs (Dk ** -0.5).  Returns
+    (y, s_last): y [N][L][H][Dv], s_last fp32 [N][H][Dk][Dv] the last state."""
+    if stream is not None:
+        return _on(stream, linear_attention, q, k, v, log_decay, s0, lengths, scale, y)
+    dev, code, sizes, heads, gp = _attention(q, k, v, log_decay, 4)
+    Nn, L = q.shape[:2]
+    H, Dk, Dv = sizes[3:]
+    y, yh = _out_heads(y, "y", (Nn, L, H, Dv), q)
+    sp = 0 if s0 is None else _dense(s0, "s0", (Nn, H, Dk, Dv), torch.float32, dev)
+    lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
+    s_last = torch.empty((Nn, H, Dk, Dv), dtype=torch.float32, device=q.device)
+    need = _attention_size(dev, 0, code, Nn, L, sizes)
+    ws = _workspace(need, q)
+    st = N.lib().winograd_linear_attention(
+        _pack_attention(code, Nn, L, *sizes, *heads[0], *heads[1], *heads[2], *yh, gp, sp, lp, s_last.data_ptr(),
+                        _scale(scale, Dk), 0 if ws is None else ws.data_ptr(), need), _raw_stream(None))
+    if st != N.WG_OK:
+        N.check(st)
+    return y, s_last
+
+
+def linear_attention_backward(dy, q, k, v, log_decay, s0=None, ds_last=None, lengths=None, scale=None, out=None,
+                              stream=None):
+    """Gradients of ``linear_attention`` from dy [N][L][H][Dv] and ds_last (fp32
+    [N][H][Dk][Dv], zeros if absent); the other arguments as in the forward call.
+    Returns (dq, dk, dv, ds0), the first three shaped as q, k and v (sums over the heads
+    that share an input) and 0 at padding.  ``out``: tensors for them, as slices of the
+    gradient of one projection.  The decays have no gradient."""
+    if stream is not None:
+        return _on(stream, linear_attention_backward, dy, q, k, v, log_decay, s0, ds_last, lengths, scale, out)
+    dev, code, sizes, heads, gp = _attention(q, k, v, log_decay, 4)
+    Nn, L = q.shape[:2]
+    H, Dk, Dv = sizes[3:]
+    dyh = _heads(dy, "dy", (Nn, L, H, Dv), q.dtype, dev)
+    sp = 0 if s0 is None else _dense(s0, "s0", (Nn, H, Dk, Dv), torch.float32, dev)
+    dsp = 0 if ds_last is None else _dense(ds_last, "ds_last", (Nn, H, Dk, Dv), torch.float32, dev)
+    lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
+    if out is None:
+        out = (None, None, None)
+    elif len(out) != 3:
+        raise ValueError("out must hold dq, dk and dv")
+    dq, dqh = _out_heads(out[0], "dq", q.shape, q)
+    dk, dkh = _out_heads(out[1], "dk", k.shape, q)
+    dv, dvh = _out_heads(out[2], "dv", v.shape, q)
+    ds0 = torch.empty((Nn, H, Dk, Dv), dtype=torch.float32, device=q.device)
+    need = _attention_size(dev, 1, code, Nn, L, sizes)
+    ws = _workspace(need, q)
+    st = N.lib().winograd_linear_attention_backward(
+        _pack_attention_backward(code, Nn, L, *sizes, *dyh, *heads[0], *heads[1], *heads[2], *dqh, *dkh, *dvh, gp, sp, dsp,
+                                 lp, ds0.data_ptr(), _scale(scale, Dk), 0 if ws is None else ws.data_ptr(), need),
+        _raw_stream(None))
+    if st != N.WG_OK:
+        N.check(st)
+    return dq, dk, dv, ds0
+
+
+def linear_attention_step(q, k, v, log_decay, s, scale=None, s_new=None, y=None, stream=None):
+    """One step for N sequences: q [N][Hq][Dk], k [N][Hk][Dk], v [N][Hv][Dv], log_decay
+    fp32 [H], s fp32 [N][H][Dk][Dv] the states.  Returns (y, s_new), y [N][H][Dv];
+    ``s_new=s`` updates the states in place."""
+    if stream is not None:
+        return _on(stream, linear_attention_step, q, k, v, log_decay, s, scale, s_new, y)
+    dev, code, sizes, heads, gp = _attention(q, k, v, log_decay, 3)
+    Nn = q.shape[0]
+    H, Dk, Dv = sizes[3:]
+    sp = _dense(s, "s", (Nn, H, Dk, Dv), torch.float32, dev)
+    y, yh = _out_heads(y, "y", (Nn, H, Dv), q)
+    if s_new is None:
+        s_new = torch.empty_like(s)
+        snp = s_new.data_ptr()
+    else:
+        snp = _dense(s_new, "s_new", s.shape, torch.float32, dev)
+    st = N.lib().winograd_linear_attention_step(
+        _pack_attention_step(code, Nn, *sizes, *heads[0], *heads[1], *heads[2], *yh, gp, sp, snp, _scale(scale, Dk)),
+        _raw_stream(None))
+    if st != N.WG_OK:
+        N.check(st)
+    return y, s_new
+
+
+# 2 pi to 60 digits
+_TWO_PI = Fraction(6283185307179586476925286766559005768394338798750211641949889, 10 ** 60)
+
+
+class Rotary:
+    """The rotation of ``head_norm_rotate``: pair i of a head's first ``channels`` channels
+    turns by ``frequencies[i]`` radians a position, base ** (-2 i / channels) if they are
+    not given.  Pairs are (i, i + channels / 2) or, with ``adjacent``, (2 i, 2 i + 1).
+    Holds the frequencies on the GPU as 64-bit fractions of a turn."""
+    __slots__ = ("_turns", "_channels", "_adjacent")
+    turns = property(lambda self: self._turns)
+    channels = property(lambda self: self._channels)
+    adjacent = property(lambda self: self._adjacent)
+
+    def __init__(self, channels, base=10000.0, frequencies=None, adjacent=False, device="cuda"):
+        if channels < 2 or channels % 2:
+            raise ValueError("channels must be even and positive")
+        if frequencies is None:
+            if not (math.isfinite(base) and base > 0):
+                raise ValueError("base must be positive")
+            frequencies = [base ** (-2.0 * i / channels) for i in range(channels // 2)]
+        frequencies = [float(f) for f in frequencies]
+        if len(frequencies) != channels // 2 or not all(map(math.isfinite, frequencies)):
+            raise ValueError("frequencies must be channels / 2 finite numbers")
+        words = [round(Fraction(f) / _TWO_PI * 2 ** 64) % 2 ** 64 for f in frequencies]
+        self._turns = torch.tensor([w - 2 ** 64 if w >= 2 ** 63 else w for w in words], dtype=torch.int64, device=device)
+        self._channels, self._adjacent = channels, bool(adjacent)
+
+
+def _rotation(q, k, q_weight, k_weight, rotary, positions, start):
+    dev = _first(q, "q", (3, 4))
+    dt, lead = q.dtype, q.shape[:-2]
+    code = _code(q, "q")
+    if not isinstance(k, torch.Tensor):
+        raise TypeError("k must be a torch tensor")
+    if k.dim() != q.dim():
+        raise ValueError(f"k must have {q.dim()} dimensions, got {k.dim()}")
+    if not isinstance(rotary, Rotary):
+        raise TypeError("rotary must be a Rotary")
+    (Hq, D), Hk = q.shape[-2:], k.shape[-2]
+    Nn, L = (*lead, 1)[:2]
+    shapes = q.shape, (*lead, Hk, D)
+    heads = _heads(q, "q", shapes[0], dt, dev), _heads(k, "k", shapes[1], dt, dev)
+    w = _dense(q_weight, "q_weight", (D,), dt, dev), _dense(k_weight, "k_weight", (D,), dt, dev)
+    turns = _dense(rotary._turns, "rotary", (rotary._channels // 2,), torch.int64, dev)
+    pp = 0 if positions is None else _dense(positions, "positions", lead, torch.int32, dev)
+    return dev, (code, Nn, L, Hq, Hk, D, rotary._channels, rotary._adjacent), shapes, heads, (*w, turns, pp, start)
+
+
+def head_norm_rotate(q, k, q_weight, k_weight, rotary, positions=None, start=0, eps=1e-6, q_out=None, k_out=None,
+                     stream=None):
+    """The root-mean-square norm of each head of q [N][L][Hq][D] and k [N][L][Hk][D],
+    times the weights [D], and the rotation by the ``Rotary`` at positions int32 [N][L],
+    or start + l.  For single tokens q, k and positions may be [N][H][D] and [N].  Returns
+    (q_out, k_out); they may be given, and be q and k themselves."""
+    if stream is not None:
+        return _on(stream, head_norm_rotate, q, k, q_weight, k_weight, rotary, positions, start, eps, q_out, k_out)
+    _, sizes, shapes, heads, rest = _rotation(q, k, q_weight, k_weight, rotary, positions, start)
+    q_out, qh = _out_heads(q_out, "q_out", shapes[0], q)
+    k_out, kh = _out_heads(k_out, "k_out", shapes[1], q)
+    st = N.lib().winograd_head_norm_rotate(_pack_rotate(*sizes, *heads[0], *heads[1], *qh, *kh, *rest, eps), _raw_stream(None))
+    if st != N.WG_OK:
+        N.check(st)
+    return q_out, k_out
+
+
+def head_norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, rotary, positions=None, start=0, eps=1e-6, out=None,
+                              stream=None):
+    """Gradients of ``head_norm_rotate`` from those of its outputs; the other arguments as
+    in the forward call.  Returns (dq, dk, dq_weight, dk_weight), the weights' fp32 [D].
+    ``out``: tensors for dq and dk, which may be dq_out and dk_out."""
+    if stream is not None:
+        return _on(stream, head_norm_rotate_backward, dq_out, dk_out, q, k, q_weight, k_weight, rotary, positions, start, eps,
+                   out)
+    dev, sizes, shapes, heads, rest = _rotation(q, k, q_weight, k_weight, rotary, positions, start)
+    code, Nn, L, Hq, Hk, D, R, adjacent = sizes
+    dqo = _heads(dq_out, "dq_out", shapes[0], q.dtype, dev)
+    dko = _heads(dk_out, "dk_out", shapes[1], q.dtype, dev)
+    if out is None:
+        out = (None, None)
+    elif len(out) != 2:
+        raise ValueError("out must hold dq and dk")
+    dq, dqh = _out_heads(out[0], "dq", shapes[0], q)
+    dk, dkh = _out_heads(out[1], "dk", shapes[1], q)
+    dw = _new_f32(q, 2, D)
+    need = _size("winograd_head_norm_rotate_workspace", dev, code, Nn, L, Hq + Hk, D, R, adjacent)
+    ws = _workspace(need, q)
+    st = N.lib().winograd_head_norm_rotate_backward(
+        _pack_rotate_backward(*sizes, *dqo, *dko, *heads[0], *heads[1], *dqh, *dkh, *rest, eps, dw.data_ptr(),
+                              dw.data_ptr() + 4 * D, 0 if ws is None else ws.data_ptr(), need), _raw_stream(None))
+    if st != N.WG_OK:
+        N.check(st)
+    return dq, dk, dw[0], dw[1]
 
 
 def _norm(x, weight, residual, eps, out, r, quant, group):
