@@ -43,12 +43,14 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 256;   // of the kernels beside the attention itself
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// bf16 parts of an input, and of a value computed in fp32
+// bf16 parts of an input, of the values computed in fp32 that outputs are made of, and
+// of those that the state is made of, which is returned in fp32
 template <typename Elem> constexpr int kParts = std::is_same_v<Elem, bf16_t> ? 1 : std::is_same_v<Elem, _Float16> ? 2 : 3;
 template <typename Elem> constexpr int kSums = std::is_same_v<Elem, float> ? 3 : 2;
+constexpr int kStateParts = 3;
 // steps of a tile
 template <typename Elem> constexpr int kTile = std::is_same_v<Elem, bf16_t> ? 64 : 32;
 
@@ -79,6 +81,7 @@ struct Pass {
     StateAt at;
     float in_scale, out_scale;
     int32_t reverse;
+    int32_t from_segments;    // s_in holds a state for each segment, [N][H][segments]
 };
 
 struct Args {
@@ -86,6 +89,7 @@ struct Args {
     int32_t first[4];         // workgroups of a segment of each pass, added up
     int64_t N;
     int32_t L, H;
+    int32_t segments, each;   // runs of `each` tiles in the order of the walk
     const float* log_decay;
     const int32_t* lengths;
     float scale;
@@ -97,9 +101,13 @@ __device__ __forceinline__ int32_t steps_of(const int32_t* lengths, int64_t n, i
     return v < 0 ? 0 : (v > L ? L : v);
 }
 
-// lambda^n from log2(lambda), also where lambda is 0
+// log2(lambda); where lambda is 0 a number whose every multiple but that by 0 is a
+// power that is 0 in fp32.
+__device__ __forceinline__ float log2_of(float log_decay) {
+    return log_decay == -__builtin_inff() ? -1e30f : log_decay * kLog2e;
+}
 __device__ __forceinline__ float power(float log2_decay, int n) {
-    return n == 0 ? 1.0f : __builtin_amdgcn_exp2f(log2_decay * static_cast<float>(n));
+    return __builtin_amdgcn_exp2f(log2_decay * static_cast<float>(n));
 }
 // lambda^n to fp32's last place: the state is multiplied by it once a tile, and its
 // errors would add up.
@@ -107,25 +115,31 @@ __device__ __forceinline__ float exact_power(float log_decay, int n) {
     return n == 0 ? 1.0f : static_cast<float>(exp(static_cast<double>(log_decay) * n));
 }
 
-// x as the sum of bf16 parts.  What is left of an infinity is made finite, so that
-// infinities stay infinities.
-template <int P, int V> struct Split {
+// x as the sum of bf16 parts.  What an input's rounding leaves of an infinity is made
+// finite (FINITE), so that the parts stay an infinity together.
+template <int P, int V, bool FINITE> struct Split {
     typedef __bf16 Run __attribute__((ext_vector_type(V)));
     Run part[P];
     __device__ __forceinline__ void of(const float (&x)[V]) {
+        float left[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float left = x[e];
+        for (int e = 0; e < V; ++e) left[e] = x[e];
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                part[p][e] = static_cast<__bf16>(left);
-                if (p + 1 < P) left = __builtin_amdgcn_fmed3f(left - static_cast<float>(part[p][e]), -0x1p120f, 0x1p120f);
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) part[p][e] = static_cast<__bf16>(left[e]);
+            if (p + 1 < P) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    left[e] -= static_cast<float>(part[p][e]);
+                    if (FINITE) left[e] = __builtin_amdgcn_fmed3f(left[e], -0x1p120f, 0x1p120f);
+                }
             }
         }
     }
 };
 
-// c += a b over the parts whose product is not below the last part's
+// c += a b over the parts whose product is not below the last of P
 template <int PA, int PB, int P>
 __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[PA], const bf16x8 (&b)[PB], f32x4 c) {
 #pragma unroll
@@ -162,29 +176,39 @@ template <int PLANES, int ROWS, int WIDTH> struct TileLds {
 };
 
 // A tile's rows on their way from memory: 16 bytes of U rows a thread.
-template <typename Elem, int ROWS, int WIDTH> struct TileLoad {
-    static constexpr int V = Vec<Elem>::V, kRuns = WIDTH / V, kPer = kThreads / kRuns, U = (ROWS + kPer - 1) / kPer;
-    static_assert(kRuns <= kThreads && (ROWS % kPer == 0 || U == 1), "threads cover whole rows");
+template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
+    static constexpr int V = Vec<Elem>::V, kRuns = WIDTH / V, kPer = THREADS / kRuns, U = (ROWS + kPer - 1) / kPer;
+    static_assert(THREADS % kRuns == 0 && (ROWS % kPer == 0 || U == 1), "threads cover whole rows");
     u32x4 raw[U];
 
     // rows 0 .. live - 1 from p, `stride` apart; channels c0 .. of D; zeros elsewhere
     __device__ __forceinline__ void load(const Elem* p, int64_t stride, int live, int c0, int D) {
         const int c = c0 + static_cast<int>(threadIdx.x) % kRuns * V, r0 = threadIdx.x / kRuns;
+        const Elem* at = p + r0 * stride + c;
+        if (live == ROWS && ROWS % kPer == 0 && D - c0 >= WIDTH) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = reinterpret_cast<const Bytes16*>(at + u * kPer * stride)->v;
+            return;
+        }
+        const int over = c + V - D;   // a short run is the end of 16 bytes that end with the row
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int row = r0 + u * kPer;
             raw[u] = u32x4{0, 0, 0, 0};
-            if (row >= live) continue;
-            const Elem* at = p + row * stride + c;
-            if (c + V <= D) {
-                raw[u] = reinterpret_cast<const Bytes16*>(at)->v;
-            } else if (c < D) {
+            if (r0 + u * kPer >= live || over >= V) continue;
+            const Elem* run = at + u * kPer * stride;
+            if (D >= V) {
+                raw[u] = reinterpret_cast<const Bytes16*>(run - max(0, over))->v;
+            } else {
                 typename Vec<Elem>::Packed e{};
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    if (c + j < D) e.v[j] = at[j];
+                    if (j < V - over) e.v[j] = run[j];
                 raw[u] = __builtin_bit_cast(u32x4, e);
             }
+        }
+        if (over > 0 && D >= V) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = drop_first<Elem>(raw[u], over);
         }
     }
     template <int PLANES> __device__ __forceinline__ void store(TileLds<PLANES, ROWS, WIDTH>& to) const {
@@ -198,70 +222,98 @@ template <typename Elem, int ROWS, int WIDTH> struct TileLoad {
             } else {
                 float x[V];
                 Vec<Elem>::widen(raw[u], x);
-                Split<PLANES, V> s;
+                Split<PLANES, V, true> s;
                 s.of(x);
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) *reinterpret_cast<typename Split<PLANES, V>::Run*>(&to.v[p][row][c]) = s.part[p];
+                for (int p = 0; p < PLANES; ++p)
+                    *reinterpret_cast<typename Split<PLANES, V, true>::Run*>(&to.v[p][row][c]) = s.part[p];
             }
         }
     }
     __device__ __forceinline__ bool finite() const {
-        bool all = true;
+        if constexpr (sizeof(Elem) == 4) {
+            uint32_t top = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[V];
-            Vec<Elem>::widen(raw[u], x);
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) all &= fabsf(x[e]) < __builtin_inff();
+                for (int e = 0; e < 4; ++e) top = max(top, raw[u][e] & 0x7fffffffu);
+            return top < 0x7f800000u;
+        } else {
+            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 top = {0, 0};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, raw[u][e] & 0x7fff7fffu));
+            constexpr unsigned short kInf = std::is_same_v<Elem, bf16_t> ? 0x7f80 : 0x7c00;
+            return top[0] < kInf && top[1] < kInf;
         }
-        return all;
     }
-};
-
-// Where a pass's workgroup stands.
-struct Place {
-    int32_t pass, block, h;
-    int64_t n;
 };
 
 template <typename Elem> __device__ __forceinline__ const Elem* heads_at(const HeadsIn& t, int64_t n, int32_t h) {
     return static_cast<const Elem*>(t.p) + n * t.sn + h / t.per * t.sh;
 }
 
-template <typename Elem, int KD, int CB> struct Shape {
+// 4 CB values side by side, of which those below `valid` are wanted
+template <typename T, int COUNT> __device__ __forceinline__ void store_values(T* to, const float (&x)[COUNT], int valid) {
+    struct __attribute__((packed, aligned(sizeof(T)))) Values {
+        T v[COUNT];
+    };
+    if (valid >= COUNT) {
+        Values w;
+#pragma unroll
+        for (int e = 0; e < COUNT; ++e) w.v[e] = Storage<T>::from_f32(x[e]);
+        *reinterpret_cast<Values*>(to) = w;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e)
+        if (e < valid) to[e] = Storage<T>::from_f32(x[e]);
+}
+
+// Tiles of K channels of q and k for W waves of 16 C columns each.
+template <typename Elem, int K, int W, int C> struct Shape {
     static constexpr int T = kTile<Elem>, PI = kParts<Elem>, PS = kSums<Elem>;
-    static constexpr int VB = 64 * CB;          // columns of a workgroup
+    static constexpr int kColumns = 16 * C * W, kThreads = 64 * W;
     struct Lds {
-        TileLds<PI, T, KD> q, k;
-        TileLds<PI, T, VB> v;
+        TileLds<PI, T, K> q, k;
+        TileLds<PI, T, kColumns> v;
         TileLds<PS, T, T> p;
-        int32_t odd;                            // v holds an infinity or NaN
+        int32_t odd;   // the tile (+ 1) of which v holds an infinity or NaN
+    };
+    struct StatesLds {
+        TileLds<PI, T, K> k;
+        TileLds<PI, T, kColumns> v;
     };
 };
 
-// A pass.  A wave's accumulators of the state: S[b][c], lane m + 16 g, register r holds
-// the state at (32 (b / 2) + 8 g + 4 (b % 2) + r, column(c, m)), so that those of two
-// blocks side by side are the 8 consecutive rows that a lane hands a matrix
-// instruction, without a move.  Outputs come transposed, O[i][c] with row 16 i + m and
-// columns column(c, 4 g + r): four or eight side by side.
-template <typename Elem, int KD, int CB>
-__global__ __launch_bounds__(kThreads) void attention_kernel(Args a) {
-    using Sh = Shape<Elem, KD, CB>;
-    constexpr int T = Sh::T, PI = Sh::PI, PS = Sh::PS, VB = Sh::VB, IB = T / 16, JS = T / 32, KS = KD / 32;
-    __shared__ __align__(16) typename Sh::Lds lds;
+// A pass, or (STATES) only what its segments add to the state.  A wave's accumulators of
+// the state: S[b][c], lane m + 16 g, register r holds the state at
+// (32 (b / 2) + 8 g + 4 (b % 2) + r, column(c, m)), so that those of two blocks side by
+// side are the 8 consecutive rows that a lane hands a matrix instruction, without a
+// move.  Outputs come transposed, O[i][c] with row 16 i + m and columns
+// column(c, 4 g + r): 4 C of them side by side.
+template <typename Elem, int KD, int W, int CB, bool STATES>
+__global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void attention_kernel(Args a) {
+    using Sh = Shape<Elem, KD, W, CB>;
+    constexpr int T = Sh::T, PI = Sh::PI, PS = Sh::PS, VB = Sh::kColumns, NT = Sh::kThreads, IB = T / 16, JS = T / 32, KS = KD / 32;
+    __shared__ __align__(16) std::conditional_t<STATES, typename Sh::StatesLds, typename Sh::Lds> lds;
     const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, m = lane % 16, g = lane / 16;
 
-    int32_t which = 0;
-    const uint32_t id = blockIdx.x;
-    while (id >= static_cast<uint32_t>(a.first[which + 1])) ++which;
+    const int32_t segment = blockIdx.x / static_cast<uint32_t>(a.first[3]);
+    const int32_t id = blockIdx.x - segment * a.first[3];
+    const int which = id >= a.first[2] ? 2 : id >= a.first[1] ? 1 : 0;
     const Pass& pass = a.pass[which];
     const uint32_t unit = id - a.first[which];
-    const int32_t block = unit % pass.blocks;
-    const int32_t h = unit / pass.blocks % a.H;
-    const int64_t n = unit / pass.blocks / a.H;
+    const uint32_t head = unit / static_cast<uint32_t>(pass.blocks);
+    const int32_t block = unit - head * pass.blocks, h = head % static_cast<uint32_t>(a.H);
+    const int64_t n = head / static_cast<uint32_t>(a.H);
     const int32_t steps = steps_of(a.lengths, n, a.L), kd = pass.kd, vd = pass.vd, v0 = block * VB;
     const bool reverse = pass.reverse != 0;
-    const float log_decay = a.log_decay[h], log2_decay = log_decay * kLog2e;
+    const float log_decay = a.log_decay[h], log2_decay = log2_of(log_decay);
+    const float in_scale = pass.in_scale, out_scale = pass.out_scale, scale = a.scale;
 
     auto column = [&](int c, int i) { return CB == 1 ? 16 * wave + i : 32 * wave + 8 * (i / 4) + 4 * c + i % 4; };
     // channels that a lane hands to a transposing read, of the state's rows and columns
@@ -269,111 +321,131 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(Args a) {
     auto column_chunk = [&](int c) { return column(c, 4 * (m % 4)); };
 
     f32x4 S[KD / 16][CB];
-    const int64_t state = (n * a.H + h) * static_cast<int64_t>(kd) * vd;
-#pragma unroll
-    for (int b = 0; b < KD / 16; ++b)
-#pragma unroll
-        for (int c = 0; c < CB; ++c)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + column(c, m);
-                S[b][c][r] = pass.s_in && i < kd && j < vd ? pass.s_in[state + i * pass.at.row + j * pass.at.col] : 0.0f;
-            }
-
-    const Elem* q = heads_at<Elem>(pass.q, n, h);
-    const Elem* k = heads_at<Elem>(pass.k, n, h);
-    const Elem* v = heads_at<Elem>(pass.v, n, h);
-    TileLoad<Elem, T, KD> lq, lk;
-    TileLoad<Elem, T, VB> lv;
-    const int32_t tiles = (steps + T - 1) / T;
-    auto first_of = [&](int32_t t) { return (reverse ? tiles - 1 - t : t) * T; };
-    auto load = [&](int32_t t) {
-        const int32_t t0 = first_of(t), live = min(T, steps - t0);
-        lq.load(q + t0 * pass.q.sl, pass.q.sl, live, 0, kd);
-        lk.load(k + t0 * pass.k.sl, pass.k.sl, live, 0, kd);
-        lv.load(v + t0 * pass.v.sl, pass.v.sl, live, v0, vd);
-    };
-    // weights above the diagonal are zeros that nothing writes
-    for (int i = tid; i < static_cast<int>(sizeof(lds.p) / 4); i += kThreads) reinterpret_cast<uint32_t*>(&lds.p)[i] = 0;
-    if (tid == 0) lds.odd = 0;
-    if (tiles > 0) load(0);
-    __syncthreads();
-
-    for (int32_t t = 0; t < tiles; ++t) {
-        const int32_t t0 = first_of(t), live = min(T, steps - t0);
-        lq.template store<PI>(lds.q);
-        lk.template store<PI>(lds.k);
-        lv.template store<PI>(lds.v);
-        if (!lv.finite()) lds.odd = t + 1;
-        if (t + 1 < tiles) load(t + 1);
-        __syncthreads();
-
-        // the weights of the tile, in blocks of 16 x 16 of the triangle
-        for (int blk = wave; blk < IB * (IB + 1) / 2; blk += kWaves) {
-            const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
-            const int ib = reverse ? near : far, jb = reverse ? far : near;
-            f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                bf16x8 fk[PI], fq[PI];
-                lds.k.across(16 * jb + m, 32 * s + 8 * g, fk);
-                lds.q.across(16 * ib + m, 32 * s + 8 * g, fq);
-                w = multiply<PI, PI, PS>(fk, fq, w);
-            }
-            float x[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * ib + m, j = 16 * jb + 4 * g + r, d = reverse ? j - i : i - j;
-                x[r] = d < 0 ? 0.0f : w[r] * (a.scale * power(log2_decay, d));
-            }
-            Split<PS, 4> parts;
-            parts.of(x);
-#pragma unroll
-            for (int p = 0; p < PS; ++p) *reinterpret_cast<bf16x4*>(&lds.p.v[p][16 * ib + m][16 * jb + 4 * g]) = parts.part[p];
-        }
-
-        // what the state gives
-        f32x4 O[IB][CB];
-#pragma unroll
-        for (int i = 0; i < IB; ++i)
-#pragma unroll
-            for (int c = 0; c < CB; ++c) O[i][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            Split<PS, 8> fs[CB];
-#pragma unroll
-            for (int c = 0; c < CB; ++c) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][c][e % 4];
-                fs[c].of(x);
-            }
-#pragma unroll
-            for (int i = 0; i < IB; ++i) {
-                bf16x8 fq[PI];
-                lds.q.across(16 * i + m, 32 * s + 8 * g, fq);
-#pragma unroll
-                for (int c = 0; c < CB; ++c) O[i][c] = multiply<PS, PI, PS>(fs[c].part, fq, O[i][c]);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < IB; ++i) {
-            const int row = 16 * i + m;
-            const float f = pass.out_scale * power(log2_decay, reverse ? max(0, live - 1 - row) : row + 1);
-#pragma unroll
-            for (int c = 0; c < CB; ++c) O[i][c] *= f;
-        }
-
-        // the state behind the tile
-        const float whole = exact_power(log_decay, live);
+    auto each_state = [&](auto&& f) {
 #pragma unroll
         for (int b = 0; b < KD / 16; ++b)
 #pragma unroll
-            for (int c = 0; c < CB; ++c) S[b][c] *= whole;
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + column(c, m);
+                    if (i < kd && j < vd) S[b][c][r] = f(S[b][c][r], i * pass.at.row + j * pass.at.col);
+                }
+    };
+#pragma unroll
+    for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) S[b][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int64_t size = static_cast<int64_t>(kd) * vd, by_segment = (static_cast<int64_t>(head) * a.segments + segment) * size;
+    if (!STATES && pass.s_in) {
+        const float* s = pass.s_in + (pass.from_segments ? by_segment : head * size);
+        each_state([&](float, int at) { return s[at]; });
+    }
+
+    const int32_t tiles = (steps + T - 1) / T, t_end = min(tiles, (segment + 1) * a.each);
+    int32_t t = segment * a.each;
+    const int64_t q_sl = pass.q.sl, k_sl = pass.k.sl, v_sl = pass.v.sl, y_sl = pass.y.sl;
+    const Elem* q = heads_at<Elem>(pass.q, n, h);
+    const Elem* k = heads_at<Elem>(pass.k, n, h);
+    const Elem* v = heads_at<Elem>(pass.v, n, h);
+    TileLoad<Elem, T, KD, NT> lq, lk;
+    TileLoad<Elem, T, VB, NT> lv;
+    auto first_of = [&](int32_t t) { return (reverse ? tiles - 1 - t : t) * T; };
+    auto load = [&](int32_t t) {
+        const int32_t t0 = first_of(t), live = min(T, steps - t0);
+        if (!STATES) lq.load(q + t0 * q_sl, q_sl, live, 0, kd);
+        lk.load(k + t0 * k_sl, k_sl, live, 0, kd);
+        lv.load(v + t0 * v_sl, v_sl, live, v0, vd);
+    };
+    if (t < t_end) load(t);
+    if constexpr (!STATES) {
+        // weights above the diagonal are zeros that nothing writes
+        for (int i = tid; i < static_cast<int>(sizeof(lds.p) / 4); i += NT) reinterpret_cast<uint32_t*>(&lds.p)[i] = 0;
+        if (tid == 0) lds.odd = 0;
+        __syncthreads();
+    }
+
+    // decays of a whole tile; the last one may be short
+    const float whole = exact_power(log_decay, T);
+    for (; t < t_end; ++t) {
+        const int32_t t0 = first_of(t), live = min(T, steps - t0);
+        if constexpr (!STATES) lq.template store<PI>(lds.q);
+        lk.template store<PI>(lds.k);
+        lv.template store<PI>(lds.v);
+        if constexpr (!STATES)
+            if (!lv.finite()) lds.odd = t + 1;
+        if (t + 1 < t_end) load(t + 1);
+        __syncthreads();
+
+        f32x4 O[IB][CB];
+        if constexpr (!STATES) {
+            // the weights of the tile, in blocks of 16 x 16 of the triangle
+            for (int blk = wave; blk < IB * (IB + 1) / 2; blk += W) {
+                const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
+                const int ib = reverse ? near : far, jb = reverse ? far : near;
+                f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    bf16x8 fk[PI], fq[PI];
+                    lds.k.across(16 * jb + m, 32 * s + 8 * g, fk);
+                    lds.q.across(16 * ib + m, 32 * s + 8 * g, fq);
+                    w = multiply<PI, PI, PS>(fk, fq, w);
+                }
+                float x[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * ib + m, j = 16 * jb + 4 * g + r, d = reverse ? j - i : i - j;
+                    x[r] = d < 0 ? 0.0f : w[r] * (scale * power(log2_decay, d));
+                }
+                Split<PS, 4, false> parts;
+                parts.of(x);
+#pragma unroll
+                for (int p = 0; p < PS; ++p)
+                    *reinterpret_cast<bf16x4*>(&lds.p.v[p][16 * ib + m][16 * jb + 4 * g]) = parts.part[p];
+            }
+
+            // what the state gives
+#pragma unroll
+            for (int i = 0; i < IB; ++i)
+#pragma unroll
+                for (int c = 0; c < CB; ++c) O[i][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                Split<PS, 8, false> fs[CB];
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][c][e % 4];
+                    fs[c].of(x);
+                }
+#pragma unroll
+                for (int i = 0; i < IB; ++i) {
+                    bf16x8 fq[PI];
+                    lds.q.across(16 * i + m, 32 * s + 8 * g, fq);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) O[i][c] = multiply<PS, PI, PS>(fs[c].part, fq, O[i][c]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < IB; ++i) {
+                const int row = 16 * i + m;
+                const float f = out_scale * power(log2_decay, reverse ? max(0, live - 1 - row) : row + 1);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) O[i][c] *= f;
+            }
+        }
+
+        // the state behind the tile
+        const float decay = live == T ? whole : exact_power(log_decay, live);
+#pragma unroll
+        for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) S[b][c] *= decay;
         bf16x8 fv[JS][CB][PI];
 #pragma unroll
         for (int s = 0; s < JS; ++s) {
-            Split<PS, 8> late[CB];
+            Split<kStateParts, 8, false> late[CB];
 #pragma unroll
             for (int c = 0; c < CB; ++c) {
                 lds.v.down(32 * s + 8 * g + m / 4, column_chunk(c), fv[s][c]);
@@ -384,7 +456,7 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(Args a) {
                     float sum = 0.0f;
 #pragma unroll
                     for (int p = PI - 1; p >= 0; --p) sum += static_cast<float>(fv[s][c][p][e]);
-                    x[e] = sum * (pass.in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j)));
+                    x[e] = sum * (in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j)));
                 }
                 late[c].of(x);
             }
@@ -393,87 +465,132 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(Args a) {
                 bf16x8 fk[PI];
                 lds.k.down(32 * s + 8 * g + m / 4, row_chunk(b), fk);
 #pragma unroll
-                for (int c = 0; c < CB; ++c) S[b][c] = multiply<PI, PS, PS>(fk, late[c].part, S[b][c]);
+                for (int c = 0; c < CB; ++c) S[b][c] = multiply<PI, kStateParts, kStateParts>(fk, late[c].part, S[b][c]);
             }
         }
         __syncthreads();
+        if constexpr (STATES) continue;
 
-        // what the tile's own steps give
-        if (lds.odd != t + 1) {
+        if constexpr (!STATES) {
+            // what the tile's own steps give
+            if (lds.odd != t + 1) {
 #pragma unroll
-            for (int i = 0; i < IB; ++i)
+                for (int i = 0; i < IB; ++i)
 #pragma unroll
-                for (int s = 0; s < JS; ++s) {
-                    if (reverse ? 32 * s + 31 < 16 * i : 32 * s > 16 * i + 15) continue;
-                    bf16x8 fp[PS];
-                    lds.p.across(16 * i + m, 32 * s + 8 * g, fp);
+                    for (int s = 0; s < JS; ++s) {
+                        if (reverse ? 32 * s + 31 < 16 * i : 32 * s > 16 * i + 15) continue;
+                        bf16x8 fp[PS];
+                        lds.p.across(16 * i + m, 32 * s + 8 * g, fp);
 #pragma unroll
-                    for (int c = 0; c < CB; ++c) O[i][c] = multiply<PI, PS, PS>(fv[s][c], fp, O[i][c]);
+                        for (int c = 0; c < CB; ++c) O[i][c] = multiply<PI, PS, PS>(fv[s][c], fp, O[i][c]);
+                    }
+            } else {
+                // step by step: a weight of zero would not remove an infinity or NaN of a later v
+#pragma unroll
+                for (int i = 0; i < IB; ++i) {
+                    const int row = 16 * i + m;
+                    for (int j = reverse ? row : 0; j < (reverse ? T : row + 1); ++j) {
+                        float w = 0.0f;
+#pragma unroll
+                        for (int p = PS - 1; p >= 0; --p) w += __uint_as_float(static_cast<uint32_t>(lds.p.v[p][row][j]) << 16);
+#pragma unroll
+                        for (int c = 0; c < CB; ++c)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                float x = 0.0f;
+#pragma unroll
+                                for (int p = PI - 1; p >= 0; --p)
+                                    x += __uint_as_float(static_cast<uint32_t>(lds.v.v[p][j][column(c, 4 * g + r)]) << 16);
+                                O[i][c][r] += w * x;
+                            }
+                    }
                 }
-        } else {
-            // step by step: a weight of zero would not remove an infinity or NaN of a later v
+            }
 #pragma unroll
             for (int i = 0; i < IB; ++i) {
-                const int row = 16 * i + m;
-                for (int j = reverse ? row : 0; j < (reverse ? T : row + 1); ++j) {
-                    float w = 0.0f;
-#pragma unroll
-                    for (int p = PS - 1; p >= 0; --p) w += __uint_as_float(static_cast<uint32_t>(lds.p.v[p][row][j]) << 16);
-#pragma unroll
-                    for (int c = 0; c < CB; ++c)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            float x = 0.0f;
-#pragma unroll
-                            for (int p = PI - 1; p >= 0; --p)
-                                x += __uint_as_float(static_cast<uint32_t>(lds.v.v[p][j][column(c, 4 * g + r)]) << 16);
-                            O[i][c][r] += w * x;
-                        }
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < IB; ++i) {
-            const int row = 16 * i + m, j = v0 + column(0, 4 * g);
-            if (row >= live || j >= vd) continue;
-            const int64_t at = n * pass.y.sn + (t0 + row) * pass.y.sl + h * pass.y.sh + j;
-            if (pass.y.f32) {
-                float* y = static_cast<float*>(pass.y.p) + at;
+                const int row = 16 * i + m, j = v0 + column(0, 4 * g);
+                if (row >= live || j >= vd) continue;
+                const int64_t at = n * pass.y.sn + (t0 + row) * y_sl + h * pass.y.sh + j;
+                float x[4 * CB];
 #pragma unroll
                 for (int c = 0; c < CB; ++c)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (j + 4 * c + r < vd) y[4 * c + r] = O[i][c][r];
-            } else {
-                Elem* y = static_cast<Elem*>(pass.y.p) + at;
-#pragma unroll
-                for (int c = 0; c < CB; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (j + 4 * c + r < vd) y[4 * c + r] = Storage<Elem>::from_f32(O[i][c][r]);
+                    for (int r = 0; r < 4; ++r) x[4 * c + r] = O[i][c][r];
+                if (pass.y.f32) store_values<float>(static_cast<float*>(pass.y.p) + at, x, vd - j);
+                else store_values<Elem>(static_cast<Elem*>(pass.y.p) + at, x, vd - j);
             }
+            __syncthreads();
         }
-        __syncthreads();
     }
 
-    // padding
-    const int width = min(VB, vd - v0);
-    for (int64_t i = tid; i < static_cast<int64_t>(a.L - steps) * width; i += kThreads) {
-        const int64_t row = steps + i / width;
-        const int64_t at = n * pass.y.sn + row * pass.y.sl + h * pass.y.sh + v0 + i % width;
-        if (pass.y.f32) static_cast<float*>(pass.y.p)[at] = 0.0f;
-        else static_cast<Elem*>(pass.y.p)[at] = Storage<Elem>::from_f32(0.0f);
+    if constexpr (STATES) {
+        float* s = pass.s_out + by_segment;
+        each_state([&](float x, int at) { return s[at] = x; });
+        return;
+    } else {
+        // padding, of which each segment takes a share of rows
+        const int width = min(VB, vd - v0), share = (a.L - steps + a.segments - 1) / a.segments;
+        const int32_t row0 = steps + min(segment * static_cast<int64_t>(share), static_cast<int64_t>(a.L - steps));
+        const int64_t values = static_cast<int64_t>(min(share, a.L - row0)) * width;
+        for (int64_t i = tid; i < values; i += NT) {
+            const int64_t at = n * pass.y.sn + (row0 + i / width) * y_sl + h * pass.y.sh + v0 + i % width;
+            if (pass.y.f32) static_cast<float*>(pass.y.p)[at] = 0.0f;
+            else static_cast<Elem*>(pass.y.p)[at] = Storage<Elem>::from_f32(0.0f);
+        }
+        if (!pass.s_out) return;
+        float* s = pass.s_out + head * size;
+        each_state([&](float x, int at) { return s[at] = x; });
     }
-    if (!pass.s_out) return;
+}
+
+// The states ahead of the segments from what each adds: in place, [N][H][segments] of
+// `size` values, from s_in [N][H] (or null: zeros) to s_out (or null).
+struct Chain {
+    float* states;
+    const float* s_in;
+    float* s_out;
+    int32_t size, reverse;
+};
+struct ChainArgs {
+    Chain chain[2];
+    int64_t heads;            // N H
+    int32_t L, H, segments, each_steps, tile, blocks, of;
+    const float* log_decay;
+    const int32_t* lengths;
+};
+__global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
+    constexpr int U = 8;      // segments whose loads are in flight together
+    const Chain& c = a.chain[blockIdx.x % a.of];
+    const uint32_t unit = blockIdx.x / a.of;
+    const int64_t head = unit / a.blocks;
+    const int32_t i = static_cast<int32_t>(unit % a.blocks) * kThreads + threadIdx.x;
+    if (i >= c.size) return;
+    const int32_t steps = steps_of(a.lengths, head / a.H, a.L), end = (steps + a.tile - 1) / a.tile * a.tile;
+    const float log_decay = a.log_decay[head % a.H];
+    // steps of a segment: all but the last have each_steps, but the reverse of a walk
+    // begins with the tile that may be short
+    auto steps_in = [&](int32_t w) {
+        const int64_t from = static_cast<int64_t>(w) * a.each_steps, to = min(static_cast<int64_t>(end), from + a.each_steps);
+        if (from >= end) return 0;
+        return static_cast<int32_t>(c.reverse ? min(static_cast<int64_t>(steps), end - from) - (end - to)
+                                              : min(static_cast<int64_t>(steps), to) - from);
+    };
+    const float whole = exact_power(log_decay, a.each_steps);
+    float* s = c.states + head * a.segments * static_cast<int64_t>(c.size) + i;
+    float run = c.s_in ? c.s_in[head * c.size + i] : 0.0f;
+    for (int32_t w = 0; w < a.segments; w += U) {
+        float add[U];
 #pragma unroll
-    for (int b = 0; b < KD / 16; ++b)
+        for (int u = 0; u < U; ++u) add[u] = w + u < a.segments ? s[(w + u) * static_cast<int64_t>(c.size)] : 0.0f;
 #pragma unroll
-        for (int c = 0; c < CB; ++c)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + column(c, m);
-                if (i < kd && j < vd) pass.s_out[state + i * pass.at.row + j * pass.at.col] = S[b][c][r];
-            }
+        for (int u = 0; u < U; ++u) {
+            if (w + u >= a.segments) continue;
+            s[(w + u) * static_cast<int64_t>(c.size)] = run;
+            const int32_t count = steps_in(w + u);
+            if (count > 0) run = fmaf(count == a.each_steps ? whole : exact_power(log_decay, count), run, add[u]);
+        }
+    }
+    if (c.s_out) c.s_out[head * c.size + i] = run;
 }
 
 // Gradients of an input that heads share: the sum over them of their parts
@@ -565,45 +682,83 @@ HeadsIn heads_in(const wg_heads& t, int64_t heads, int64_t H) {
 }
 HeadsOut heads_out(const wg_heads& t) { return {const_cast<void*>(t.data), t.stride_n, t.stride_l, t.stride_h, 0}; }
 
-// launch(args with first set, workgroups).  HIP takes fewer than 2^32 threads: more
-// sequences than that go in several launches.
-hipError_t over_sequences(const Args& a, int passes, int dtype, void (*kernel)(Args), hipStream_t stream) {
-    int64_t per = 0;   // workgroups of a sequence
+// How a call is cut: the kernel's form and the segments of a sequence.
+struct Cut {
+    int kd, waves;            // channels of q and k and waves of a workgroup that the kernel is made for
+    int32_t segments, each;   // tiles of a segment
+};
+// Segments, where the heads do not fill the chip: as many as make kUnits workgroups, of
+// kLeast tiles at least.
+constexpr int64_t kFull = 192, kUnits = 512, kLeast = 4;
+constexpr int columns_of(int waves) { return 16 * waves; }
+int64_t blocks_of(int vd, int waves) { return (vd + columns_of(waves) - 1) / columns_of(waves); }
+Cut cut_of(int tile, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
+    int kd = 0, vd = 0;
+    for (int p = 0; p < passes; ++p) kd = std::max(kd, dims[p][0]), vd = std::max(vd, dims[p][1]);
+    Cut c{kd <= 32 ? 32 : kd <= 64 ? 64 : kd <= 128 ? 128 : 256, vd <= 64 ? 4 : 8, 1, 1};
+    int64_t units = 0;
+    for (int p = 0; p < passes; ++p) units += N * H * blocks_of(dims[p][1], c.waves);
+    const int64_t tiles = (L + tile - 1) / tile;
+    int64_t segments = 1;
+    if (units < kFull * passes && tiles >= 2 * kLeast) segments = std::min(tiles / kLeast, kUnits / units);
+    segments = std::max<int64_t>(1, segments);
+    c.each = static_cast<int32_t>(std::max<int64_t>(1, (tiles + segments - 1) / segments));
+    c.segments = static_cast<int32_t>(std::max<int64_t>(1, (tiles + c.each - 1) / c.each));
+    return c;
+}
+constexpr int tile_of(int dtype) { return dtype == kBF16 ? kTile<bf16_t> : kTile<float>; }
+
+// HIP takes fewer than 2^32 threads: more sequences than that go in several launches.
+hipError_t over_sequences(const Args& a, int passes, int dtype, int threads, void (*kernel)(Args), hipStream_t stream) {
+    int64_t per = 0;          // workgroups of a sequence
     for (int p = 0; p < passes; ++p) per += static_cast<int64_t>(a.H) * a.pass[p].blocks;
-    const int64_t most = std::max<int64_t>(1, 0xffffff / per);
+    const int64_t most = std::max<int64_t>(1, int64_t(0x7fffff) / per);
     for (int64_t n0 = 0; n0 < a.N; n0 += most) {
         Args k = a;
         k.N = std::min(a.N - n0, most);
         if (a.lengths) k.lengths = a.lengths + n0;
-        auto from = [&](auto& t, int es) { t.p = const_cast<char*>(static_cast<const char*>(t.p)) + n0 * t.sn * es; };
         k.first[0] = 0;
         for (int p = 0; p < passes; ++p) {
             Pass& s = k.pass[p];
-            for (HeadsIn* t : {&s.q, &s.k, &s.v}) from(*t, dtype_bytes(dtype));
-            from(s.y, s.y.f32 ? 4 : dtype_bytes(dtype));
-            const int64_t states = n0 * a.H * s.kd * s.vd;
+            const int es = dtype_bytes(dtype);
+            for (HeadsIn* t : {&s.q, &s.k, &s.v}) t->p = static_cast<const char*>(t->p) + n0 * t->sn * es;
+            s.y.p = static_cast<char*>(s.y.p) + n0 * s.y.sn * (s.y.f32 ? 4 : es);
+            const int64_t states = n0 * a.H * s.kd * s.vd;   // with segments all sequences go in one launch
             if (s.s_in) s.s_in += states;
             if (s.s_out) s.s_out += states;
             k.first[p + 1] = k.first[p] + static_cast<int32_t>(k.N * a.H * s.blocks);
         }
         for (int p = passes; p < 3; ++p) k.first[p + 1] = k.first[p];
-        kernel<<<static_cast<unsigned>(k.first[passes]), kThreads, 0, stream>>>(k);
+        kernel<<<static_cast<unsigned>(k.first[3]) * k.segments, threads, 0, stream>>>(k);
     }
     return hipGetLastError();
 }
 
-#define WG_ATTENTION_SHAPES(X) X(32, 1) X(32, 2) X(64, 1) X(64, 2) X(128, 1) X(128, 2) X(256, 1)
+#define WG_ATTENTION_SHAPES(X) X(32, 4) X(32, 8) X(64, 4) X(64, 8) X(128, 4) X(128, 8) X(256, 4) X(256, 8)
 
-template <typename Elem> hipError_t run_passes(Args& a, int passes, int dtype, hipStream_t stream) {
-    int kd = 0, vd = 0;
-    for (int p = 0; p < passes; ++p) kd = std::max(kd, a.pass[p].kd), vd = std::max(vd, a.pass[p].vd);
-    const int KD = kd <= 32 ? 32 : kd <= 64 ? 64 : kd <= 128 ? 128 : 256, CB = vd <= 64 || KD == 256 ? 1 : 2;
-    for (int p = 0; p < passes; ++p) a.pass[p].blocks = (a.pass[p].vd + 64 * CB - 1) / (64 * CB);
-#define WG_ATTENTION_CASE(K, C) \
-    if (KD == K && CB == C) return over_sequences(a, passes, dtype, attention_kernel<Elem, K, C>, stream);
+template <typename Elem, bool STATES> hipError_t run_passes(Args& a, int passes, const Cut& cut, int dtype, hipStream_t stream) {
+    for (int p = 0; p < passes; ++p) a.pass[p].blocks = static_cast<int32_t>(blocks_of(a.pass[p].vd, cut.waves));
+    a.segments = cut.segments, a.each = cut.each;
+#define WG_ATTENTION_CASE(K, W) \
+    if (cut.kd == K && cut.waves == W) return over_sequences(a, passes, dtype, 64 * W, attention_kernel<Elem, K, W, 1, STATES>, stream);
     WG_ATTENTION_SHAPES(WG_ATTENTION_CASE)
 #undef WG_ATTENTION_CASE
     return hipErrorInvalidValue;
+}
+
+// The states of `of` chains' segments: the pass that adds to each goes first.
+template <typename Elem>
+hipError_t run_chains(Args a, const Chain* chains, int of, const Cut& cut, int dtype, hipStream_t stream) {
+    for (int c = 0; c < of; ++c) a.pass[c].s_out = chains[c].states;
+    if (const hipError_t e = run_passes<Elem, true>(a, of, cut, dtype, stream)) return e;
+    ChainArgs k{};
+    int32_t size = 0;
+    for (int c = 0; c < of; ++c) k.chain[c] = chains[c], size = std::max(size, chains[c].size);
+    k.heads = a.N * a.H, k.L = a.L, k.H = a.H, k.segments = cut.segments;
+    k.tile = tile_of(dtype), k.each_steps = cut.each * k.tile, k.blocks = (size + kThreads - 1) / kThreads, k.of = of;
+    k.log_decay = a.log_decay, k.lengths = a.lengths;
+    chain_kernel<<<static_cast<unsigned>(k.heads * k.blocks * of), kThreads, 0, stream>>>(k);
+    return hipGetLastError();
 }
 
 // Bytes of the parts that an input's gradient is summed from: none where no heads share it.
@@ -611,37 +766,72 @@ size_t part_bytes(int64_t N, int64_t L, int64_t heads, int64_t H, int64_t D) {
     return heads == H ? 0 : static_cast<size_t>((N * L * H * D * 4 + 15) / 16 * 16);
 }
 
+// The passes' channels: of the attention itself, and of its gradients dq, dk and dv.
+struct Dims {
+    int forward[1][2], backward[3][2];
+    Dims(int64_t Dk, int64_t Dv) {
+        const int k = static_cast<int>(Dk), v = static_cast<int>(Dv);
+        forward[0][0] = backward[2][0] = backward[0][1] = backward[1][1] = k;
+        forward[0][1] = backward[2][1] = backward[0][0] = backward[1][0] = v;
+    }
+};
+size_t segment_bytes(const Cut& c, int64_t N, int64_t H, int64_t Dk, int64_t Dv) {
+    return c.segments == 1 ? 0 : static_cast<size_t>((N * H * c.segments * Dk * Dv * 4 + 15) / 16 * 16);
+}
+
 }  // namespace
 
 #if WG_DTYPE == 0
-size_t linear_attention_workspace(int, int64_t N, int64_t L, int64_t q_heads, int64_t k_heads, int64_t v_heads, int64_t H,
+size_t linear_attention_workspace(int dtype, int64_t N, int64_t L, int64_t q_heads, int64_t k_heads, int64_t v_heads, int64_t H,
                                   int64_t Dk, int64_t Dv, bool backward) {
-    if (!backward) return 0;
-    return part_bytes(N, L, q_heads, H, Dk) + part_bytes(N, L, k_heads, H, Dk) + part_bytes(N, L, v_heads, H, Dv);
+    const Dims dims(Dk, Dv);
+    if (!backward) return segment_bytes(cut_of(tile_of(dtype), N, L, H, dims.forward, 1), N, H, Dk, Dv);
+    return 2 * segment_bytes(cut_of(tile_of(dtype), N, L, H, dims.backward, 3), N, H, Dk, Dv) +
+           part_bytes(N, L, q_heads, H, Dk) + part_bytes(N, L, k_heads, H, Dk) + part_bytes(N, L, v_heads, H, Dv);
 }
 #endif
 
 template <int D> hipError_t launch_linear_attention_t(const wg_linear_attention& a, hipStream_t stream) {
     using Elem = typename DTypeOf<D>::type;
     const int32_t Dk = static_cast<int32_t>(a.Dk), Dv = static_cast<int32_t>(a.Dv);
+    const Dims dims(Dk, Dv);
+    const Cut cut = cut_of(tile_of(D), a.N, a.L, a.heads, dims.forward, 1);
     Args k{};
     k.N = a.N, k.L = static_cast<int32_t>(a.L), k.H = static_cast<int32_t>(a.heads);
     k.log_decay = a.log_decay, k.lengths = a.lengths, k.scale = static_cast<float>(a.scale);
     k.pass[0] = Pass{heads_in(a.q, a.q_heads, a.heads), heads_in(a.k, a.k_heads, a.heads), heads_in(a.v, a.v_heads, a.heads),
-                     heads_out(a.y), Dk, Dv, 0, a.s0, a.s_last, {Dv, 1}, 1.0f, k.scale, 0};
-    return run_passes<Elem>(k, 1, D, stream);
+                     heads_out(a.y), Dk, Dv, 0, a.s0, a.s_last, {Dv, 1}, 1.0f, k.scale, 0, 0};
+    if (cut.segments > 1) {
+        const Chain chain{static_cast<float*>(a.workspace), a.s0, a.s_last, Dk * Dv, 0};
+        if (const hipError_t e = run_chains<Elem>(k, &chain, 1, cut, D, stream)) return e;
+        k.pass[0].s_in = chain.states, k.pass[0].s_out = nullptr, k.pass[0].from_segments = 1;
+    }
+    return run_passes<Elem, false>(k, 1, cut, D, stream);
 }
 
 template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_attention_backward& a, hipStream_t stream) {
     using Elem = typename DTypeOf<D>::type;
     const int64_t H = a.heads;
     const int32_t Dk = static_cast<int32_t>(a.Dk), Dv = static_cast<int32_t>(a.Dv);
+    const Dims dims_of(Dk, Dv);
+    const Cut cut = cut_of(tile_of(D), a.N, a.L, H, dims_of.backward, 3);
     Args k{};
     k.N = a.N, k.L = static_cast<int32_t>(a.L), k.H = static_cast<int32_t>(H);
     k.log_decay = a.log_decay, k.lengths = a.lengths, k.scale = static_cast<float>(a.scale);
     const HeadsIn q = heads_in(a.q, a.q_heads, H), kk = heads_in(a.k, a.k_heads, H), v = heads_in(a.v, a.v_heads, H),
                   dy = heads_in(a.dy, H, H);
     char* ws = static_cast<char*>(a.workspace);
+    const float *s_in = a.s0, *g_in = a.ds_last;
+    if (cut.segments > 1) {
+        const size_t bytes = segment_bytes(cut, a.N, H, Dk, Dv);
+        const Chain chains[2] = {{reinterpret_cast<float*>(ws), a.s0, nullptr, Dk * Dv, 0},
+                                 {reinterpret_cast<float*>(ws + bytes), a.ds_last, a.ds0, Dk * Dv, 1}};
+        ws += 2 * bytes;
+        k.pass[0] = Pass{q, kk, v, {}, Dk, Dv, 0, nullptr, nullptr, {Dv, 1}, 1.0f, 1.0f, 0, 0};
+        k.pass[1] = Pass{kk, q, dy, {}, Dk, Dv, 0, nullptr, nullptr, {Dv, 1}, k.scale, 1.0f, 1, 0};
+        if (const hipError_t e = run_chains<Elem>(k, chains, 2, cut, D, stream)) return e;
+        s_in = chains[0].states, g_in = chains[1].states;
+    }
     HeadsOut out[3] = {heads_out(a.dq), heads_out(a.dk), heads_out(a.dv)};
     const int64_t heads[3] = {a.q_heads, a.k_heads, a.v_heads};
     const int32_t dims[3] = {Dk, Dk, Dv};
@@ -655,10 +845,11 @@ template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_a
         if (!parts[p]) return out[p];
         return HeadsOut{const_cast<float*>(parts[p]), a.L * H * dims[p], H * dims[p], dims[p], 1};
     };
-    k.pass[0] = Pass{dy, v, kk, to(0), Dv, Dk, 0, a.s0, nullptr, {1, Dv}, 1.0f, k.scale, 0};
-    k.pass[1] = Pass{v, dy, q, to(1), Dv, Dk, 0, a.ds_last, nullptr, {1, Dv}, k.scale, 1.0f, 1};
-    k.pass[2] = Pass{kk, q, dy, to(2), Dk, Dv, 0, a.ds_last, a.ds0, {Dv, 1}, k.scale, 1.0f, 1};
-    if (const hipError_t e = run_passes<Elem>(k, 3, D, stream)) return e;
+    const int32_t segmented = cut.segments > 1;
+    k.pass[0] = Pass{dy, v, kk, to(0), Dv, Dk, 0, s_in, nullptr, {1, Dv}, 1.0f, k.scale, 0, segmented};
+    k.pass[1] = Pass{v, dy, q, to(1), Dv, Dk, 0, g_in, nullptr, {1, Dv}, k.scale, 1.0f, 1, segmented};
+    k.pass[2] = Pass{kk, q, dy, to(2), Dk, Dv, 0, g_in, segmented ? nullptr : a.ds0, {Dv, 1}, k.scale, 1.0f, 1, segmented};
+    if (const hipError_t e = run_passes<Elem, false>(k, 3, cut, D, stream)) return e;
     for (int p = 0; p < 3; ++p) {
         const int64_t all = a.N * a.L * heads[p] * dims[p];
         if (!parts[p] || all == 0) continue;
