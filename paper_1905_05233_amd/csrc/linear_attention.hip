@@ -44,6 +44,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;   // of the kernels beside the attention itself
+constexpr size_t kLdsBytes = 160 * 1024;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // bf16 parts of an input, of the values computed in fp32 that outputs are made of, and
@@ -121,18 +122,23 @@ template <int P, int V, bool FINITE> struct Split {
     typedef __bf16 Run __attribute__((ext_vector_type(V)));
     Run part[P];
     __device__ __forceinline__ void of(const float (&x)[V]) {
-        float left[V];
+        typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+        typedef uint32_t Words __attribute__((ext_vector_type(V / 2)));
 #pragma unroll
-        for (int e = 0; e < V; ++e) left[e] = x[e];
+        for (int e = 0; e < V; e += 2) {
+            float a = x[e], b = x[e + 1];
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) part[p][e] = static_cast<__bf16>(left[e]);
-            if (p + 1 < P) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    left[e] -= static_cast<float>(part[p][e]);
-                    if (FINITE) left[e] = __builtin_amdgcn_fmed3f(left[e], -0x1p120f, 0x1p120f);
+            for (int p = 0; p < P; ++p) {
+                const uint32_t w = __builtin_bit_cast(uint32_t, Pair{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+                Words words = __builtin_bit_cast(Words, part[p]);
+                words[e / 2] = w;
+                part[p] = __builtin_bit_cast(Run, words);
+                if (p + 1 == P) continue;
+                a -= __uint_as_float(w << 16);
+                b -= __uint_as_float(w & 0xffff0000u);
+                if (FINITE) {
+                    a = __builtin_amdgcn_fmed3f(a, -0x1p120f, 0x1p120f);
+                    b = __builtin_amdgcn_fmed3f(b, -0x1p120f, 0x1p120f);
                 }
             }
         }
@@ -150,17 +156,23 @@ __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[PA], const bf16x8 (&
     return c;
 }
 
-// Rows of a tile in LDS, one plane a part; 16 bytes between rows keep the 16 rows that
-// a fragment reads on different banks.
-template <int PLANES, int ROWS, int WIDTH> struct TileLds {
-    static constexpr int kStride = WIDTH + 8;
-    uint16_t v[PLANES][ROWS][kStride];
+// Rows of a tile in LDS, one plane a part, in runs of 8 channels whose order changes from
+// row to row: the 16 rows that a fragment reads the same run of, and the four rows and
+// runs that a transposing read takes, fall on different banks.
+template <int PLANES, int ROWS, int WIDTH> struct alignas(16) TileLds {
+    static constexpr int kRuns = WIDTH / 8;
+    uint16_t v[PLANES][ROWS][WIDTH];
 
+    static __device__ __forceinline__ int at(int row, int c) {
+        const int by4 = row >> 2 & 3;
+        const int mix = kRuns >= 16 ? (row & 3) << 2 | by4 : kRuns == 8 ? (row & 2) << 1 | by4 : by4;
+        return (c / 8 ^ mix) * 8 + c % 8;
+    }
     // 8 channels from c of a row, as a matrix instruction takes them of its row (or
     // column) `row`: lane m + 16 g holds 8 g .. 8 g + 7 of row m
     __device__ __forceinline__ void across(int row, int c, bf16x8 (&f)[PLANES]) const {
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p) f[p] = *reinterpret_cast<const bf16x8*>(&v[p][row][c]);
+        for (int p = 0; p < PLANES; ++p) f[p] = *reinterpret_cast<const bf16x8*>(&v[p][row][at(row, c)]);
     }
     // 8 rows from `row` of a channel: the lanes of 16 hand in the places of four
     // channels in each of four rows, and lane m gets the four rows of channel m
@@ -168,57 +180,85 @@ template <int PLANES, int ROWS, int WIDTH> struct TileLds {
         using At = __attribute__((address_space(3))) s16x4*;
 #pragma unroll
         for (int p = 0; p < PLANES; ++p) {
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row][c]));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row + 4][c]));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row][at(row, c)]));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row + 4][at(row + 4, c)]));
             f[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
 };
 
-// A tile's rows on their way from memory: 16 bytes of U rows a thread.
+// A tile's rows on their way from memory: 16 bytes of U rows a thread.  Every thread
+// loads, from the first row and from the end of its row's channels where it has none of
+// its own; what it then holds too many is dropped on the way to LDS.
 template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
     static constexpr int V = Vec<Elem>::V, kRuns = WIDTH / V, kPer = THREADS / kRuns, U = (ROWS + kPer - 1) / kPer;
     static_assert(THREADS % kRuns == 0 && (ROWS % kPer == 0 || U == 1), "threads cover whole rows");
     u32x4 raw[U];
+    const Elem* base;   // the thread's channels of the sequence's first row
+    int64_t stride, own;
+    int r0, over;       // its first row; channels too many
 
-    // rows 0 .. live - 1 from p, `stride` apart; channels c0 .. of D; zeros elsewhere
-    __device__ __forceinline__ void load(const Elem* p, int64_t stride, int live, int c0, int D) {
-        const int c = c0 + static_cast<int>(threadIdx.x) % kRuns * V, r0 = threadIdx.x / kRuns;
-        const Elem* at = p + r0 * stride + c;
-        if (live == ROWS && ROWS % kPer == 0 && D - c0 >= WIDTH) {
+    __device__ __forceinline__ TileLoad(const Elem* p, int64_t row_stride, int c0, int D) {
+        const int c = c0 + static_cast<int>(threadIdx.x) % kRuns * V;
+        r0 = threadIdx.x / kRuns;
+        over = max(0, c + V - D);
+        stride = row_stride;
+        own = r0 * stride;
+        base = p + (D >= V ? c - over : 0);
+    }
+    // rows 0 .. live - 1 (at least one) from row t0 of the sequence
+    __device__ __forceinline__ void load(int32_t t0, int live, int D) {
+        const Elem* p = base + t0 * stride;
+        if (D >= V) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = reinterpret_cast<const Bytes16*>(at + u * kPer * stride)->v;
+            for (int u = 0; u < U; ++u)
+                raw[u] = reinterpret_cast<const Bytes16*>(r0 + u * kPer < live ? p + own + u * kPer * stride : p)->v;
             return;
         }
-        const int over = c + V - D;   // a short run is the end of 16 bytes that end with the row
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < U; ++u) {   // rows shorter than 16 bytes, in pieces of 8, 4 and 2
             raw[u] = u32x4{0, 0, 0, 0};
             if (r0 + u * kPer >= live || over >= V) continue;
-            const Elem* run = at + u * kPer * stride;
-            if (D >= V) {
-                raw[u] = reinterpret_cast<const Bytes16*>(run - max(0, over))->v;
-            } else {
-                typename Vec<Elem>::Packed e{};
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (j < V - over) e.v[j] = run[j];
-                raw[u] = __builtin_bit_cast(u32x4, e);
+            const Elem* at = p + own + u * kPer * stride;
+            constexpr int kPer8 = 8 / sizeof(Elem);
+            uint64_t head = 0, tail = 0;
+            if (D & kPer8) {
+                __builtin_memcpy(&head, at, 8);
+                at += kPer8;
             }
+            if (sizeof(Elem) == 4 ? D & 1 : D & 2) {
+                uint32_t w;
+                __builtin_memcpy(&w, at, 4);
+                at += 4 / sizeof(Elem);
+                tail = w;
+            }
+            if (sizeof(Elem) == 2 && D & 1) {
+                uint16_t w;
+                __builtin_memcpy(&w, at, 2);
+                tail |= static_cast<uint64_t>(w) << (D & 2 ? 32 : 0);
+            }
+            if (!(D & kPer8)) head = tail, tail = 0;
+            raw[u] = u32x4{static_cast<uint32_t>(head), static_cast<uint32_t>(head >> 32), static_cast<uint32_t>(tail),
+                           static_cast<uint32_t>(tail >> 32)};
         }
-        if (over > 0 && D >= V) {
+    }
+    // what is loaded without what it holds too many; `whole`: that is nothing, for all threads
+    __device__ __forceinline__ void trim(bool whole, int live, int D) {
+        if (whole || D < V) return;
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = drop_first<Elem>(raw[u], over);
+        for (int u = 0; u < U; ++u) {
+            raw[u] = drop_first<Elem>(raw[u], over);
+            if (r0 + u * kPer >= live) raw[u] = u32x4{0, 0, 0, 0};
         }
     }
     template <int PLANES> __device__ __forceinline__ void store(TileLds<PLANES, ROWS, WIDTH>& to) const {
-        const int c = static_cast<int>(threadIdx.x) % kRuns * V, r0 = threadIdx.x / kRuns;
+        const int c = static_cast<int>(threadIdx.x) % kRuns * V;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int row = r0 + u * kPer;
             if (ROWS % kPer != 0 && row >= ROWS) continue;
             if constexpr (PLANES == 1) {
-                *reinterpret_cast<u32x4*>(&to.v[0][row][c]) = raw[u];
+                *reinterpret_cast<u32x4*>(&to.v[0][row][to.at(row, c)]) = raw[u];
             } else {
                 float x[V];
                 Vec<Elem>::widen(raw[u], x);
@@ -226,7 +266,7 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
                 s.of(x);
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p)
-                    *reinterpret_cast<typename Split<PLANES, V, true>::Run*>(&to.v[p][row][c]) = s.part[p];
+                    *reinterpret_cast<typename Split<PLANES, V, true>::Run*>(&to.v[p][row][to.at(row, c)]) = s.part[p];
             }
         }
     }
@@ -256,36 +296,45 @@ template <typename Elem> __device__ __forceinline__ const Elem* heads_at(const H
     return static_cast<const Elem*>(t.p) + n * t.sn + h / t.per * t.sh;
 }
 
-// 4 CB values side by side, of which those below `valid` are wanted
-template <typename T, int COUNT> __device__ __forceinline__ void store_values(T* to, const float (&x)[COUNT], int valid) {
-    struct __attribute__((packed, aligned(sizeof(T)))) Values {
-        T v[COUNT];
+// Four values side by side, of which those below `valid` are wanted.
+template <typename T> __device__ __forceinline__ void store_values(T* to, const f32x4& x, int valid) {
+    struct __attribute__((packed, aligned(sizeof(T)))) Two {
+        T v[2];
     };
-    if (valid >= COUNT) {
-        Values w;
+    struct __attribute__((packed, aligned(sizeof(T)))) Four {
+        T v[4];
+    };
+    T e[4];
 #pragma unroll
-        for (int e = 0; e < COUNT; ++e) w.v[e] = Storage<T>::from_f32(x[e]);
-        *reinterpret_cast<Values*>(to) = w;
-        return;
+    for (int r = 0; r < 4; ++r) e[r] = Storage<T>::from_f32(x[r]);
+    if (valid >= 4) *reinterpret_cast<Four*>(to) = Four{e[0], e[1], e[2], e[3]};
+    else {
+        if (valid >= 2) *reinterpret_cast<Two*>(to) = Two{e[0], e[1]};
+        if (valid == 1) to[0] = e[0];
+        if (valid == 3) to[2] = e[2];
     }
-#pragma unroll
-    for (int e = 0; e < COUNT; ++e)
-        if (e < valid) to[e] = Storage<T>::from_f32(x[e]);
 }
 
+struct None {};
+
 // Tiles of K channels of q and k for W waves of 16 C columns each.
-template <typename Elem, int K, int W, int C> struct Shape {
+template <typename Elem, int K, int W, int C, bool STATES> struct Shape {
     static constexpr int T = kTile<Elem>, PI = kParts<Elem>, PS = kSums<Elem>;
     static constexpr int kColumns = 16 * C * W, kThreads = 64 * W;
-    struct Lds {
-        TileLds<PI, T, K> q, k;
-        TileLds<PI, T, kColumns> v;
-        TileLds<PS, T, T> p;
-        int32_t odd;   // the tile (+ 1) of which v holds an infinity or NaN
-    };
-    struct StatesLds {
+    struct Steps {
+        std::conditional_t<STATES, None, TileLds<PI, T, K>> q;
         TileLds<PI, T, K> k;
         TileLds<PI, T, kColumns> v;
+    };
+    struct Weights {
+        TileLds<PS, T, T> p;
+        int32_t odd[2];   // the tile (+ 1) of which v holds an infinity or NaN
+    };
+    // two tiles of steps, where they find room
+    static constexpr int kStages = 2 * sizeof(Steps) + sizeof(Weights) <= kLdsBytes ? 2 : 1;
+    struct Lds {
+        Steps steps[kStages];
+        std::conditional_t<STATES, None, Weights> weights;
     };
 };
 
@@ -296,10 +345,11 @@ template <typename Elem, int K, int W, int C> struct Shape {
 // move.  Outputs come transposed, O[i][c] with row 16 i + m and columns
 // column(c, 4 g + r): 4 C of them side by side.
 template <typename Elem, int KD, int W, int CB, bool STATES>
-__global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void attention_kernel(Args a) {
-    using Sh = Shape<Elem, KD, W, CB>;
+__global__ __launch_bounds__(64 * W, 2) void attention_kernel(Args a) {
+    using Sh = Shape<Elem, KD, W, CB, STATES>;
     constexpr int T = Sh::T, PI = Sh::PI, PS = Sh::PS, VB = Sh::kColumns, NT = Sh::kThreads, IB = T / 16, JS = T / 32, KS = KD / 32;
-    __shared__ __align__(16) std::conditional_t<STATES, typename Sh::StatesLds, typename Sh::Lds> lds;
+    constexpr int STAGES = Sh::kStages;
+    __shared__ __align__(16) typename Sh::Lds lds;
     const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, m = lane % 16, g = lane / 16;
 
     const int32_t segment = blockIdx.x / static_cast<uint32_t>(a.first[3]);
@@ -311,7 +361,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void attention_kernel(Args 
     const int32_t block = unit - head * pass.blocks, h = head % static_cast<uint32_t>(a.H);
     const int64_t n = head / static_cast<uint32_t>(a.H);
     const int32_t steps = steps_of(a.lengths, n, a.L), kd = pass.kd, vd = pass.vd, v0 = block * VB;
-    const bool reverse = pass.reverse != 0;
+    const bool reverse = pass.reverse != 0, y_f32 = pass.y.f32 != 0;
     const float log_decay = a.log_decay[h], log2_decay = log2_of(log_decay);
     const float in_scale = pass.in_scale, out_scale = pass.out_scale, scale = a.scale;
 
@@ -342,191 +392,229 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void attention_kernel(Args 
         each_state([&](float, int at) { return s[at]; });
     }
 
-    const int32_t tiles = (steps + T - 1) / T, t_end = min(tiles, (segment + 1) * a.each);
-    int32_t t = segment * a.each;
-    const int64_t q_sl = pass.q.sl, k_sl = pass.k.sl, v_sl = pass.v.sl, y_sl = pass.y.sl;
+    const int32_t tiles = (steps + T - 1) / T, t_first = segment * a.each, t_end = min(tiles, t_first + a.each);
+    const int64_t y_sl = pass.y.sl;
     const Elem* q = heads_at<Elem>(pass.q, n, h);
     const Elem* k = heads_at<Elem>(pass.k, n, h);
     const Elem* v = heads_at<Elem>(pass.v, n, h);
-    TileLoad<Elem, T, KD, NT> lq, lk;
-    TileLoad<Elem, T, VB, NT> lv;
-    auto first_of = [&](int32_t t) { return (reverse ? tiles - 1 - t : t) * T; };
-    auto load = [&](int32_t t) {
-        const int32_t t0 = first_of(t), live = min(T, steps - t0);
-        if (!STATES) lq.load(q + t0 * q_sl, q_sl, live, 0, kd);
-        lk.load(k + t0 * k_sl, k_sl, live, 0, kd);
-        lv.load(v + t0 * v_sl, v_sl, live, v0, vd);
-    };
-    if (t < t_end) load(t);
+    // a lane's outputs: 4 CB values side by side in row m of every 16
+    const int y_valid = vd - (v0 + column(0, 4 * g));
+    const int64_t y_at = n * pass.y.sn + h * pass.y.sh + m * y_sl + v0 + column(0, 4 * g);
+    TileLoad<Elem, T, KD, NT> lq(q, pass.q.sl, 0, kd), lk(k, pass.k.sl, 0, kd);
+    TileLoad<Elem, T, VB, NT> lv(v, pass.v.sl, v0, vd);
+    const bool wide = kd == KD && vd - v0 >= VB;
     if constexpr (!STATES) {
         // weights above the diagonal are zeros that nothing writes
-        for (int i = tid; i < static_cast<int>(sizeof(lds.p) / 4); i += NT) reinterpret_cast<uint32_t*>(&lds.p)[i] = 0;
-        if (tid == 0) lds.odd = 0;
-        __syncthreads();
+        for (int i = tid; i < static_cast<int>(sizeof(lds.weights) / 4); i += NT) reinterpret_cast<uint32_t*>(&lds.weights)[i] = 0;
     }
 
-    // decays of a whole tile; the last one may be short
-    const float whole = exact_power(log_decay, T);
-    for (; t < t_end; ++t) {
-        const int32_t t0 = first_of(t), live = min(T, steps - t0);
-        if constexpr (!STATES) lq.template store<PI>(lds.q);
-        lk.template store<PI>(lds.k);
-        lv.template store<PI>(lds.v);
-        if constexpr (!STATES)
-            if (!lv.finite()) lds.odd = t + 1;
-        if (t + 1 < t_end) load(t + 1);
-        __syncthreads();
+    // decays: over a tile, from the state to its steps, from its steps to the state
+    float whole = 1.0f, out_decay[IB], in_decay[JS][8];
+    int decays_of = 0;
+    auto set_decays = [&](int live) {
+        decays_of = live;
+        whole = exact_power(log_decay, live);
+#pragma unroll
+        for (int i = 0; i < IB; ++i)
+            out_decay[i] = out_scale * power(log2_decay, reverse ? max(0, live - 1 - (16 * i + m)) : 16 * i + m + 1);
+#pragma unroll
+        for (int s = 0; s < JS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = 32 * s + 8 * g + e;
+                in_decay[s][e] = in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j));
+            }
+    };
 
+    // The first state is there ahead of the rounds: each of them would wait for it, and
+    // for its own loads with it.
+#pragma unroll
+    for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) asm volatile("" : "+v"(S[b][c]));
+    // a round multiplies tile t, and has tile t + 1 loaded and brought to LDS
+    for (int32_t t = t_first - 1; t < t_end; ++t) {
+        const int32_t next0 = (reverse ? tiles - 2 - t : t + 1) * T, t0 = reverse ? next0 + T : next0 - T;
+        const bool more = t + 1 < t_end, has = t >= t_first;
+        auto& now = lds.steps[t & (STAGES - 1)];
+        auto& next = lds.steps[(t + 1) & (STAGES - 1)];
+        if (more) {
+            const int32_t live = min(T, steps - next0);
+            if constexpr (!STATES) lq.load(next0, live, kd);
+            lk.load(next0, live, kd);
+            lv.load(next0, live, vd);
+        }
+        const int32_t live = min(T, steps - t0);
         f32x4 O[IB][CB];
-        if constexpr (!STATES) {
-            // the weights of the tile, in blocks of 16 x 16 of the triangle
-            for (int blk = wave; blk < IB * (IB + 1) / 2; blk += W) {
-                const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
-                const int ib = reverse ? near : far, jb = reverse ? far : near;
-                f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    bf16x8 fk[PI], fq[PI];
-                    lds.k.across(16 * jb + m, 32 * s + 8 * g, fk);
-                    lds.q.across(16 * ib + m, 32 * s + 8 * g, fq);
-                    w = multiply<PI, PI, PS>(fk, fq, w);
-                }
-                float x[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * ib + m, j = 16 * jb + 4 * g + r, d = reverse ? j - i : i - j;
-                    x[r] = d < 0 ? 0.0f : w[r] * (scale * power(log2_decay, d));
-                }
-                Split<PS, 4, false> parts;
-                parts.of(x);
-#pragma unroll
-                for (int p = 0; p < PS; ++p)
-                    *reinterpret_cast<bf16x4*>(&lds.p.v[p][16 * ib + m][16 * jb + 4 * g]) = parts.part[p];
-            }
-
-            // what the state gives
-#pragma unroll
-            for (int i = 0; i < IB; ++i)
-#pragma unroll
-                for (int c = 0; c < CB; ++c) O[i][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                Split<PS, 8, false> fs[CB];
-#pragma unroll
-                for (int c = 0; c < CB; ++c) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][c][e % 4];
-                    fs[c].of(x);
-                }
-#pragma unroll
-                for (int i = 0; i < IB; ++i) {
-                    bf16x8 fq[PI];
-                    lds.q.across(16 * i + m, 32 * s + 8 * g, fq);
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) O[i][c] = multiply<PS, PI, PS>(fs[c].part, fq, O[i][c]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < IB; ++i) {
-                const int row = 16 * i + m;
-                const float f = out_scale * power(log2_decay, reverse ? max(0, live - 1 - row) : row + 1);
-#pragma unroll
-                for (int c = 0; c < CB; ++c) O[i][c] *= f;
-            }
-        }
-
-        // the state behind the tile
-        const float decay = live == T ? whole : exact_power(log_decay, live);
-#pragma unroll
-        for (int b = 0; b < KD / 16; ++b)
-#pragma unroll
-            for (int c = 0; c < CB; ++c) S[b][c] *= decay;
         bf16x8 fv[JS][CB][PI];
+        if (has) {
+            if (live != decays_of) set_decays(live);
+            if constexpr (!STATES) {
+                // the weights of the tile, in blocks of 16 x 16 of the triangle
+                for (int blk = wave; blk < IB * (IB + 1) / 2; blk += W) {
+                    const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
+                    const int ib = reverse ? near : far, jb = reverse ? far : near;
+                    f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int s = 0; s < JS; ++s) {
-            Split<kStateParts, 8, false> late[CB];
+                    for (int s = 0; s < KS; ++s) {
+                        bf16x8 fk[PI], fq[PI];
+                        now.k.across(16 * jb + m, 32 * s + 8 * g, fk);
+                        now.q.across(16 * ib + m, 32 * s + 8 * g, fq);
+                        w = multiply<PI, PI, PS>(fk, fq, w);
+                    }
+                    float x[4];
 #pragma unroll
-            for (int c = 0; c < CB; ++c) {
-                lds.v.down(32 * s + 8 * g + m / 4, column_chunk(c), fv[s][c]);
-                float x[8];
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = 16 * ib + m, j = 16 * jb + 4 * g + r, d = reverse ? j - i : i - j;
+                        x[r] = d < 0 ? 0.0f : w[r] * (scale * power(log2_decay, d));
+                    }
+                    Split<PS, 4, false> parts;
+                    parts.of(x);
+                    auto& to = lds.weights.p;
+                    const int row = 16 * ib + m, c = 16 * jb + 4 * g;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int j = 32 * s + 8 * g + e;
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int p = PI - 1; p >= 0; --p) sum += static_cast<float>(fv[s][c][p][e]);
-                    x[e] = sum * (in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j)));
+                    for (int p = 0; p < PS; ++p) *reinterpret_cast<bf16x4*>(&to.v[p][row][to.at(row, c)]) = parts.part[p];
                 }
-                late[c].of(x);
-            }
-#pragma unroll
-            for (int b = 0; b < KD / 16; ++b) {
-                bf16x8 fk[PI];
-                lds.k.down(32 * s + 8 * g + m / 4, row_chunk(b), fk);
-#pragma unroll
-                for (int c = 0; c < CB; ++c) S[b][c] = multiply<PI, kStateParts, kStateParts>(fk, late[c].part, S[b][c]);
-            }
-        }
-        __syncthreads();
-        if constexpr (STATES) continue;
 
-        if constexpr (!STATES) {
-            // what the tile's own steps give
-            if (lds.odd != t + 1) {
+                // what the state gives
 #pragma unroll
                 for (int i = 0; i < IB; ++i)
 #pragma unroll
-                    for (int s = 0; s < JS; ++s) {
-                        if (reverse ? 32 * s + 31 < 16 * i : 32 * s > 16 * i + 15) continue;
-                        bf16x8 fp[PS];
-                        lds.p.across(16 * i + m, 32 * s + 8 * g, fp);
+                    for (int c = 0; c < CB; ++c) O[i][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int c = 0; c < CB; ++c) O[i][c] = multiply<PI, PS, PS>(fv[s][c], fp, O[i][c]);
+                for (int s = 0; s < KS; ++s) {
+                    Split<PS, 8, false> fs[CB];
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][c][e % 4];
+                        fs[c].of(x);
                     }
-            } else {
-                // step by step: a weight of zero would not remove an infinity or NaN of a later v
+#pragma unroll
+                    for (int i = 0; i < IB; ++i) {
+                        bf16x8 fq[PI];
+                        now.q.across(16 * i + m, 32 * s + 8 * g, fq);
+#pragma unroll
+                        for (int c = 0; c < CB; ++c) O[i][c] = multiply<PS, PI, PS>(fs[c].part, fq, O[i][c]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < IB; ++i)
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) O[i][c] *= out_decay[i];
+            }
+
+            // the state behind the tile
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+                for (int c = 0; c < CB; ++c) S[b][c] *= whole;
+#pragma unroll
+            for (int s = 0; s < JS; ++s) {
+                Split<kStateParts, 8, false> late[CB];
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    now.v.down(32 * s + 8 * g + m / 4, column_chunk(c), fv[s][c]);
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int p = PI - 1; p >= 0; --p) sum += static_cast<float>(fv[s][c][p][e]);
+                        x[e] = sum * in_decay[s][e];
+                    }
+                    late[c].of(x);
+                }
+#pragma unroll
+                for (int b = 0; b < KD / 16; ++b) {
+                    bf16x8 fk[PI];
+                    now.k.down(32 * s + 8 * g + m / 4, row_chunk(b), fk);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) S[b][c] = multiply<PI, kStateParts, kStateParts>(fk, late[c].part, S[b][c]);
+                }
+            }
+        }
+        // The next tile's rows go to LDS ahead of this one's outputs: the wait for them
+        // is for every access to memory before it, stores too.
+        auto stage = [&] {
+            if (!more) return;
+            const int32_t live = min(T, steps - next0);
+            const bool whole_tile = wide && live == T;
+            lk.trim(whole_tile, live, kd);
+            lv.trim(whole_tile, live, vd);
+            if constexpr (!STATES) {
+                lq.trim(whole_tile, live, kd);
+                lq.template store<PI>(next.q);
+                if (!lv.finite()) lds.weights.odd[(t + 1) & 1] = t + 2;
+            }
+            lk.template store<PI>(next.k);
+            lv.template store<PI>(next.v);
+        };
+        if constexpr (!STATES) __syncthreads();   // the weights
+        if constexpr (STAGES == 2) stage();
+        if constexpr (!STATES) {
+            if (has) {
+                // what the tile's own steps give
+                if (lds.weights.odd[t & 1] != t + 1) {
+#pragma unroll
+                    for (int i = 0; i < IB; ++i)
+#pragma unroll
+                        for (int s = 0; s < JS; ++s) {
+                            if (reverse ? 32 * s + 31 < 16 * i : 32 * s > 16 * i + 15) continue;
+                            bf16x8 fp[PS];
+                            lds.weights.p.across(16 * i + m, 32 * s + 8 * g, fp);
+#pragma unroll
+                            for (int c = 0; c < CB; ++c) O[i][c] = multiply<PI, PS, PS>(fv[s][c], fp, O[i][c]);
+                        }
+                } else {
+                    // step by step: a weight of zero would not remove an infinity or NaN of a later v
+                    auto value = [](const auto& tile, int row, int c) {
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int p = std::extent_v<std::remove_reference_t<decltype(tile.v)>> - 1; p >= 0; --p)
+                            sum += __uint_as_float(static_cast<uint32_t>(tile.v[p][row][tile.at(row, c)]) << 16);
+                        return sum;
+                    };
+#pragma unroll 1
+                    for (int j = 0; j < T; ++j)
+#pragma unroll
+                        for (int i = 0; i < IB; ++i) {
+                            const int row = 16 * i + m;
+                            if (reverse ? j < row : j > row) continue;
+                            const float w = value(lds.weights.p, row, j);
+#pragma unroll
+                            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) O[i][c][r] += w * value(now.v, j, column(c, 4 * g + r));
+                        }
+                }
+            }
+        }
+        if constexpr (STAGES == 1) {
+            __syncthreads();
+            stage();
+        }
+        if constexpr (!STATES) {
+            if (has && y_valid > 0) {
 #pragma unroll
                 for (int i = 0; i < IB; ++i) {
-                    const int row = 16 * i + m;
-                    for (int j = reverse ? row : 0; j < (reverse ? T : row + 1); ++j) {
-                        float w = 0.0f;
+                    if (16 * i + m >= live) continue;
+                    const int64_t at = y_at + (t0 + 16 * i) * y_sl;
 #pragma unroll
-                        for (int p = PS - 1; p >= 0; --p) w += __uint_as_float(static_cast<uint32_t>(lds.p.v[p][row][j]) << 16);
-#pragma unroll
-                        for (int c = 0; c < CB; ++c)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                float x = 0.0f;
-#pragma unroll
-                                for (int p = PI - 1; p >= 0; --p)
-                                    x += __uint_as_float(static_cast<uint32_t>(lds.v.v[p][j][column(c, 4 * g + r)]) << 16);
-                                O[i][c][r] += w * x;
-                            }
+                    for (int c = 0; c < CB; ++c) {
+                        if (y_f32) store_values<float>(static_cast<float*>(pass.y.p) + at + 4 * c, O[i][c], y_valid - 4 * c);
+                        else store_values<Elem>(static_cast<Elem*>(pass.y.p) + at + 4 * c, O[i][c], y_valid - 4 * c);
                     }
                 }
             }
-#pragma unroll
-            for (int i = 0; i < IB; ++i) {
-                const int row = 16 * i + m, j = v0 + column(0, 4 * g);
-                if (row >= live || j >= vd) continue;
-                const int64_t at = n * pass.y.sn + (t0 + row) * y_sl + h * pass.y.sh + j;
-                float x[4 * CB];
-#pragma unroll
-                for (int c = 0; c < CB; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[4 * c + r] = O[i][c][r];
-                if (pass.y.f32) store_values<float>(static_cast<float*>(pass.y.p) + at, x, vd - j);
-                else store_values<Elem>(static_cast<Elem*>(pass.y.p) + at, x, vd - j);
-            }
-            __syncthreads();
         }
+        __syncthreads();
     }
 
     if constexpr (STATES) {
         float* s = pass.s_out + by_segment;
         each_state([&](float x, int at) { return s[at] = x; });
-        return;
     } else {
         // padding, of which each segment takes a share of rows
         const int width = min(VB, vd - v0), share = (a.L - steps + a.segments - 1) / a.segments;
@@ -534,7 +622,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void attention_kernel(Args 
         const int64_t values = static_cast<int64_t>(min(share, a.L - row0)) * width;
         for (int64_t i = tid; i < values; i += NT) {
             const int64_t at = n * pass.y.sn + (row0 + i / width) * y_sl + h * pass.y.sh + v0 + i % width;
-            if (pass.y.f32) static_cast<float*>(pass.y.p)[at] = 0.0f;
+            if (y_f32) static_cast<float*>(pass.y.p)[at] = 0.0f;
             else static_cast<Elem*>(pass.y.p)[at] = Storage<Elem>::from_f32(0.0f);
         }
         if (!pass.s_out) return;
