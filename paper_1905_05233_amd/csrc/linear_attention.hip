@@ -52,8 +52,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 template <typename Elem> constexpr int kParts = std::is_same_v<Elem, bf16_t> ? 1 : std::is_same_v<Elem, _Float16> ? 2 : 3;
 template <typename Elem> constexpr int kSums = std::is_same_v<Elem, float> ? 3 : 2;
 constexpr int kStateParts = 3;
-// steps of a tile
-template <typename Elem> constexpr int kTile = std::is_same_v<Elem, bf16_t> ? 64 : 32;
+// Steps of a tile: as many as find room in LDS twice.
+constexpr int tile_steps(bool bf16, int kd) { return bf16 && kd <= 128 ? 64 : 32; }
 
 // Heads of one tensor: [N][L][H][D] with the channels contiguous; `per` of the
 // attention's heads read each.
@@ -145,15 +145,19 @@ template <int P, int V, bool FINITE> struct Split {
     }
 };
 
-// c += a b over the parts whose product is not below the last of P
-template <int PA, int PB, int P>
-__device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[PA], const bf16x8 (&b)[PB], f32x4 c) {
+// c[i] += a[i] b[i] over the parts whose product is not below the last of P.  The
+// accumulators take turns: a matrix instruction waits for the one ahead of it on its own.
+// A and B: part p of operand i.
+template <int PA, int PB, int P, int COUNT, typename A, typename B>
+__device__ __forceinline__ void multiply(A&& a, B&& b, f32x4 (&c)[COUNT]) {
 #pragma unroll
-    for (int i = 0; i < PA; ++i)
+    for (int p = 0; p < PA; ++p)
 #pragma unroll
-        for (int j = 0; j < PB; ++j)
-            if (i + j < P) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
-    return c;
+        for (int r = 0; r < PB; ++r)
+            if (p + r < P) {
+#pragma unroll
+                for (int i = 0; i < COUNT; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a(i, p), b(i, r), c[i], 0, 0, 0);
+            }
 }
 
 // Rows of a tile in LDS, one plane a part, in runs of 8 channels whose order changes from
@@ -196,11 +200,12 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
     u32x4 raw[U];
     const Elem* base;   // the thread's channels of the sequence's first row
     int64_t stride, own;
-    int r0, over;       // its first row; channels too many
+    int run, r0, over;  // its place in a row, its first row; channels too many
 
-    __device__ __forceinline__ TileLoad(const Elem* p, int64_t row_stride, int c0, int D) {
-        const int c = c0 + static_cast<int>(threadIdx.x) % kRuns * V;
-        r0 = threadIdx.x / kRuns;
+    __device__ __forceinline__ TileLoad(int thread, const Elem* p, int64_t row_stride, int c0, int D) {
+        run = thread % kRuns * V;
+        const int c = c0 + run;
+        r0 = thread / kRuns;
         over = max(0, c + V - D);
         stride = row_stride;
         own = r0 * stride;
@@ -252,13 +257,12 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
         }
     }
     template <int PLANES> __device__ __forceinline__ void store(TileLds<PLANES, ROWS, WIDTH>& to) const {
-        const int c = static_cast<int>(threadIdx.x) % kRuns * V;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int row = r0 + u * kPer;
             if (ROWS % kPer != 0 && row >= ROWS) continue;
             if constexpr (PLANES == 1) {
-                *reinterpret_cast<u32x4*>(&to.v[0][row][to.at(row, c)]) = raw[u];
+                *reinterpret_cast<u32x4*>(&to.v[0][row][to.at(row, run)]) = raw[u];
             } else {
                 float x[V];
                 Vec<Elem>::widen(raw[u], x);
@@ -266,7 +270,7 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
                 s.of(x);
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p)
-                    *reinterpret_cast<typename Split<PLANES, V, true>::Run*>(&to.v[p][row][to.at(row, c)]) = s.part[p];
+                    *reinterpret_cast<typename Split<PLANES, V, true>::Run*>(&to.v[p][row][to.at(row, run)]) = s.part[p];
             }
         }
     }
@@ -296,61 +300,63 @@ template <typename Elem> __device__ __forceinline__ const Elem* heads_at(const H
     return static_cast<const Elem*>(t.p) + n * t.sn + h / t.per * t.sh;
 }
 
-// Four values side by side, of which those below `valid` are wanted.
-template <typename T> __device__ __forceinline__ void store_values(T* to, const f32x4& x, int valid) {
-    struct __attribute__((packed, aligned(sizeof(T)))) Two {
-        T v[2];
-    };
-    struct __attribute__((packed, aligned(sizeof(T)))) Four {
-        T v[4];
-    };
-    T e[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) e[r] = Storage<T>::from_f32(x[r]);
-    if (valid >= 4) *reinterpret_cast<Four*>(to) = Four{e[0], e[1], e[2], e[3]};
-    else {
-        if (valid >= 2) *reinterpret_cast<Two*>(to) = Two{e[0], e[1]};
-        if (valid == 1) to[0] = e[0];
-        if (valid == 3) to[2] = e[2];
-    }
-}
-
 struct None {};
 
-// Tiles of K channels of q and k for W waves of 16 C columns each.
-template <typename Elem, int K, int W, int C, bool STATES> struct Shape {
-    static constexpr int T = kTile<Elem>, PI = kParts<Elem>, PS = kSums<Elem>;
-    static constexpr int kColumns = 16 * C * W, kThreads = 64 * W;
+// What a workgroup holds in LDS, for tiles of K channels of q and k and W waves of 16
+// columns each.
+template <typename Elem, int K, int W, bool STATES> struct Shape {
+    static constexpr int T = tile_steps(std::is_same_v<Elem, bf16_t>, K), PI = kParts<Elem>, PS = kSums<Elem>;
+    static constexpr int kColumns = 16 * W, kPanels = T == 64 ? 3 : 1;
     struct Steps {
         std::conditional_t<STATES, None, TileLds<PI, T, K>> q;
         TileLds<PI, T, K> k;
         TileLds<PI, T, kColumns> v;
     };
-    struct Weights {
-        TileLds<PS, T, T> p;
-        int32_t odd[2];   // the tile (+ 1) of which v holds an infinity or NaN
+    struct Own {
+        // the weights in panels of 32 x 32: rows and columns 32 a .. and 32 b .. are panel a + b
+        TileLds<PS, 32 * kPanels, 32> weights;
+        u32x4 outputs[T][kColumns / 4];   // in fp32 or the storage type, from the row's start on
+        int32_t odd[2];                   // the tile (+ 1) of which v holds an infinity or NaN
+    };
+    struct Least {
+        alignas(16) float in_decay[T];    // from a tile's steps to the state behind it
+        std::conditional_t<STATES, None, Own> own;
     };
     // two tiles of steps, where they find room
-    static constexpr int kStages = 2 * sizeof(Steps) + sizeof(Weights) <= kLdsBytes ? 2 : 1;
-    struct Lds {
+    static constexpr int kStages = 2 * sizeof(Steps) + sizeof(Least) <= kLdsBytes ? 2 : 1;
+    struct Lds : Least {
         Steps steps[kStages];
-        std::conditional_t<STATES, None, Weights> weights;
     };
+    // W waves for the state, half as many for memory and, but for STATES, as many for the weights
+    static constexpr int kMemory = 32 * W, kWeights = STATES ? 0 : 32 * W, kThreads = 64 * W + kMemory + kWeights;
+    static constexpr int kWavesPerSimd = 2 * sizeof(Lds) <= kLdsBytes || W == 8 ? 4 : 2;
 };
+// where run `run` of 16 bytes of a row of outputs stands: the order changes from row to row
+__device__ __forceinline__ int output_run(int row, int run) { return run ^ (row & 7); }
 
-// A pass, or (STATES) only what its segments add to the state.  A wave's accumulators of
-// the state: S[b][c], lane m + 16 g, register r holds the state at
-// (32 (b / 2) + 8 g + 4 (b % 2) + r, column(c, m)), so that those of two blocks side by
-// side are the 8 consecutive rows that a lane hands a matrix instruction, without a
-// move.  Outputs come transposed, O[i][c] with row 16 i + m and columns
-// column(c, 4 g + r): 4 C of them side by side.
-template <typename Elem, int KD, int W, int CB, bool STATES>
-__global__ __launch_bounds__(64 * W, 2) void attention_kernel(Args a) {
-    using Sh = Shape<Elem, KD, W, CB, STATES>;
-    constexpr int T = Sh::T, PI = Sh::PI, PS = Sh::PS, VB = Sh::kColumns, NT = Sh::kThreads, IB = T / 16, JS = T / 32, KS = KD / 32;
-    constexpr int STAGES = Sh::kStages;
-    __shared__ __align__(16) typename Sh::Lds lds;
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, m = lane % 16, g = lane / 16;
+// A pass, or (STATES) only what its segments add to the state.  The waves of a workgroup
+// have three tasks, so that some work where others wait:
+//   * W hold the state, 16 columns each: they multiply it by q, add what the tile's own
+//     steps give (weights times v), and bring the state over the tile;
+//   * W / 2 make the weights (q.k, decayed) of the next tile;
+//   * W / 2 move: load the tile after the next, unpack the next one, store the outputs.
+// Two barriers a tile: ahead of the first, tile t's outputs are made and tile t + 1 is
+// unpacked; ahead of the second, the state is brought over tile t, the weights of tile
+// t + 1 are made, and the outputs leave.  With one stage in LDS the next tile's unpacking
+// and its weights follow in turn.
+//
+// S[b], lane m + 16 g, register r is the state at (32 (b / 2) + 8 g + 4 (b % 2) + r,
+// 16 wave + m), so that those of two blocks side by side are the 8 consecutive rows that a
+// lane hands a matrix instruction, without a move.  Outputs come transposed, O[i] with row
+// 16 i + m and columns 16 wave + 4 g + r.
+template <typename Elem, int KD, int W, bool STATES>
+__global__ __launch_bounds__((Shape<Elem, KD, W, STATES>::kThreads), (Shape<Elem, KD, W, STATES>::kWavesPerSimd))
+void attention_kernel(Args a) {
+    using Sh = Shape<Elem, KD, W, STATES>;
+    constexpr int T = Sh::T, PI = Sh::PI, PS = Sh::PS, VB = Sh::kColumns, IB = T / 16, JS = T / 32, KS = KD / 32;
+    constexpr int STAGES = Sh::kStages, BLOCKS = IB * (IB + 1) / 2;
+    __shared__ typename Sh::Lds lds;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
 
     const int32_t segment = blockIdx.x / static_cast<uint32_t>(a.first[3]);
     const int32_t id = blockIdx.x - segment * a.first[3];
@@ -363,210 +369,87 @@ __global__ __launch_bounds__(64 * W, 2) void attention_kernel(Args a) {
     const int32_t steps = steps_of(a.lengths, n, a.L), kd = pass.kd, vd = pass.vd, v0 = block * VB;
     const bool reverse = pass.reverse != 0, y_f32 = pass.y.f32 != 0;
     const float log_decay = a.log_decay[h], log2_decay = log2_of(log_decay);
-    const float in_scale = pass.in_scale, out_scale = pass.out_scale, scale = a.scale;
 
-    auto column = [&](int c, int i) { return CB == 1 ? 16 * wave + i : 32 * wave + 8 * (i / 4) + 4 * c + i % 4; };
-    // channels that a lane hands to a transposing read, of the state's rows and columns
-    auto row_chunk = [&](int b) { return 32 * (b / 2) + 8 * (m % 4) + 4 * (b % 2); };
-    auto column_chunk = [&](int c) { return column(c, 4 * (m % 4)); };
-
-    f32x4 S[KD / 16][CB];
-    auto each_state = [&](auto&& f) {
-#pragma unroll
-        for (int b = 0; b < KD / 16; ++b)
-#pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + column(c, m);
-                    if (i < kd && j < vd) S[b][c][r] = f(S[b][c][r], i * pass.at.row + j * pass.at.col);
-                }
-    };
-#pragma unroll
-    for (int b = 0; b < KD / 16; ++b)
-#pragma unroll
-        for (int c = 0; c < CB; ++c) S[b][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t size = static_cast<int64_t>(kd) * vd, by_segment = (static_cast<int64_t>(head) * a.segments + segment) * size;
-    if (!STATES && pass.s_in) {
-        const float* s = pass.s_in + (pass.from_segments ? by_segment : head * size);
-        each_state([&](float, int at) { return s[at]; });
-    }
-
+    // a segment's tiles, in the order of the walk
     const int32_t tiles = (steps + T - 1) / T, t_first = segment * a.each, t_end = min(tiles, t_first + a.each);
-    const int64_t y_sl = pass.y.sl;
-    const Elem* q = heads_at<Elem>(pass.q, n, h);
-    const Elem* k = heads_at<Elem>(pass.k, n, h);
-    const Elem* v = heads_at<Elem>(pass.v, n, h);
-    // a lane's outputs: 4 CB values side by side in row m of every 16
-    const int y_valid = vd - (v0 + column(0, 4 * g));
-    const int64_t y_at = n * pass.y.sn + h * pass.y.sh + m * y_sl + v0 + column(0, 4 * g);
-    TileLoad<Elem, T, KD, NT> lq(q, pass.q.sl, 0, kd), lk(k, pass.k.sl, 0, kd);
-    TileLoad<Elem, T, VB, NT> lv(v, pass.v.sl, v0, vd);
-    const bool wide = kd == KD && vd - v0 >= VB;
-    if constexpr (!STATES) {
-        // weights above the diagonal are zeros that nothing writes
-        for (int i = tid; i < static_cast<int>(sizeof(lds.weights) / 4); i += NT) reinterpret_cast<uint32_t*>(&lds.weights)[i] = 0;
-    }
+    auto row_of = [&](int32_t t) { return (reverse ? tiles - 1 - t : t) * T; };
+    auto rows_of = [&](int32_t t) { return min(T, steps - row_of(t)); };
+    auto stage_of = [&](int32_t t) -> auto& { return lds.steps[t & (STAGES - 1)]; };
+    const bool any = t_first < t_end;
 
-    // decays: over a tile, from the state to its steps, from its steps to the state
-    float whole = 1.0f, out_decay[IB], in_decay[JS][8];
-    int decays_of = 0;
-    auto set_decays = [&](int live) {
-        decays_of = live;
-        whole = exact_power(log_decay, live);
-#pragma unroll
-        for (int i = 0; i < IB; ++i)
-            out_decay[i] = out_scale * power(log2_decay, reverse ? max(0, live - 1 - (16 * i + m)) : 16 * i + m + 1);
-#pragma unroll
-        for (int s = 0; s < JS; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = 32 * s + 8 * g + e;
-                in_decay[s][e] = in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j));
-            }
-    };
-
-    // The first state is there ahead of the rounds: each of them would wait for it, and
-    // for its own loads with it.
-#pragma unroll
-    for (int b = 0; b < KD / 16; ++b)
-#pragma unroll
-        for (int c = 0; c < CB; ++c) asm volatile("" : "+v"(S[b][c]));
-    // a round multiplies tile t, and has tile t + 1 loaded and brought to LDS
-    for (int32_t t = t_first - 1; t < t_end; ++t) {
-        const int32_t next0 = (reverse ? tiles - 2 - t : t + 1) * T, t0 = reverse ? next0 + T : next0 - T;
-        const bool more = t + 1 < t_end, has = t >= t_first;
-        auto& now = lds.steps[t & (STAGES - 1)];
-        auto& next = lds.steps[(t + 1) & (STAGES - 1)];
-        if (more) {
-            const int32_t live = min(T, steps - next0);
-            if constexpr (!STATES) lq.load(next0, live, kd);
-            lk.load(next0, live, kd);
-            lv.load(next0, live, vd);
-        }
-        const int32_t live = min(T, steps - t0);
-        f32x4 O[IB][CB];
-        bf16x8 fv[JS][CB][PI];
-        if (has) {
-            if (live != decays_of) set_decays(live);
-            if constexpr (!STATES) {
-                // the weights of the tile, in blocks of 16 x 16 of the triangle
-                for (int blk = wave; blk < IB * (IB + 1) / 2; blk += W) {
-                    const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
-                    const int ib = reverse ? near : far, jb = reverse ? far : near;
-                    f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        bf16x8 fk[PI], fq[PI];
-                        now.k.across(16 * jb + m, 32 * s + 8 * g, fk);
-                        now.q.across(16 * ib + m, 32 * s + 8 * g, fq);
-                        w = multiply<PI, PI, PS>(fk, fq, w);
-                    }
-                    float x[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int i = 16 * ib + m, j = 16 * jb + 4 * g + r, d = reverse ? j - i : i - j;
-                        x[r] = d < 0 ? 0.0f : w[r] * (scale * power(log2_decay, d));
-                    }
-                    Split<PS, 4, false> parts;
-                    parts.of(x);
-                    auto& to = lds.weights.p;
-                    const int row = 16 * ib + m, c = 16 * jb + 4 * g;
-#pragma unroll
-                    for (int p = 0; p < PS; ++p) *reinterpret_cast<bf16x4*>(&to.v[p][row][to.at(row, c)]) = parts.part[p];
-                }
-
-                // what the state gives
-#pragma unroll
-                for (int i = 0; i < IB; ++i)
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) O[i][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    Split<PS, 8, false> fs[CB];
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) {
-                        float x[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][c][e % 4];
-                        fs[c].of(x);
-                    }
-#pragma unroll
-                    for (int i = 0; i < IB; ++i) {
-                        bf16x8 fq[PI];
-                        now.q.across(16 * i + m, 32 * s + 8 * g, fq);
-#pragma unroll
-                        for (int c = 0; c < CB; ++c) O[i][c] = multiply<PS, PI, PS>(fs[c].part, fq, O[i][c]);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < IB; ++i)
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) O[i][c] *= out_decay[i];
-            }
-
-            // the state behind the tile
+    if (wave < W) {   // the state
+        // channels that a lane hands to a transposing read of k
+        auto row_chunk = [&](int b) { return 32 * (b / 2) + 8 * (m % 4) + 4 * (b % 2); };
+        f32x4 S[KD / 16];
+        auto each_state = [&](auto&& f) {
 #pragma unroll
             for (int b = 0; b < KD / 16; ++b)
 #pragma unroll
-                for (int c = 0; c < CB; ++c) S[b][c] *= whole;
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + 16 * wave + m;
+                    if (i < kd && j < vd) S[b][r] = f(S[b][r], i * pass.at.row + j * pass.at.col);
+                }
+        };
 #pragma unroll
-            for (int s = 0; s < JS; ++s) {
-                Split<kStateParts, 8, false> late[CB];
+        for (int b = 0; b < KD / 16; ++b) S[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const int64_t size = static_cast<int64_t>(kd) * vd, by_segment = (static_cast<int64_t>(head) * a.segments + segment) * size;
+        if (!STATES && pass.s_in) {
+            const float* s = pass.s_in + (pass.from_segments ? by_segment : head * size);
+            each_state([&](float, int at) { return s[at]; });
+        }
+        float whole = 1.0f, out_decay[IB];   // the decays over a tile, and from the state to its steps
+        int decays_of = 0;
+        if (!STATES && any) __syncthreads();
+        if (any) __syncthreads();            // the first tile
+        if (!STATES && any) __syncthreads(); // its weights
+        for (int32_t t = t_first; t < t_end; ++t) {
+            const auto& now = stage_of(t);
+            const int live = rows_of(t);
+            if (live != decays_of) {
+                decays_of = live;
+                whole = exact_power(log_decay, live);
+                const int j = threadIdx.x;
+                if (j < T) lds.in_decay[j] = pass.in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j));
+                if constexpr (STATES) __syncthreads();
 #pragma unroll
-                for (int c = 0; c < CB; ++c) {
-                    now.v.down(32 * s + 8 * g + m / 4, column_chunk(c), fv[s][c]);
+                for (int i = 0; i < IB; ++i)
+                    out_decay[i] = pass.out_scale * power(log2_decay, reverse ? max(0, live - 1 - (16 * i + m)) : 16 * i + m + 1);
+            }
+            if constexpr (!STATES) {
+                const bool odd = lds.own.odd[t & 1] == t + 1;
+                f32x4 O[IB];
+#pragma unroll
+                for (int i = 0; i < IB; ++i) O[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    Split<PS, 8, false> fs;
                     float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float sum = 0.0f;
+                    for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][e % 4];
+                    fs.of(x);
+                    bf16x8 fq[IB][PI];
 #pragma unroll
-                        for (int p = PI - 1; p >= 0; --p) sum += static_cast<float>(fv[s][c][p][e]);
-                        x[e] = sum * in_decay[s][e];
-                    }
-                    late[c].of(x);
+                    for (int i = 0; i < IB; ++i) now.q.across(16 * i + m, 32 * s + 8 * g, fq[i]);
+                    multiply<PS, PI, PS>([&](int, int p) { return fs.part[p]; }, [&](int i, int p) { return fq[i][p]; }, O);
                 }
 #pragma unroll
-                for (int b = 0; b < KD / 16; ++b) {
-                    bf16x8 fk[PI];
-                    now.k.down(32 * s + 8 * g + m / 4, row_chunk(b), fk);
+                for (int i = 0; i < IB; ++i) O[i] *= out_decay[i];
+                if (!odd) {
 #pragma unroll
-                    for (int c = 0; c < CB; ++c) S[b][c] = multiply<PI, kStateParts, kStateParts>(fk, late[c].part, S[b][c]);
-                }
-            }
-        }
-        // The next tile's rows go to LDS ahead of this one's outputs: the wait for them
-        // is for every access to memory before it, stores too.
-        auto stage = [&] {
-            if (!more) return;
-            const int32_t live = min(T, steps - next0);
-            const bool whole_tile = wide && live == T;
-            lk.trim(whole_tile, live, kd);
-            lv.trim(whole_tile, live, vd);
-            if constexpr (!STATES) {
-                lq.trim(whole_tile, live, kd);
-                lq.template store<PI>(next.q);
-                if (!lv.finite()) lds.weights.odd[(t + 1) & 1] = t + 2;
-            }
-            lk.template store<PI>(next.k);
-            lv.template store<PI>(next.v);
-        };
-        if constexpr (!STATES) __syncthreads();   // the weights
-        if constexpr (STAGES == 2) stage();
-        if constexpr (!STATES) {
-            if (has) {
-                // what the tile's own steps give
-                if (lds.weights.odd[t & 1] != t + 1) {
+                    for (int s = 0; s < JS; ++s) {
+                        bf16x8 fv[PI];
+                        now.v.down(32 * s + 8 * g + m / 4, 16 * wave + 4 * (m % 4), fv);
 #pragma unroll
-                    for (int i = 0; i < IB; ++i)
-#pragma unroll
-                        for (int s = 0; s < JS; ++s) {
-                            if (reverse ? 32 * s + 31 < 16 * i : 32 * s > 16 * i + 15) continue;
-                            bf16x8 fp[PS];
-                            lds.weights.p.across(16 * i + m, 32 * s + 8 * g, fp);
-#pragma unroll
-                            for (int c = 0; c < CB; ++c) O[i][c] = multiply<PI, PS, PS>(fv[s][c], fp, O[i][c]);
+                        for (int i = 0; i < IB; i += 2) {
+                            if (reverse ? s < i / 2 : s > i / 2) continue;
+                            bf16x8 fp[2][PS];
+                            lds.own.weights.across(32 * (i / 2 + s) + m, 8 * g, fp[0]);
+                            lds.own.weights.across(32 * (i / 2 + s) + 16 + m, 8 * g, fp[1]);
+                            f32x4 pair[2] = {O[i], O[i + 1]};
+                            multiply<PI, PS, PS>([&](int, int p) { return fv[p]; }, [&](int u, int p) { return fp[u][p]; }, pair);
+                            O[i] = pair[0], O[i + 1] = pair[1];
                         }
+                    }
                 } else {
                     // step by step: a weight of zero would not remove an infinity or NaN of a later v
                     auto value = [](const auto& tile, int row, int c) {
@@ -582,52 +465,204 @@ __global__ __launch_bounds__(64 * W, 2) void attention_kernel(Args a) {
                         for (int i = 0; i < IB; ++i) {
                             const int row = 16 * i + m;
                             if (reverse ? j < row : j > row) continue;
-                            const float w = value(lds.weights.p, row, j);
+                            const float w = value(lds.own.weights, 32 * (i / 2 + j / 32) + 16 * (i % 2) + m, j % 32);
 #pragma unroll
-                            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) O[i][c][r] += w * value(now.v, j, column(c, 4 * g + r));
+                            for (int r = 0; r < 4; ++r) O[i][r] += w * value(now.v, j, 16 * wave + 4 * g + r);
                         }
                 }
-            }
-        }
-        if constexpr (STAGES == 1) {
-            __syncthreads();
-            stage();
-        }
-        if constexpr (!STATES) {
-            if (has && y_valid > 0) {
+                if (y_f32) {
 #pragma unroll
-                for (int i = 0; i < IB; ++i) {
-                    if (16 * i + m >= live) continue;
-                    const int64_t at = y_at + (t0 + 16 * i) * y_sl;
+                    for (int i = 0; i < IB; ++i)
+                        lds.own.outputs[16 * i + m][output_run(16 * i + m, 4 * wave + g)] = __builtin_bit_cast(u32x4, O[i]);
+                } else {
+                    struct alignas(4 * sizeof(Elem)) Four {
+                        Elem v[4];
+                    };
+                    constexpr int kPer = 16 / sizeof(Four);
 #pragma unroll
-                    for (int c = 0; c < CB; ++c) {
-                        if (y_f32) store_values<float>(static_cast<float*>(pass.y.p) + at + 4 * c, O[i][c], y_valid - 4 * c);
-                        else store_values<Elem>(static_cast<Elem*>(pass.y.p) + at + 4 * c, O[i][c], y_valid - 4 * c);
+                    for (int i = 0; i < IB; ++i) {
+                        const Four four{Storage<Elem>::from_f32(O[i][0]), Storage<Elem>::from_f32(O[i][1]),
+                                        Storage<Elem>::from_f32(O[i][2]), Storage<Elem>::from_f32(O[i][3])};
+                        const int c = 4 * wave + g;
+                        auto* run = &lds.own.outputs[16 * i + m][output_run(16 * i + m, c / kPer)];
+                        reinterpret_cast<Four*>(run)[c % kPer] = four;
                     }
                 }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b) S[b] *= whole;
+#pragma unroll
+            for (int s = 0; s < JS; ++s) {
+                bf16x8 fv[PI];
+                now.v.down(32 * s + 8 * g + m / 4, 16 * wave + 4 * (m % 4), fv);
+                Split<kStateParts, 8, false> late;
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int p = PI - 1; p >= 0; --p) sum += static_cast<float>(fv[p][e]);
+                    x[e] = sum * lds.in_decay[32 * s + 8 * g + e];
+                }
+                late.of(x);
+#pragma unroll
+                for (int b = 0; b < KD / 16; b += 2) {
+                    bf16x8 fk[2][PI];
+                    now.k.down(32 * s + 8 * g + m / 4, row_chunk(b), fk[0]);
+                    now.k.down(32 * s + 8 * g + m / 4, row_chunk(b + 1), fk[1]);
+                    f32x4 pair[2] = {S[b], S[b + 1]};
+                    multiply<PI, kStateParts, kStateParts>([&](int i, int p) { return fk[i][p]; },
+                                                           [&](int, int p) { return late.part[p]; }, pair);
+                    S[b] = pair[0], S[b + 1] = pair[1];
+                }
+            }
+            __syncthreads();
+            if constexpr (STAGES == 1) {
+                __syncthreads();
+                if constexpr (!STATES) __syncthreads();
             }
         }
-        __syncthreads();
+        if constexpr (STATES) {
+            float* s = pass.s_out + by_segment;
+            each_state([&](float x, int at) { return s[at] = x; });
+        } else if (pass.s_out) {
+            float* s = pass.s_out + head * size;
+            each_state([&](float x, int at) { return s[at] = x; });
+        }
+        return;
     }
 
-    if constexpr (STATES) {
-        float* s = pass.s_out + by_segment;
-        each_state([&](float x, int at) { return s[at] = x; });
-    } else {
+    if (STATES || wave < W + W / 2) {   // memory
+        const int tid = threadIdx.x - 64 * W;
+        TileLoad<Elem, T, KD, Sh::kMemory> lq(tid, heads_at<Elem>(pass.q, n, h), pass.q.sl, 0, kd);
+        TileLoad<Elem, T, KD, Sh::kMemory> lk(tid, heads_at<Elem>(pass.k, n, h), pass.k.sl, 0, kd);
+        TileLoad<Elem, T, VB, Sh::kMemory> lv(tid, heads_at<Elem>(pass.v, n, h), pass.v.sl, v0, vd);
+        auto load = [&](int32_t t) {
+            if (t >= t_end) return;
+            lk.load(row_of(t), rows_of(t), kd);
+            if constexpr (!STATES) lq.load(row_of(t), rows_of(t), kd);
+            lv.load(row_of(t), rows_of(t), vd);
+        };
+        auto unpack = [&](int32_t t) {
+            if (t >= t_end) return;
+            const int rows = rows_of(t);
+            const bool whole = kd == KD && vd - v0 >= VB && rows == T;
+            auto& to = stage_of(t);
+            lk.trim(whole, rows, kd);
+            lk.template store<PI>(to.k);
+            if constexpr (!STATES) {
+                lq.trim(whole, rows, kd);
+                lq.template store<PI>(to.q);
+            }
+            lv.trim(whole, rows, vd);
+            if constexpr (!STATES)
+                if (!lv.finite()) lds.own.odd[t & 1] = t + 1;
+            lv.template store<PI>(to.v);
+        };
+        // a tile's outputs, whole lines of them
+        auto put = [&](const auto& own, auto* y, int32_t t) {
+            using Out = std::remove_pointer_t<decltype(y)>;
+            constexpr int V = Vec<Out>::V, RUNS = VB / V, PER = Sh::kMemory / RUNS;
+            const int run = tid % RUNS, valid = min(V, vd - v0 - run * V), rows = rows_of(t);
+            if (valid <= 0) return;
+            y += n * pass.y.sn + h * pass.y.sh + row_of(t) * pass.y.sl + v0 + run * V;
+#pragma unroll
+            for (int u = 0; u < T / PER; ++u) {
+                const int row = tid / RUNS + u * PER;
+                if (row < rows) store_run<Out, false>(y + row * pass.y.sl, valid, own.outputs[row][output_run(row, run)]);
+            }
+        };
+        load(t_first);
+        if (!STATES && any) __syncthreads();   // the weights' waves have cleared odd
+        unpack(t_first);
+        if (any) __syncthreads();
+        if constexpr (STAGES == 2) load(t_first + 1);
+        if (!STATES && any) __syncthreads();
+        int decays_of = 0;
+        for (int32_t t = t_first; t < t_end; ++t) {
+            if (STATES && rows_of(t) != decays_of) {   // they are set by the waves of the state
+                decays_of = rows_of(t);
+                __syncthreads();
+            }
+            if constexpr (STAGES == 2) unpack(t + 1);
+            if constexpr (!STATES) __syncthreads();
+            load(t + STAGES);
+            if constexpr (!STATES) {
+                if (y_f32) put(lds.own, static_cast<float*>(pass.y.p), t);
+                else put(lds.own, static_cast<Elem*>(pass.y.p), t);
+            }
+            __syncthreads();
+            if constexpr (STAGES == 1) {
+                unpack(t + 1);
+                __syncthreads();
+                if constexpr (!STATES) __syncthreads();
+            }
+        }
+        if constexpr (STATES) return;
         // padding, of which each segment takes a share of rows
         const int width = min(VB, vd - v0), share = (a.L - steps + a.segments - 1) / a.segments;
         const int32_t row0 = steps + min(segment * static_cast<int64_t>(share), static_cast<int64_t>(a.L - steps));
         const int64_t values = static_cast<int64_t>(min(share, a.L - row0)) * width;
-        for (int64_t i = tid; i < values; i += NT) {
-            const int64_t at = n * pass.y.sn + (row0 + i / width) * y_sl + h * pass.y.sh + v0 + i % width;
+        for (int64_t i = tid; i < values; i += Sh::kMemory) {
+            const int64_t at = n * pass.y.sn + (row0 + i / width) * pass.y.sl + h * pass.y.sh + v0 + i % width;
             if (y_f32) static_cast<float*>(pass.y.p)[at] = 0.0f;
             else static_cast<Elem*>(pass.y.p)[at] = Storage<Elem>::from_f32(0.0f);
         }
-        if (!pass.s_out) return;
-        float* s = pass.s_out + head * size;
-        each_state([&](float x, int at) { return s[at] = x; });
+        return;
+    }
+
+    // the weights
+    if constexpr (!STATES) {
+        auto weigh = [&](int32_t t) {
+            if (t >= t_end) return;
+            const auto& now = stage_of(t);
+            // in blocks of 16 x 16 of the triangle
+            for (int blk = wave - W - W / 2; blk < BLOCKS; blk += W / 2) {
+                const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
+                const int ib = reverse ? near : far, jb = reverse ? far : near;
+                f32x4 w[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    bf16x8 fk[PI], fq[PI];
+                    now.k.across(16 * jb + m, 32 * s + 8 * g, fk);
+                    now.q.across(16 * ib + m, 32 * s + 8 * g, fq);
+                    multiply<PI, PI, PS>([&](int, int p) { return fk[p]; }, [&](int, int p) { return fq[p]; }, w);
+                }
+                float x[4];
+                const int d0 = reverse ? 16 * (jb - ib) + 4 * g - m : 16 * (ib - jb) + m - 4 * g;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int d = reverse ? d0 + r : d0 - r;
+                    x[r] = d < 0 ? 0.0f : w[0][r] * (a.scale * power(log2_decay, d));
+                }
+                Split<PS, 4, false> parts;
+                parts.of(x);
+                auto& to = lds.own.weights;
+                const int row = 32 * (ib / 2 + jb / 2) + 16 * (ib % 2) + m, c = 16 * (jb % 2) + 4 * g;
+#pragma unroll
+                for (int p = 0; p < PS; ++p) *reinterpret_cast<bf16x4*>(&to.v[p][row][to.at(row, c)]) = parts.part[p];
+            }
+        };
+        // weights above the diagonal are zeros that nothing writes
+        const int tid = threadIdx.x - 96 * W;
+        for (int i = tid; i < static_cast<int>(sizeof(lds.own.weights) / 4); i += Sh::kWeights)
+            reinterpret_cast<uint32_t*>(&lds.own.weights)[i] = 0;
+        if (tid < 2) lds.own.odd[tid] = 0;
+        if (any) __syncthreads();
+        if (any) __syncthreads();
+        weigh(t_first);
+        if (any) __syncthreads();
+        for (int32_t t = t_first; t < t_end; ++t) {
+            __syncthreads();
+            if constexpr (STAGES == 2) weigh(t + 1);
+            __syncthreads();
+            if constexpr (STAGES == 1) {
+                __syncthreads();
+                weigh(t + 1);
+                __syncthreads();
+            }
+        }
     }
 }
 
@@ -772,7 +807,7 @@ HeadsOut heads_out(const wg_heads& t) { return {const_cast<void*>(t.data), t.str
 
 // How a call is cut: the kernel's form and the segments of a sequence.
 struct Cut {
-    int kd, waves;            // channels of q and k and waves of a workgroup that the kernel is made for
+    int kd, waves;            // channels of q and k, and waves that hold the state, of the kernel's form
     int32_t segments, each;   // tiles of a segment
 };
 // Segments, where the heads do not fill the chip: as many as make kUnits workgroups, of
@@ -780,10 +815,11 @@ struct Cut {
 constexpr int64_t kFull = 192, kUnits = 512, kLeast = 4;
 constexpr int columns_of(int waves) { return 16 * waves; }
 int64_t blocks_of(int vd, int waves) { return (vd + columns_of(waves) - 1) / columns_of(waves); }
-Cut cut_of(int tile, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
+Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
     int kd = 0, vd = 0;
     for (int p = 0; p < passes; ++p) kd = std::max(kd, dims[p][0]), vd = std::max(vd, dims[p][1]);
-    Cut c{kd <= 32 ? 32 : kd <= 64 ? 64 : kd <= 128 ? 128 : 256, vd <= 64 ? 4 : 8, 1, 1};
+    Cut c{kd <= 32 ? 32 : kd <= 64 ? 64 : kd <= 128 ? 128 : 256, vd <= 64 || kd > 128 || dtype == kF32 ? 4 : 8, 1, 1};
+    const int tile = tile_steps(dtype == kBF16, c.kd);
     int64_t units = 0;
     for (int p = 0; p < passes; ++p) units += N * H * blocks_of(dims[p][1], c.waves);
     const int64_t tiles = (L + tile - 1) / tile;
@@ -794,7 +830,6 @@ Cut cut_of(int tile, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int 
     c.segments = static_cast<int32_t>(std::max<int64_t>(1, (tiles + c.each - 1) / c.each));
     return c;
 }
-constexpr int tile_of(int dtype) { return dtype == kBF16 ? kTile<bf16_t> : kTile<float>; }
 
 // HIP takes fewer than 2^32 threads: more sequences than that go in several launches.
 hipError_t over_sequences(const Args& a, int passes, int dtype, int threads, void (*kernel)(Args), hipStream_t stream) {
@@ -822,13 +857,14 @@ hipError_t over_sequences(const Args& a, int passes, int dtype, int threads, voi
     return hipGetLastError();
 }
 
-#define WG_ATTENTION_SHAPES(X) X(32, 4) X(32, 8) X(64, 4) X(64, 8) X(128, 4) X(128, 8) X(256, 4) X(256, 8)
+#define WG_ATTENTION_SHAPES(X) X(32, 4) X(32, 8) X(64, 4) X(64, 8) X(128, 4) X(128, 8) X(256, 4)
 
 template <typename Elem, bool STATES> hipError_t run_passes(Args& a, int passes, const Cut& cut, int dtype, hipStream_t stream) {
     for (int p = 0; p < passes; ++p) a.pass[p].blocks = static_cast<int32_t>(blocks_of(a.pass[p].vd, cut.waves));
     a.segments = cut.segments, a.each = cut.each;
 #define WG_ATTENTION_CASE(K, W) \
-    if (cut.kd == K && cut.waves == W) return over_sequences(a, passes, dtype, 64 * W, attention_kernel<Elem, K, W, 1, STATES>, stream);
+    if constexpr (W == 4 || sizeof(Elem) == 2) \
+        if (cut.kd == K && cut.waves == W) return over_sequences(a, passes, dtype, Shape<Elem, K, W, STATES>::kThreads, attention_kernel<Elem, K, W, STATES>, stream);
     WG_ATTENTION_SHAPES(WG_ATTENTION_CASE)
 #undef WG_ATTENTION_CASE
     return hipErrorInvalidValue;
@@ -843,7 +879,7 @@ hipError_t run_chains(Args a, const Chain* chains, int of, const Cut& cut, int d
     int32_t size = 0;
     for (int c = 0; c < of; ++c) k.chain[c] = chains[c], size = std::max(size, chains[c].size);
     k.heads = a.N * a.H, k.L = a.L, k.H = a.H, k.segments = cut.segments;
-    k.tile = tile_of(dtype), k.each_steps = cut.each * k.tile, k.blocks = (size + kThreads - 1) / kThreads, k.of = of;
+    k.tile = tile_steps(dtype == kBF16, cut.kd), k.each_steps = cut.each * k.tile, k.blocks = (size + kThreads - 1) / kThreads, k.of = of;
     k.log_decay = a.log_decay, k.lengths = a.lengths;
     chain_kernel<<<static_cast<unsigned>(k.heads * k.blocks * of), kThreads, 0, stream>>>(k);
     return hipGetLastError();
@@ -873,8 +909,8 @@ size_t segment_bytes(const Cut& c, int64_t N, int64_t H, int64_t Dk, int64_t Dv)
 size_t linear_attention_workspace(int dtype, int64_t N, int64_t L, int64_t q_heads, int64_t k_heads, int64_t v_heads, int64_t H,
                                   int64_t Dk, int64_t Dv, bool backward) {
     const Dims dims(Dk, Dv);
-    if (!backward) return segment_bytes(cut_of(tile_of(dtype), N, L, H, dims.forward, 1), N, H, Dk, Dv);
-    return 2 * segment_bytes(cut_of(tile_of(dtype), N, L, H, dims.backward, 3), N, H, Dk, Dv) +
+    if (!backward) return segment_bytes(cut_of(dtype, N, L, H, dims.forward, 1), N, H, Dk, Dv);
+    return 2 * segment_bytes(cut_of(dtype, N, L, H, dims.backward, 3), N, H, Dk, Dv) +
            part_bytes(N, L, q_heads, H, Dk) + part_bytes(N, L, k_heads, H, Dk) + part_bytes(N, L, v_heads, H, Dv);
 }
 #endif
@@ -883,7 +919,7 @@ template <int D> hipError_t launch_linear_attention_t(const wg_linear_attention&
     using Elem = typename DTypeOf<D>::type;
     const int32_t Dk = static_cast<int32_t>(a.Dk), Dv = static_cast<int32_t>(a.Dv);
     const Dims dims(Dk, Dv);
-    const Cut cut = cut_of(tile_of(D), a.N, a.L, a.heads, dims.forward, 1);
+    const Cut cut = cut_of(D, a.N, a.L, a.heads, dims.forward, 1);
     Args k{};
     k.N = a.N, k.L = static_cast<int32_t>(a.L), k.H = static_cast<int32_t>(a.heads);
     k.log_decay = a.log_decay, k.lengths = a.lengths, k.scale = static_cast<float>(a.scale);
@@ -902,7 +938,7 @@ template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_a
     const int64_t H = a.heads;
     const int32_t Dk = static_cast<int32_t>(a.Dk), Dv = static_cast<int32_t>(a.Dv);
     const Dims dims_of(Dk, Dv);
-    const Cut cut = cut_of(tile_of(D), a.N, a.L, H, dims_of.backward, 3);
+    const Cut cut = cut_of(D, a.N, a.L, H, dims_of.backward, 3);
     Args k{};
     k.N = a.N, k.L = static_cast<int32_t>(a.L), k.H = static_cast<int32_t>(H);
     k.log_decay = a.log_decay, k.lengths = a.lengths, k.scale = static_cast<float>(a.scale);
