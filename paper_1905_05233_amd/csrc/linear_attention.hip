@@ -198,8 +198,8 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
     static constexpr int V = Vec<Elem>::V, kRuns = WIDTH / V, kPer = THREADS / kRuns, U = (ROWS + kPer - 1) / kPer;
     static_assert(THREADS % kRuns == 0 && (ROWS % kPer == 0 || U == 1), "threads cover whole rows");
     u32x4 raw[U];
-    const Elem* base;   // the thread's channels of the sequence's first row
-    int64_t stride, own;
+    const Elem* base;   // the thread's channels of its first row of the sequence
+    int64_t stride;
     int run, r0, over;  // its place in a row, its first row; channels too many
 
     __device__ __forceinline__ TileLoad(int thread, const Elem* p, int64_t row_stride, int c0, int D) {
@@ -208,23 +208,23 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
         r0 = thread / kRuns;
         over = max(0, c + V - D);
         stride = row_stride;
-        own = r0 * stride;
-        base = p + (D >= V ? c - over : 0);
+        base = p + r0 * stride + (D >= V ? c - over : 0);
     }
     // rows 0 .. live - 1 (at least one) from row t0 of the sequence
     __device__ __forceinline__ void load(int32_t t0, int live, int D) {
         const Elem* p = base + t0 * stride;
         if (D >= V) {
+            const Elem* first = p - r0 * stride;
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                raw[u] = reinterpret_cast<const Bytes16*>(r0 + u * kPer < live ? p + own + u * kPer * stride : p)->v;
+                raw[u] = reinterpret_cast<const Bytes16*>(r0 + u * kPer < live ? p + u * kPer * stride : first)->v;
             return;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {   // rows shorter than 16 bytes, in pieces of 8, 4 and 2
             raw[u] = u32x4{0, 0, 0, 0};
             if (r0 + u * kPer >= live || over >= V) continue;
-            const Elem* at = p + own + u * kPer * stride;
+            const Elem* at = p + u * kPer * stride;
             constexpr int kPer8 = 8 / sizeof(Elem);
             uint64_t head = 0, tail = 0;
             if (D & kPer8) {
@@ -315,7 +315,8 @@ template <typename Elem, int K, int W, bool STATES> struct Shape {
     struct Own {
         // the weights in panels of 32 x 32: rows and columns 32 a .. and 32 b .. are panel a + b
         TileLds<PS, 32 * kPanels, 32> weights;
-        u32x4 outputs[T][kColumns / 4];   // in fp32 or the storage type, from the row's start on
+        // a tile's outputs: two tiles in the storage type, or one in fp32
+        u32x4 outputs[T * kColumns / 4 * (sizeof(Elem) == 4 ? 2 : 1)];
         int32_t odd[2];                   // the tile (+ 1) of which v holds an infinity or NaN
     };
     struct Least {
@@ -331,19 +332,21 @@ template <typename Elem, int K, int W, bool STATES> struct Shape {
     static constexpr int kMemory = 32 * W, kWeights = STATES ? 0 : 32 * W, kThreads = 64 * W + kMemory + kWeights;
     static constexpr int kWavesPerSimd = 2 * sizeof(Lds) <= kLdsBytes || W == 8 ? 4 : 2;
 };
-// where run `run` of 16 bytes of a row of outputs stands: the order changes from row to row
-__device__ __forceinline__ int output_run(int row, int run) { return run ^ (row & 7); }
+// Where run `run` of 16 bytes of a row of outputs stands, of RUNS a row: the order changes
+// from row to row.
+template <int RUNS> __device__ __forceinline__ int output_at(int row, int run) { return row * RUNS + (run ^ (row & (RUNS < 8 ? RUNS - 1 : 7))); }
 
 // A pass, or (STATES) only what its segments add to the state.  The waves of a workgroup
 // have three tasks, so that some work where others wait:
 //   * W hold the state, 16 columns each: they multiply it by q, add what the tile's own
 //     steps give (weights times v), and bring the state over the tile;
-//   * W / 2 make the weights (q.k, decayed) of the next tile;
-//   * W / 2 move: load the tile after the next, unpack the next one, store the outputs.
-// Two barriers a tile: ahead of the first, tile t's outputs are made and tile t + 1 is
-// unpacked; ahead of the second, the state is brought over tile t, the weights of tile
-// t + 1 are made, and the outputs leave.  With one stage in LDS the next tile's unpacking
-// and its weights follow in turn.
+//   * W / 2 load the tile after the next and unpack the next one;
+//   * W / 2 store the last tile's outputs and make the weights (q.k, decayed) of the next.
+// Two barriers a tile: ahead of the first, tile t's outputs are made, those of tile t - 1
+// leave and tile t + 1 is unpacked; ahead of the second, the state is brought over tile t
+// and the weights of tile t + 1 are made.  Loads go out on both sides of the first, since
+// they hold up their waves as long as the path to memory is taken.  With one stage in LDS
+// the next tile's unpacking and its weights follow in turn.
 //
 // S[b], lane m + 16 g, register r is the state at (32 (b / 2) + 8 g + 4 (b % 2) + r,
 // 16 wave + m), so that those of two blocks side by side are the 8 consecutive rows that a
@@ -367,7 +370,7 @@ void attention_kernel(Args a) {
     const int32_t block = unit - head * pass.blocks, h = head % static_cast<uint32_t>(a.H);
     const int64_t n = head / static_cast<uint32_t>(a.H);
     const int32_t steps = steps_of(a.lengths, n, a.L), kd = pass.kd, vd = pass.vd, v0 = block * VB;
-    const bool reverse = pass.reverse != 0, y_f32 = pass.y.f32 != 0;
+    const bool reverse = pass.reverse != 0, y_f32 = sizeof(Elem) == 2 && pass.y.f32 != 0;
     const float log_decay = a.log_decay[h], log2_decay = log2_of(log_decay);
 
     // a segment's tiles, in the order of the walk
@@ -399,9 +402,10 @@ void attention_kernel(Args a) {
         }
         float whole = 1.0f, out_decay[IB];   // the decays over a tile, and from the state to its steps
         int decays_of = 0;
-        if (!STATES && any) __syncthreads();
-        if (any) __syncthreads();            // the first tile
-        if (!STATES && any) __syncthreads(); // its weights
+        if (any) {                           // the first tile and its weights
+#pragma unroll
+            for (int i = 0; i < 2 * (STATES ? 0 : 1) + (STAGES == 2 ? 1 : STATES ? 2 : 3); ++i) __syncthreads();
+        }
         for (int32_t t = t_first; t < t_end; ++t) {
             const auto& now = stage_of(t);
             const int live = rows_of(t);
@@ -470,21 +474,21 @@ void attention_kernel(Args a) {
                             for (int r = 0; r < 4; ++r) O[i][r] += w * value(now.v, j, 16 * wave + 4 * g + r);
                         }
                 }
+                const int c = 4 * wave + g;
                 if (y_f32) {
 #pragma unroll
                     for (int i = 0; i < IB; ++i)
-                        lds.own.outputs[16 * i + m][output_run(16 * i + m, 4 * wave + g)] = __builtin_bit_cast(u32x4, O[i]);
+                        lds.own.outputs[output_at<VB / 4>(16 * i + m, c)] = __builtin_bit_cast(u32x4, O[i]);
                 } else {
                     struct alignas(4 * sizeof(Elem)) Four {
                         Elem v[4];
                     };
-                    constexpr int kPer = 16 / sizeof(Four);
+                    constexpr int kPer = 16 / sizeof(Four), RUNS = VB * sizeof(Elem) / 16;
 #pragma unroll
                     for (int i = 0; i < IB; ++i) {
                         const Four four{Storage<Elem>::from_f32(O[i][0]), Storage<Elem>::from_f32(O[i][1]),
                                         Storage<Elem>::from_f32(O[i][2]), Storage<Elem>::from_f32(O[i][3])};
-                        const int c = 4 * wave + g;
-                        auto* run = &lds.own.outputs[16 * i + m][output_run(16 * i + m, c / kPer)];
+                        auto* run = &lds.own.outputs[(t & 1) * T * RUNS + output_at<RUNS>(16 * i + m, c / kPer)];
                         reinterpret_cast<Four*>(run)[c % kPer] = four;
                     }
                 }
@@ -533,14 +537,31 @@ void attention_kernel(Args a) {
         return;
     }
 
+    // a tile's outputs, whole lines of them, by NT threads
+    auto put = [&](const auto& own, auto* y, int32_t t, int tid, auto threads) {
+        using Out = std::remove_pointer_t<decltype(y)>;
+        constexpr int V = Vec<Out>::V, RUNS = VB / V, PER = threads() / RUNS;
+        const int run = tid % RUNS, valid = min(V, vd - v0 - run * V), rows = rows_of(t);
+        const auto* from = own.outputs + (std::is_same_v<Out, Elem> ? (t & 1) * T * RUNS : 0);
+        if (valid <= 0) return;
+        y += n * pass.y.sn + h * pass.y.sh + row_of(t) * pass.y.sl + v0 + run * V;
+#pragma unroll
+        for (int u = 0; u < T / PER; ++u) {
+            const int row = tid / RUNS + u * PER;
+            if (row < rows) store_run<Out, false>(y + row * pass.y.sl, valid, from[output_at<RUNS>(row, run)]);
+        }
+    };
+
     if (STATES || wave < W + W / 2) {   // memory
         const int tid = threadIdx.x - 64 * W;
         TileLoad<Elem, T, KD, Sh::kMemory> lq(tid, heads_at<Elem>(pass.q, n, h), pass.q.sl, 0, kd);
         TileLoad<Elem, T, KD, Sh::kMemory> lk(tid, heads_at<Elem>(pass.k, n, h), pass.k.sl, 0, kd);
         TileLoad<Elem, T, VB, Sh::kMemory> lv(tid, heads_at<Elem>(pass.v, n, h), pass.v.sl, v0, vd);
-        auto load = [&](int32_t t) {
+        auto load_k = [&](int32_t t) {
+            if (t < t_end) lk.load(row_of(t), rows_of(t), kd);
+        };
+        auto load_others = [&](int32_t t) {
             if (t >= t_end) return;
-            lk.load(row_of(t), rows_of(t), kd);
             if constexpr (!STATES) lq.load(row_of(t), rows_of(t), kd);
             lv.load(row_of(t), rows_of(t), vd);
         };
@@ -560,43 +581,30 @@ void attention_kernel(Args a) {
                 if (!lv.finite()) lds.own.odd[t & 1] = t + 1;
             lv.template store<PI>(to.v);
         };
-        // a tile's outputs, whole lines of them
-        auto put = [&](const auto& own, auto* y, int32_t t) {
-            using Out = std::remove_pointer_t<decltype(y)>;
-            constexpr int V = Vec<Out>::V, RUNS = VB / V, PER = Sh::kMemory / RUNS;
-            const int run = tid % RUNS, valid = min(V, vd - v0 - run * V), rows = rows_of(t);
-            if (valid <= 0) return;
-            y += n * pass.y.sn + h * pass.y.sh + row_of(t) * pass.y.sl + v0 + run * V;
-#pragma unroll
-            for (int u = 0; u < T / PER; ++u) {
-                const int row = tid / RUNS + u * PER;
-                if (row < rows) store_run<Out, false>(y + row * pass.y.sl, valid, own.outputs[row][output_run(row, run)]);
-            }
-        };
-        load(t_first);
+        if (STAGES == 2 && any) {
+            load_k(t_first);
+            load_others(t_first);
+        }
         if (!STATES && any) __syncthreads();   // the weights' waves have cleared odd
-        unpack(t_first);
-        if (any) __syncthreads();
-        if constexpr (STAGES == 2) load(t_first + 1);
-        if (!STATES && any) __syncthreads();
         int decays_of = 0;
-        for (int32_t t = t_first; t < t_end; ++t) {
-            if (STATES && rows_of(t) != decays_of) {   // they are set by the waves of the state
+        for (int32_t t = t_first - 1; t < t_end; ++t) {
+            if (STATES && t >= t_first && rows_of(t) != decays_of) {   // they are set by the waves of the state
                 decays_of = rows_of(t);
                 __syncthreads();
             }
             if constexpr (STAGES == 2) unpack(t + 1);
-            if constexpr (!STATES) __syncthreads();
-            load(t + STAGES);
-            if constexpr (!STATES) {
-                if (y_f32) put(lds.own, static_cast<float*>(pass.y.p), t);
-                else put(lds.own, static_cast<Elem*>(pass.y.p), t);
-            }
-            __syncthreads();
+            load_k(t + STAGES);
+            if constexpr (!STATES)
+                if (any) __syncthreads();
+            load_others(t + STAGES);
+            if constexpr (!STATES)
+                if (y_f32 && t >= t_first) put(lds.own, static_cast<float*>(pass.y.p), t, tid, [] { return Sh::kMemory; });
+            if (any) __syncthreads();
             if constexpr (STAGES == 1) {
                 unpack(t + 1);
-                __syncthreads();
-                if constexpr (!STATES) __syncthreads();
+                if (any) __syncthreads();
+                if constexpr (!STATES)
+                    if (any) __syncthreads();
             }
         }
         if constexpr (STATES) return;
@@ -612,13 +620,17 @@ void attention_kernel(Args a) {
         return;
     }
 
-    // the weights
-    if constexpr (!STATES) {
+    if constexpr (!STATES) {   // outputs and weights
+        if (!any) return;
+        const int tid = threadIdx.x - 96 * W, own_wave = wave - W - W / 2;
         auto weigh = [&](int32_t t) {
             if (t >= t_end) return;
             const auto& now = stage_of(t);
             // in blocks of 16 x 16 of the triangle
-            for (int blk = wave - W - W / 2; blk < BLOCKS; blk += W / 2) {
+#pragma unroll
+            for (int first = 0; first < BLOCKS; first += W / 2) {
+                const int blk = first + own_wave;
+                if (first + W / 2 > BLOCKS && blk >= BLOCKS) break;
                 const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
                 const int ib = reverse ? near : far, jb = reverse ? far : near;
                 f32x4 w[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
@@ -645,15 +657,12 @@ void attention_kernel(Args a) {
             }
         };
         // weights above the diagonal are zeros that nothing writes
-        const int tid = threadIdx.x - 96 * W;
         for (int i = tid; i < static_cast<int>(sizeof(lds.own.weights) / 4); i += Sh::kWeights)
             reinterpret_cast<uint32_t*>(&lds.own.weights)[i] = 0;
         if (tid < 2) lds.own.odd[tid] = 0;
-        if (any) __syncthreads();
-        if (any) __syncthreads();
-        weigh(t_first);
-        if (any) __syncthreads();
-        for (int32_t t = t_first; t < t_end; ++t) {
+        __syncthreads();
+        for (int32_t t = t_first - 1; t < t_end; ++t) {
+            if (!y_f32 && t > t_first) put(lds.own, static_cast<Elem*>(pass.y.p), t - 1, tid, [] { return Sh::kWeights; });
             __syncthreads();
             if constexpr (STAGES == 2) weigh(t + 1);
             __syncthreads();
@@ -663,6 +672,7 @@ void attention_kernel(Args a) {
                 __syncthreads();
             }
         }
+        if (!y_f32) put(lds.own, static_cast<Elem*>(pass.y.p), t_end - 1, tid, [] { return Sh::kWeights; });
     }
 }
 
