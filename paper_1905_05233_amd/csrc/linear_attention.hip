@@ -129,7 +129,8 @@ template <int P, int V, bool FINITE> struct Split {
             float a = x[e], b = x[e + 1];
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const uint32_t w = __builtin_bit_cast(uint32_t, Pair{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+                uint32_t w = __builtin_bit_cast(uint32_t, Pair{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+                asm("" : "+v"(w));   // else the compiler converts a once more for what follows
                 Words words = __builtin_bit_cast(Words, part[p]);
                 words[e / 2] = w;
                 part[p] = __builtin_bit_cast(Run, words);
@@ -161,35 +162,63 @@ __device__ __forceinline__ void multiply(A&& a, B&& b, f32x4 (&c)[COUNT]) {
 }
 
 // Rows of a tile in LDS, one plane a part, in runs of 8 channels whose order changes from
-// row to row: the 16 rows that a fragment reads the same run of, and the four rows and
-// runs that a transposing read takes, fall on different banks.
-template <int PLANES, int ROWS, int WIDTH> struct alignas(16) TileLds {
-    static constexpr int kRuns = WIDTH / 8;
-    uint16_t v[PLANES][ROWS][WIDTH];
+// row to row, so that every read below is free of bank conflicts: of 16 bytes a lane, for
+// which lanes m + 16 g meet those of m / 4 = 0, 3 with g even and 1, 2 with g odd, and the
+// other way around; of 8 bytes, for which 32 lanes meet.  A place is the byte of a lane's
+// channel c in a row, from the tile's first plane on or from LDS's start on; that of a
+// channel c + d, where d is a multiple of 8 of bits that c has not, is place ^ 2 d, and
+// that of 16 rows on place + 32 WIDTH.
+template <int PLANES, int ROWS, int WIDTH> struct alignas(512) TileLds {
+    static constexpr int kRuns = WIDTH / 8, kPlane = 2 * ROWS * WIDTH;
+    uint16_t v[PLANES][ROWS * WIDTH];
 
-    static __device__ __forceinline__ int at(int row, int c) {
-        const int by4 = row >> 2 & 3;
+    static __device__ __forceinline__ int place(int row, int c) {
+        const int high = row >> 3 & 1, by4 = (high ^ (row >> 2 & 1)) << 1 | high;
         const int mix = kRuns >= 16 ? (row & 3) << 2 | by4 : kRuns == 8 ? (row & 2) << 1 | by4 : by4;
-        return (c / 8 ^ mix) * 8 + c % 8;
+        return 2 * (row * WIDTH + (c / 8 ^ mix) * 8 + c % 8);
     }
-    // 8 channels from c of a row, as a matrix instruction takes them of its row (or
-    // column) `row`: lane m + 16 g holds 8 g .. 8 g + 7 of row m
-    __device__ __forceinline__ void across(int row, int c, bf16x8 (&f)[PLANES]) const {
+    __device__ __forceinline__ int start() const {
+        return static_cast<int>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint16_t*)&v[0][0]));
+    }
+    template <typename T> __device__ __forceinline__ T& at(int place, int plane) {
+        return *reinterpret_cast<T*>(reinterpret_cast<char*>(&v[plane][0]) + place);
+    }
+    __device__ __forceinline__ float value(int row, int c) const {
+        float sum = 0.0f;
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p) f[p] = *reinterpret_cast<const bf16x8*>(&v[p][row][at(row, c)]);
+        for (int p = PLANES - 1; p >= 0; --p) sum += __uint_as_float(static_cast<uint32_t>(v[p][place(row, c) / 2]) << 16);
+        return sum;
     }
-    // 8 rows from `row` of a channel: the lanes of 16 hand in the places of four
-    // channels in each of four rows, and lane m gets the four rows of channel m
-    __device__ __forceinline__ void down(int row, int c, bf16x8 (&f)[PLANES]) const {
+
+    // Reads at places from LDS's start on; what is added to a place goes into the
+    // instruction.
+    template <typename T> static __device__ __forceinline__ T read(int place) {
+        return *(const __attribute__((address_space(3))) T*)(static_cast<uint32_t>(place));
+    }
+    // 8 channels, as a matrix instruction takes them of its row (or column): lane m + 16 g
+    // holds those from 8 g on of row m
+    static __device__ __forceinline__ void across(int place, bf16x8 (&f)[PLANES]) {
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) f[p] = read<bf16x8>(place + p * kPlane);
+    }
+    // 8 rows of a channel: the lanes of 16 hand in the places of four channels in each of
+    // four rows, and of the four rows behind them, and lane m gets the rows of channel m
+    static __device__ __forceinline__ void down(int place, int behind, bf16x8 (&f)[PLANES]) {
         using At = __attribute__((address_space(3))) s16x4*;
 #pragma unroll
         for (int p = 0; p < PLANES; ++p) {
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row][at(row, c)]));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(&v[p][row + 4][at(row + 4, c)]));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(static_cast<uint32_t>(place + p * kPlane)));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(static_cast<uint32_t>(behind + p * kPlane)));
             f[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
 };
+// A place that the compiler takes to be a new one: it makes those that follow from it anew,
+// by one operation each, instead of holding them in registers.
+__device__ __forceinline__ int renewed(int place) {
+    asm volatile("" : "+v"(place));
+    return place;
+}
 
 // A tile's rows on their way from memory: 16 bytes of U rows a thread.  Every thread
 // loads, from the first row and from the end of its row's channels where it has none of
@@ -213,6 +242,11 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
     // rows 0 .. live - 1 (at least one) from row t0 of the sequence
     __device__ __forceinline__ void load(int32_t t0, int live, int D) {
         const Elem* p = base + t0 * stride;
+        if (D >= V && live == ROWS && ROWS % kPer == 0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = reinterpret_cast<const Bytes16*>(p + u * kPer * stride)->v;
+            return;
+        }
         if (D >= V) {
             const Elem* first = p - r0 * stride;
 #pragma unroll
@@ -256,21 +290,30 @@ template <typename Elem, int ROWS, int WIDTH, int THREADS> struct TileLoad {
             if (r0 + u * kPer >= live) raw[u] = u32x4{0, 0, 0, 0};
         }
     }
-    template <int PLANES> __device__ __forceinline__ void store(TileLds<PLANES, ROWS, WIDTH>& to) const {
+    // SWAP: rows from 8 on of every 16 with the halves of their runs of 8 channels exchanged
+    template <bool SWAP, int PLANES> __device__ __forceinline__ void store(TileLds<PLANES, ROWS, WIDTH>& to) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int row = r0 + u * kPer;
             if (ROWS % kPer != 0 && row >= ROWS) continue;
+            const bool swap = SWAP && row & 8;
             if constexpr (PLANES == 1) {
-                *reinterpret_cast<u32x4*>(&to.v[0][row][to.at(row, run)]) = raw[u];
+                const u32x4 w = swap ? u32x4{raw[u][2], raw[u][3], raw[u][0], raw[u][1]} : raw[u];
+                to.template at<u32x4>(to.place(row, run), 0) = w;
             } else {
                 float x[V];
                 Vec<Elem>::widen(raw[u], x);
                 Split<PLANES, V, true> s;
                 s.of(x);
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p)
-                    *reinterpret_cast<typename Split<PLANES, V, true>::Run*>(&to.v[p][row][to.at(row, run)]) = s.part[p];
+                for (int p = 0; p < PLANES; ++p) {
+                    if constexpr (V == 8) {
+                        const u32x4 w = __builtin_bit_cast(u32x4, s.part[p]);
+                        to.template at<u32x4>(to.place(row, run), p) = swap ? u32x4{w[2], w[3], w[0], w[1]} : w;
+                    } else {
+                        to.template at<bf16x4>(to.place(row, run) ^ (swap ? 8 : 0), p) = s.part[p];
+                    }
+                }
             }
         }
     }
@@ -330,11 +373,11 @@ template <typename Elem, int K, int W, bool STATES> struct Shape {
     };
     // W waves for the state, half as many for memory and, but for STATES, as many for the weights
     static constexpr int kMemory = 32 * W, kWeights = STATES ? 0 : 32 * W, kThreads = 64 * W + kMemory + kWeights;
-    static constexpr int kWavesPerSimd = 2 * sizeof(Lds) <= kLdsBytes || W == 8 ? 4 : 2;
+    static constexpr int kWavesPerSimd = W == 8 ? 4 : K <= 64 ? (2 * sizeof(Lds) <= kLdsBytes ? 4 : 2) : STATES && K == 128 ? 3 : 2;
 };
 // Where run `run` of 16 bytes of a row of outputs stands, of RUNS a row: the order changes
 // from row to row.
-template <int RUNS> __device__ __forceinline__ int output_at(int row, int run) { return row * RUNS + (run ^ (row & (RUNS < 8 ? RUNS - 1 : 7))); }
+template <int RUNS> __device__ __forceinline__ int output_at(int row, int run) { return row * RUNS + (run ^ (row & (RUNS < 16 ? RUNS - 1 : 15))); }
 
 // A pass, or (STATES) only what its segments add to the state.  The waves of a workgroup
 // have three tasks, so that some work where others wait:
@@ -350,11 +393,15 @@ template <int RUNS> __device__ __forceinline__ int output_at(int row, int run) {
 //
 // S[b], lane m + 16 g, register r is the state at (32 (b / 2) + 8 g + 4 (b % 2) + r,
 // 16 wave + m), so that those of two blocks side by side are the 8 consecutive rows that a
-// lane hands a matrix instruction, without a move.  Outputs come transposed, O[i] with row
-// 16 i + m and columns 16 wave + 4 g + r.
+// lane hands a matrix instruction, without a move.  The transposing reads of k then take 8
+// bytes of every run of 16; k's rows from 8 on of every 16 stand with the halves of their
+// runs in exchanged order (SWAP), so that both halves' banks are in use.  Outputs come
+// transposed, O[i] with row 16 i + m and columns 16 wave + 4 g + r.
 template <typename Elem, int KD, int W, bool STATES>
 __global__ __launch_bounds__((Shape<Elem, KD, W, STATES>::kThreads), (Shape<Elem, KD, W, STATES>::kWavesPerSimd))
-void attention_kernel(Args a) {
+void attention_kernel(Args) {
+    // the arguments where the launch left them: the compiler keeps a large copy in scratch memory
+    const Args& a = *(const Args*)__builtin_amdgcn_kernarg_segment_ptr();
     using Sh = Shape<Elem, KD, W, STATES>;
     constexpr int T = Sh::T, PI = Sh::PI, PS = Sh::PS, VB = Sh::kColumns, IB = T / 16, JS = T / 32, KS = KD / 32;
     constexpr int STAGES = Sh::kStages, BLOCKS = IB * (IB + 1) / 2;
@@ -381,8 +428,6 @@ void attention_kernel(Args a) {
     const bool any = t_first < t_end;
 
     if (wave < W) {   // the state
-        // channels that a lane hands to a transposing read of k
-        auto row_chunk = [&](int b) { return 32 * (b / 2) + 8 * (m % 4) + 4 * (b % 2); };
         f32x4 S[KD / 16];
         auto each_state = [&](auto&& f) {
 #pragma unroll
@@ -400,6 +445,16 @@ void attention_kernel(Args a) {
             const float* s = pass.s_in + (pass.from_segments ? by_segment : head * size);
             each_state([&](float, int at) { return s[at]; });
         }
+        using K = decltype(lds.steps[0].k);
+        using V = decltype(lds.steps[0].v);
+        // places of q, and of k and v for four rows and the four behind them
+        const int q_own = K::place(m, 8 * g);
+        int k_own[2], v_own[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            k_own[u] = K::place(8 * g + m / 4 + 4 * u, 8 * (m % 4)) ^ 8 * (g % 2);
+            v_own[u] = V::place(8 * g + m / 4 + 4 * u, 16 * wave + 4 * (m % 4));
+        }
         float whole = 1.0f, out_decay[IB];   // the decays over a tile, and from the state to its steps
         int decays_of = 0;
         if (any) {                           // the first tile and its weights
@@ -409,6 +464,7 @@ void attention_kernel(Args a) {
         for (int32_t t = t_first; t < t_end; ++t) {
             const auto& now = stage_of(t);
             const int live = rows_of(t);
+            const int v_place[2] = {now.v.start() + v_own[0], now.v.start() + v_own[1]};
             if (live != decays_of) {
                 decays_of = live;
                 whole = exact_power(log_decay, live);
@@ -421,6 +477,7 @@ void attention_kernel(Args a) {
             }
             if constexpr (!STATES) {
                 const bool odd = lds.own.odd[t & 1] == t + 1;
+                const int q_place = now.q.start() + q_own;
                 f32x4 O[IB];
 #pragma unroll
                 for (int i = 0; i < IB; ++i) O[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -432,23 +489,26 @@ void attention_kernel(Args a) {
                     for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][e % 4];
                     fs.of(x);
                     bf16x8 fq[IB][PI];
+                    const int place = renewed(q_place) ^ 64 * s;
 #pragma unroll
-                    for (int i = 0; i < IB; ++i) now.q.across(16 * i + m, 32 * s + 8 * g, fq[i]);
+                    for (int i = 0; i < IB; ++i) now.q.across(place + 32 * i * KD, fq[i]);
                     multiply<PS, PI, PS>([&](int, int p) { return fs.part[p]; }, [&](int i, int p) { return fq[i][p]; }, O);
                 }
 #pragma unroll
                 for (int i = 0; i < IB; ++i) O[i] *= out_decay[i];
                 if (!odd) {
+                    using P = decltype(lds.own.weights);
+                    const int p_place = lds.own.weights.start() + P::place(m, 8 * g);
 #pragma unroll
                     for (int s = 0; s < JS; ++s) {
                         bf16x8 fv[PI];
-                        now.v.down(32 * s + 8 * g + m / 4, 16 * wave + 4 * (m % 4), fv);
+                        now.v.down(v_place[0] + 64 * s * VB, v_place[1] + 64 * s * VB, fv);
 #pragma unroll
                         for (int i = 0; i < IB; i += 2) {
                             if (reverse ? s < i / 2 : s > i / 2) continue;
                             bf16x8 fp[2][PS];
-                            lds.own.weights.across(32 * (i / 2 + s) + m, 8 * g, fp[0]);
-                            lds.own.weights.across(32 * (i / 2 + s) + 16 + m, 8 * g, fp[1]);
+                            P::across(p_place + 64 * (i / 2 + s) * 32, fp[0]);
+                            P::across(p_place + 64 * (i / 2 + s) * 32 + 32 * 32, fp[1]);
                             f32x4 pair[2] = {O[i], O[i + 1]};
                             multiply<PI, PS, PS>([&](int, int p) { return fv[p]; }, [&](int u, int p) { return fp[u][p]; }, pair);
                             O[i] = pair[0], O[i + 1] = pair[1];
@@ -456,22 +516,15 @@ void attention_kernel(Args a) {
                     }
                 } else {
                     // step by step: a weight of zero would not remove an infinity or NaN of a later v
-                    auto value = [](const auto& tile, int row, int c) {
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int p = std::extent_v<std::remove_reference_t<decltype(tile.v)>> - 1; p >= 0; --p)
-                            sum += __uint_as_float(static_cast<uint32_t>(tile.v[p][row][tile.at(row, c)]) << 16);
-                        return sum;
-                    };
 #pragma unroll 1
                     for (int j = 0; j < T; ++j)
 #pragma unroll
                         for (int i = 0; i < IB; ++i) {
                             const int row = 16 * i + m;
                             if (reverse ? j < row : j > row) continue;
-                            const float w = value(lds.own.weights, 32 * (i / 2 + j / 32) + 16 * (i % 2) + m, j % 32);
+                            const float w = lds.own.weights.value(32 * (i / 2 + j / 32) + 16 * (i % 2) + m, j % 32);
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) O[i][r] += w * value(now.v, j, 16 * wave + 4 * g + r);
+                            for (int r = 0; r < 4; ++r) O[i][r] += w * now.v.value(j, 16 * wave + 4 * g + r);
                         }
                 }
                 const int c = 4 * wave + g;
@@ -486,8 +539,15 @@ void attention_kernel(Args a) {
                     constexpr int kPer = 16 / sizeof(Four), RUNS = VB * sizeof(Elem) / 16;
 #pragma unroll
                     for (int i = 0; i < IB; ++i) {
-                        const Four four{Storage<Elem>::from_f32(O[i][0]), Storage<Elem>::from_f32(O[i][1]),
-                                        Storage<Elem>::from_f32(O[i][2]), Storage<Elem>::from_f32(O[i][3])};
+                        Four four;
+                        if constexpr (std::is_same_v<Elem, bf16_t>) {   // in pairs
+                            const bf16x4 e = {static_cast<__bf16>(O[i][0]), static_cast<__bf16>(O[i][1]), static_cast<__bf16>(O[i][2]),
+                                              static_cast<__bf16>(O[i][3])};
+                            four = __builtin_bit_cast(Four, e);
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) four.v[r] = Storage<Elem>::from_f32(O[i][r]);
+                        }
                         auto* run = &lds.own.outputs[(t & 1) * T * RUNS + output_at<RUNS>(16 * i + m, c / kPer)];
                         reinterpret_cast<Four*>(run)[c % kPer] = four;
                     }
@@ -496,30 +556,37 @@ void attention_kernel(Args a) {
             }
 #pragma unroll
             for (int b = 0; b < KD / 16; ++b) S[b] *= whole;
+            Split<kStateParts, 8, false> late[JS];
 #pragma unroll
             for (int s = 0; s < JS; ++s) {
                 bf16x8 fv[PI];
-                now.v.down(32 * s + 8 * g + m / 4, 16 * wave + 4 * (m % 4), fv);
-                Split<kStateParts, 8, false> late;
+                now.v.down(v_place[0] + 64 * s * VB, v_place[1] + 64 * s * VB, fv);
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float sum = 0.0f;
+                    float sum = static_cast<float>(fv[PI - 1][e]);
 #pragma unroll
-                    for (int p = PI - 1; p >= 0; --p) sum += static_cast<float>(fv[p][e]);
+                    for (int p = PI - 2; p >= 0; --p) sum += static_cast<float>(fv[p][e]);
                     x[e] = sum * lds.in_decay[32 * s + 8 * g + e];
                 }
-                late.of(x);
+                late[s].of(x);
+            }
+            const int k_place[2] = {now.k.start() + k_own[0], now.k.start() + k_own[1]};
 #pragma unroll
-                for (int b = 0; b < KD / 16; b += 2) {
+            for (int b = 0; b < KD / 16; b += 2) {
+                f32x4 pair[2] = {S[b], S[b + 1]};
+                int own[2][2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) own[u][0] = renewed(k_place[0]) ^ (32 * b + 8 * u), own[u][1] = renewed(k_place[1]) ^ (32 * b + 8 * u);
+#pragma unroll
+                for (int s = 0; s < JS; ++s) {
                     bf16x8 fk[2][PI];
-                    now.k.down(32 * s + 8 * g + m / 4, row_chunk(b), fk[0]);
-                    now.k.down(32 * s + 8 * g + m / 4, row_chunk(b + 1), fk[1]);
-                    f32x4 pair[2] = {S[b], S[b + 1]};
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) now.k.down(own[u][0] + 64 * s * KD, own[u][1] + 64 * s * KD, fk[u]);
                     multiply<PI, kStateParts, kStateParts>([&](int i, int p) { return fk[i][p]; },
-                                                           [&](int, int p) { return late.part[p]; }, pair);
-                    S[b] = pair[0], S[b + 1] = pair[1];
+                                                           [&](int, int p) { return late[s].part[p]; }, pair);
                 }
+                S[b] = pair[0], S[b + 1] = pair[1];
             }
             __syncthreads();
             if constexpr (STAGES == 1) {
@@ -571,15 +638,15 @@ void attention_kernel(Args a) {
             const bool whole = kd == KD && vd - v0 >= VB && rows == T;
             auto& to = stage_of(t);
             lk.trim(whole, rows, kd);
-            lk.template store<PI>(to.k);
+            lk.template store<true, PI>(to.k);
             if constexpr (!STATES) {
                 lq.trim(whole, rows, kd);
-                lq.template store<PI>(to.q);
+                lq.template store<false, PI>(to.q);
             }
             lv.trim(whole, rows, vd);
             if constexpr (!STATES)
                 if (!lv.finite()) lds.own.odd[t & 1] = t + 1;
-            lv.template store<PI>(to.v);
+            lv.template store<false, PI>(to.v);
         };
         if (STAGES == 2 && any) {
             load_k(t_first);
@@ -623,37 +690,66 @@ void attention_kernel(Args a) {
     if constexpr (!STATES) {   // outputs and weights
         if (!any) return;
         const int tid = threadIdx.x - 96 * W, own_wave = wave - W - W / 2;
+        const int own_place = decltype(lds.steps[0].k)::place(m, 8 * g);
         auto weigh = [&](int32_t t) {
             if (t >= t_end) return;
             const auto& now = stage_of(t);
-            // in blocks of 16 x 16 of the triangle
+            const int k_place = now.k.start() + own_place, q_place = now.q.start() + own_place;
+            // in blocks of 16 x 16 of the triangle, two at a time
 #pragma unroll
-            for (int first = 0; first < BLOCKS; first += W / 2) {
-                const int blk = first + own_wave;
-                if (first + W / 2 > BLOCKS && blk >= BLOCKS) break;
-                const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
-                const int ib = reverse ? near : far, jb = reverse ? far : near;
-                f32x4 w[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+            for (int first = 0; first < BLOCKS; first += W) {
+                constexpr int kHalf = W / 2;
+                const bool two = first + kHalf < BLOCKS;
+                int ib[2], jb[2];
+                bool has[2];
+                f32x4 w[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int own = first + own_wave + u * kHalf;
+                    has[u] = own < BLOCKS;
+                    const int blk = has[u] ? own : 0;
+                    const int far = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, near = blk - far * (far + 1) / 2;
+                    ib[u] = reverse ? near : far, jb[u] = reverse ? far : near;
+                    w[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+                if (!has[0]) break;
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    bf16x8 fk[PI], fq[PI];
-                    now.k.across(16 * jb + m, 32 * s + 8 * g, fk);
-                    now.q.across(16 * ib + m, 32 * s + 8 * g, fq);
-                    multiply<PI, PI, PS>([&](int, int p) { return fk[p]; }, [&](int, int p) { return fq[p]; }, w);
-                }
-                float x[4];
-                const int d0 = reverse ? 16 * (jb - ib) + 4 * g - m : 16 * (ib - jb) + m - 4 * g;
+                    bf16x8 fk[2][PI], fq[2][PI];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = reverse ? d0 + r : d0 - r;
-                    x[r] = d < 0 ? 0.0f : w[0][r] * (a.scale * power(log2_decay, d));
-                }
-                Split<PS, 4, false> parts;
-                parts.of(x);
-                auto& to = lds.own.weights;
-                const int row = 32 * (ib / 2 + jb / 2) + 16 * (ib % 2) + m, c = 16 * (jb % 2) + 4 * g;
+                    for (int u = 0; u < 2; ++u) {
+                        if (u == 1 && !two) continue;
+                        now.k.across((k_place + 32 * jb[u] * KD) ^ 64 * s, fk[u]);
 #pragma unroll
-                for (int p = 0; p < PS; ++p) *reinterpret_cast<bf16x4*>(&to.v[p][row][to.at(row, c)]) = parts.part[p];
+                        for (int p = 0; p < PI; ++p)   // rows whose halves are exchanged
+                            if (m & 8) fk[u][p] = __builtin_shufflevector(fk[u][p], fk[u][p], 4, 5, 6, 7, 0, 1, 2, 3);
+                        now.q.across((q_place + 32 * ib[u] * KD) ^ 64 * s, fq[u]);
+                    }
+                    if (two) {
+                        multiply<PI, PI, PS>([&](int u, int p) { return fk[u][p]; }, [&](int u, int p) { return fq[u][p]; }, w);
+                    } else {
+                        f32x4 one[1] = {w[0]};
+                        multiply<PI, PI, PS>([&](int, int p) { return fk[0][p]; }, [&](int, int p) { return fq[0][p]; }, one);
+                        w[0] = one[0];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if (!has[u] || (u == 1 && !two)) continue;
+                    float x[4];
+                    const int d0 = reverse ? 16 * (jb[u] - ib[u]) + 4 * g - m : 16 * (ib[u] - jb[u]) + m - 4 * g;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int d = reverse ? d0 + r : d0 - r;
+                        x[r] = d < 0 ? 0.0f : w[u][r] * (a.scale * power(log2_decay, d));
+                    }
+                    Split<PS, 4, false> parts;
+                    parts.of(x);
+                    auto& to = lds.own.weights;
+                    const int row = 32 * (ib[u] / 2 + jb[u] / 2) + 16 * (ib[u] % 2) + m, c = 16 * (jb[u] % 2) + 4 * g;
+#pragma unroll
+                    for (int p = 0; p < PS; ++p) to.template at<bf16x4>(to.place(row, c), p) = parts.part[p];
+                }
             }
         };
         // weights above the diagonal are zeros that nothing writes
