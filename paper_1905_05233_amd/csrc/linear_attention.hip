@@ -597,7 +597,7 @@ void attention_kernel(Args) {
         if constexpr (STATES) {
             float* s = pass.s_out + by_segment;
             each_state([&](float x, int at) { return s[at] = x; });
-        } else if (pass.s_out) {
+        } else if (pass.s_out && segment == a.segments - 1) {
             float* s = pass.s_out + head * size;
             each_state([&](float x, int at) { return s[at] = x; });
         }
@@ -772,12 +772,11 @@ void attention_kernel(Args) {
     }
 }
 
-// The states ahead of the segments from what each adds: in place, [N][H][segments] of
-// `size` values, from s_in [N][H] (or null: zeros) to s_out (or null).
+// The states ahead of the segments from what each but the last adds: in place,
+// [N][H][segments] of `size` values, from s_in [N][H] (or null: zeros).
 struct Chain {
     float* states;
     const float* s_in;
-    float* s_out;
     int32_t size, reverse;
 };
 struct ChainArgs {
@@ -787,39 +786,37 @@ struct ChainArgs {
     const float* log_decay;
     const int32_t* lengths;
 };
-__global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
-    constexpr int U = 8;      // segments whose loads are in flight together
+// U: segments whose loads are in flight together.
+template <int U> __global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
     const Chain& c = a.chain[blockIdx.x % a.of];
-    const uint32_t unit = blockIdx.x / a.of;
-    const int64_t head = unit / a.blocks;
-    const int32_t i = static_cast<int32_t>(unit % a.blocks) * kThreads + threadIdx.x;
+    const uint32_t unit = blockIdx.x / a.of, head = unit / static_cast<uint32_t>(a.blocks);
+    const int32_t i = static_cast<int32_t>(unit - head * a.blocks) * kThreads + threadIdx.x;
+    const uint32_t n = head / static_cast<uint32_t>(a.H);
+    const int32_t steps = steps_of(a.lengths, n, a.L), last = (steps + a.tile - 1) / a.tile * a.tile - steps;
+    const float log_decay = a.log_decay[head - n * a.H];
     if (i >= c.size) return;
-    const int32_t steps = steps_of(a.lengths, head / a.H, a.L), end = (steps + a.tile - 1) / a.tile * a.tile;
-    const float log_decay = a.log_decay[head % a.H];
-    // steps of a segment: all but the last have each_steps, but the reverse of a walk
-    // begins with the tile that may be short
-    auto steps_in = [&](int32_t w) {
-        const int64_t from = static_cast<int64_t>(w) * a.each_steps, to = min(static_cast<int64_t>(end), from + a.each_steps);
-        if (from >= end) return 0;
-        return static_cast<int32_t>(c.reverse ? min(static_cast<int64_t>(steps), end - from) - (end - to)
-                                              : min(static_cast<int64_t>(steps), to) - from);
-    };
+    const int64_t size = c.size;
+    float* s = c.states + head * (a.segments * size) + i;
+    float run = c.s_in ? c.s_in[head * size + i] : 0.0f;
     const float whole = exact_power(log_decay, a.each_steps);
-    float* s = c.states + head * a.segments * static_cast<int64_t>(c.size) + i;
-    float run = c.s_in ? c.s_in[head * c.size + i] : 0.0f;
+    const int32_t adding = a.segments - 1;
     for (int32_t w = 0; w < a.segments; w += U) {
         float add[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) add[u] = w + u < a.segments ? s[(w + u) * static_cast<int64_t>(c.size)] : 0.0f;
+        for (int u = 0; u < U; ++u) add[u] = w + u < adding ? s[(w + u) * size] : 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (w + u >= a.segments) continue;
-            s[(w + u) * static_cast<int64_t>(c.size)] = run;
-            const int32_t count = steps_in(w + u);
+            if (w + u >= a.segments) break;
+            s[(w + u) * size] = run;
+            if (w + u >= adding) break;
+            // steps of the segment: all but the last have each_steps, but the reverse of a
+            // walk begins with the tile that may be short
+            const int64_t from = static_cast<int64_t>(w + u) * a.each_steps - (c.reverse && w + u > 0 ? last : 0);
+            const int64_t to = static_cast<int64_t>(w + u + 1) * a.each_steps - (c.reverse ? last : 0);
+            const int32_t count = static_cast<int32_t>(min(to, static_cast<int64_t>(steps)) - from);
             if (count > 0) run = fmaf(count == a.each_steps ? whole : exact_power(log_decay, count), run, add[u]);
         }
     }
-    if (c.s_out) c.s_out[head * c.size + i] = run;
 }
 
 // Gradients of an input that heads share: the sum over them of their parts
@@ -916,11 +913,17 @@ struct Cut {
     int kd, waves;            // channels of q and k, and waves that hold the state, of the kernel's form
     int32_t segments, each;   // tiles of a segment
 };
-// Segments, where the heads do not fill the chip: as many as make kUnits workgroups, of
-// kLeast tiles at least.
-constexpr int64_t kFull = 192, kUnits = 512, kLeast = 4;
 constexpr int columns_of(int waves) { return 16 * waves; }
 int64_t blocks_of(int vd, int waves) { return (vd + columns_of(waves) - 1) / columns_of(waves); }
+// Workgroups that a compute unit holds of a form: two where LDS has room, of 8 waves that
+// hold the state one, by its registers.
+constexpr bool holds_two(int dtype, int kd, int waves) { return waves == 4 && kd <= (dtype == kF32 ? 32 : 64); }
+
+// Segments shorten the walk where the heads do not fill the chip, and cost a pass over k
+// and v for the states ahead of them.  A form's time is taken as its rounds of workgroups,
+// each as many tiles long as a segment and kStart more; the states' pass as half a tile for
+// each; what joins them as kJoin.  The cuts that fill one to kRounds rounds are compared.
+constexpr int64_t kStart = 3, kJoin = 4, kRounds = 4;   // in halves of a tile's time
 Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
     int kd = 0, vd = 0;
     for (int p = 0; p < passes; ++p) kd = std::max(kd, dims[p][0]), vd = std::max(vd, dims[p][1]);
@@ -928,17 +931,24 @@ Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int
     const int tile = tile_steps(dtype == kBF16, c.kd);
     int64_t units = 0;
     for (int p = 0; p < passes; ++p) units += N * H * blocks_of(dims[p][1], c.waves);
-    const int64_t tiles = (L + tile - 1) / tile;
-    int64_t segments = 1;
-    if (units < kFull * passes && tiles >= 2 * kLeast) segments = std::min(tiles / kLeast, kUnits / units);
-    segments = std::max<int64_t>(1, segments);
-    c.each = static_cast<int32_t>(std::max<int64_t>(1, (tiles + segments - 1) / segments));
-    c.segments = static_cast<int32_t>(std::max<int64_t>(1, (tiles + c.each - 1) / c.each));
+    const int64_t tiles = std::max<int64_t>(1, (L + tile - 1) / tile);
+    c.each = static_cast<int32_t>(tiles);
+    if (units == 0) return c;
+    const int64_t room = int64_t(device_cu_count()) * (holds_two(dtype, c.kd, c.waves) ? 2 : 1);
+    auto rounds = [&](int64_t workgroups) { return (workgroups + room - 1) / room; };
+    const int64_t chains = std::max<int64_t>(1, units * std::min(passes, 2) / passes);
+    int64_t least = rounds(units) * (2 * tiles + kStart);
+    for (int64_t r = 1; r <= kRounds && units < r * room; ++r) {
+        const int64_t each = (tiles + r * room / units - 1) / (r * room / units), segments = (tiles + each - 1) / each;
+        if (segments == 1) continue;
+        const int64_t time = rounds(units * segments) * (2 * each + kStart) + rounds(chains * (segments - 1)) * (each + kStart) + kJoin;
+        if (time < least) least = time, c.each = static_cast<int32_t>(each), c.segments = static_cast<int32_t>(segments);
+    }
     return c;
 }
 
 // HIP takes fewer than 2^32 threads: more sequences than that go in several launches.
-hipError_t over_sequences(const Args& a, int passes, int dtype, int threads, void (*kernel)(Args), hipStream_t stream) {
+hipError_t over_sequences(const Args& a, int passes, int segments, int dtype, int threads, void (*kernel)(Args), hipStream_t stream) {
     int64_t per = 0;          // workgroups of a sequence
     for (int p = 0; p < passes; ++p) per += static_cast<int64_t>(a.H) * a.pass[p].blocks;
     const int64_t most = std::max<int64_t>(1, int64_t(0x7fffff) / per);
@@ -958,7 +968,7 @@ hipError_t over_sequences(const Args& a, int passes, int dtype, int threads, voi
             k.first[p + 1] = k.first[p] + static_cast<int32_t>(k.N * a.H * s.blocks);
         }
         for (int p = passes; p < 3; ++p) k.first[p + 1] = k.first[p];
-        kernel<<<static_cast<unsigned>(k.first[3]) * k.segments, threads, 0, stream>>>(k);
+        kernel<<<static_cast<unsigned>(k.first[3]) * segments, threads, 0, stream>>>(k);
     }
     return hipGetLastError();
 }
@@ -970,7 +980,7 @@ template <typename Elem, bool STATES> hipError_t run_passes(Args& a, int passes,
     a.segments = cut.segments, a.each = cut.each;
 #define WG_ATTENTION_CASE(K, W) \
     if constexpr (W == 4 || sizeof(Elem) == 2) \
-        if (cut.kd == K && cut.waves == W) return over_sequences(a, passes, dtype, Shape<Elem, K, W, STATES>::kThreads, attention_kernel<Elem, K, W, STATES>, stream);
+        if (cut.kd == K && cut.waves == W) return over_sequences(a, passes, STATES ? cut.segments - 1 : cut.segments, dtype, Shape<Elem, K, W, STATES>::kThreads, attention_kernel<Elem, K, W, STATES>, stream);
     WG_ATTENTION_SHAPES(WG_ATTENTION_CASE)
 #undef WG_ATTENTION_CASE
     return hipErrorInvalidValue;
@@ -987,7 +997,10 @@ hipError_t run_chains(Args a, const Chain* chains, int of, const Cut& cut, int d
     k.heads = a.N * a.H, k.L = a.L, k.H = a.H, k.segments = cut.segments;
     k.tile = tile_steps(dtype == kBF16, cut.kd), k.each_steps = cut.each * k.tile, k.blocks = (size + kThreads - 1) / kThreads, k.of = of;
     k.log_decay = a.log_decay, k.lengths = a.lengths;
-    chain_kernel<<<static_cast<unsigned>(k.heads * k.blocks * of), kThreads, 0, stream>>>(k);
+    const unsigned grid = static_cast<unsigned>(k.heads * k.blocks * of);
+    if (cut.segments <= 8) chain_kernel<8><<<grid, kThreads, 0, stream>>>(k);
+    else if (cut.segments <= 24) chain_kernel<24><<<grid, kThreads, 0, stream>>>(k);
+    else chain_kernel<64><<<grid, kThreads, 0, stream>>>(k);
     return hipGetLastError();
 }
 
@@ -1032,9 +1045,9 @@ template <int D> hipError_t launch_linear_attention_t(const wg_linear_attention&
     k.pass[0] = Pass{heads_in(a.q, a.q_heads, a.heads), heads_in(a.k, a.k_heads, a.heads), heads_in(a.v, a.v_heads, a.heads),
                      heads_out(a.y), Dk, Dv, 0, a.s0, a.s_last, {Dv, 1}, 1.0f, k.scale, 0, 0};
     if (cut.segments > 1) {
-        const Chain chain{static_cast<float*>(a.workspace), a.s0, a.s_last, Dk * Dv, 0};
+        const Chain chain{static_cast<float*>(a.workspace), a.s0, Dk * Dv, 0};
         if (const hipError_t e = run_chains<Elem>(k, &chain, 1, cut, D, stream)) return e;
-        k.pass[0].s_in = chain.states, k.pass[0].s_out = nullptr, k.pass[0].from_segments = 1;
+        k.pass[0].s_in = chain.states, k.pass[0].s_out = a.s_last, k.pass[0].from_segments = 1;
     }
     return run_passes<Elem, false>(k, 1, cut, D, stream);
 }
@@ -1054,8 +1067,8 @@ template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_a
     const float *s_in = a.s0, *g_in = a.ds_last;
     if (cut.segments > 1) {
         const size_t bytes = segment_bytes(cut, a.N, H, Dk, Dv);
-        const Chain chains[2] = {{reinterpret_cast<float*>(ws), a.s0, nullptr, Dk * Dv, 0},
-                                 {reinterpret_cast<float*>(ws + bytes), a.ds_last, a.ds0, Dk * Dv, 1}};
+        const Chain chains[2] = {{reinterpret_cast<float*>(ws), a.s0, Dk * Dv, 0},
+                                 {reinterpret_cast<float*>(ws + bytes), a.ds_last, Dk * Dv, 1}};
         ws += 2 * bytes;
         k.pass[0] = Pass{q, kk, v, {}, Dk, Dv, 0, nullptr, nullptr, {Dv, 1}, 1.0f, 1.0f, 0, 0};
         k.pass[1] = Pass{kk, q, dy, {}, Dk, Dv, 0, nullptr, nullptr, {Dv, 1}, k.scale, 1.0f, 1, 0};
@@ -1078,7 +1091,7 @@ template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_a
     const int32_t segmented = cut.segments > 1;
     k.pass[0] = Pass{dy, v, kk, to(0), Dv, Dk, 0, s_in, nullptr, {1, Dv}, 1.0f, k.scale, 0, segmented};
     k.pass[1] = Pass{v, dy, q, to(1), Dv, Dk, 0, g_in, nullptr, {1, Dv}, k.scale, 1.0f, 1, segmented};
-    k.pass[2] = Pass{kk, q, dy, to(2), Dk, Dv, 0, g_in, segmented ? nullptr : a.ds0, {Dv, 1}, k.scale, 1.0f, 1, segmented};
+    k.pass[2] = Pass{kk, q, dy, to(2), Dk, Dv, 0, g_in, a.ds0, {Dv, 1}, k.scale, 1.0f, 1, segmented};
     if (const hipError_t e = run_passes<Elem, false>(k, 3, cut, D, stream)) return e;
     for (int p = 0; p < 3; ++p) {
         const int64_t all = a.N * a.L * heads[p] * dims[p];
