@@ -278,8 +278,15 @@ __global__ __launch_bounds__(1024) void rotate_parts_kernel(const float* parts, 
     const int c = static_cast<int>(blockIdx.x) * kPartChannels + static_cast<int>(threadIdx.x) % kPartChannels;
     const int k = threadIdx.x / kPartChannels;
     float s = 0.0f;
+    constexpr int U = 16;   // loads in flight
     if (c < 2 * D)
-        for (int p = k; p < count; p += kSlices) s += parts[static_cast<int64_t>(p) * 2 * D + c];
+        for (int p = k; p < count; p += U * kSlices) {
+            float v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = p + u * kSlices < count ? parts[static_cast<int64_t>(p + u * kSlices) * 2 * D + c] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) s += v[u];
+        }
     lds[k][threadIdx.x % kPartChannels] = s;
     __syncthreads();
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;   // a wave a channel

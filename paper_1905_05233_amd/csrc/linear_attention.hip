@@ -429,22 +429,31 @@ void attention_kernel(Args) {
 
     if (wave < W) {   // the state
         f32x4 S[KD / 16];
-        auto each_state = [&](auto&& f) {
+        const int64_t size = static_cast<int64_t>(kd) * vd, by_segment = (static_cast<int64_t>(head) * a.segments + segment) * size;
+        const int column = v0 + 16 * wave + m, at_column = min(column, vd - 1) * pass.at.col;
+        auto row_of_state = [&](int b, int r) { return 32 * (b / 2) + 8 * g + 4 * (b % 2) + r; };
+        if (!STATES && pass.s_in) {
+            // every lane loads, from the last row and column where it has none: all in flight
+            const float* s = pass.s_in + (pass.from_segments ? by_segment : head * size) + at_column;
 #pragma unroll
             for (int b = 0; b < KD / 16; ++b)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 32 * (b / 2) + 8 * g + 4 * (b % 2) + r, j = v0 + 16 * wave + m;
-                    if (i < kd && j < vd) S[b][r] = f(S[b][r], i * pass.at.row + j * pass.at.col);
-                }
-        };
+                for (int r = 0; r < 4; ++r) S[b][r] = s[min(row_of_state(b, r), kd - 1) * pass.at.row];
 #pragma unroll
-        for (int b = 0; b < KD / 16; ++b) S[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const int64_t size = static_cast<int64_t>(kd) * vd, by_segment = (static_cast<int64_t>(head) * a.segments + segment) * size;
-        if (!STATES && pass.s_in) {
-            const float* s = pass.s_in + (pass.from_segments ? by_segment : head * size);
-            each_state([&](float, int at) { return s[at]; });
+            for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[b][r] = row_of_state(b, r) < kd && column < vd ? S[b][r] : 0.0f;
+        } else {
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b) S[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
+        auto store_state = [&](float* s) {
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (row_of_state(b, r) < kd && column < vd) s[row_of_state(b, r) * pass.at.row + at_column] = S[b][r];
+        };
         using K = decltype(lds.steps[0].k);
         using V = decltype(lds.steps[0].v);
         // places of q, and of k and v for four rows and the four behind them
@@ -594,13 +603,8 @@ void attention_kernel(Args) {
                 if constexpr (!STATES) __syncthreads();
             }
         }
-        if constexpr (STATES) {
-            float* s = pass.s_out + by_segment;
-            each_state([&](float x, int at) { return s[at] = x; });
-        } else if (pass.s_out && segment == a.segments - 1) {
-            float* s = pass.s_out + head * size;
-            each_state([&](float x, int at) { return s[at] = x; });
-        }
+        if constexpr (STATES) store_state(pass.s_out + by_segment);
+        else if (pass.s_out && segment == a.segments - 1) store_state(pass.s_out + head * size);
         return;
     }
 
@@ -819,19 +823,38 @@ template <int U> __global__ __launch_bounds__(kThreads) void chain_kernel(ChainA
     }
 }
 
-// Gradients of an input that heads share: the sum over them of their parts
-// [N][L][H][D] in fp32, in the order of the heads.
+// Gradients of inputs that heads share: the sums over them of their parts [N][L][H][D4]
+// in fp32 (D4 is D up to a multiple of 4), in the order of the heads.  A thread takes four
+// channels.
+struct Shared {
+    const float* part;
+    HeadsOut to;
+    int32_t heads, per, D;
+    int64_t first;            // of its work items among all
+};
+struct SharedArgs {
+    Shared of[3];
+    int32_t count, L;
+    int64_t items;
+};
 template <typename Elem>
-__global__ __launch_bounds__(kThreads) void shared_kernel(const float* part, HeadsOut to, int64_t rows, int32_t L, int32_t heads,
-                                                          int32_t per, int32_t D) {
-    const int64_t all = rows * heads * D, stride = static_cast<int64_t>(gridDim.x) * kThreads;
-    for (int64_t id = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; id < all; id += stride) {
-        const int64_t row = id / (heads * static_cast<int64_t>(D));
-        const int32_t h = id / D % heads, d = id % D;
-        const float* p = part + (row * heads + h) * per * D + d;
-        float sum = 0.0f;
-        for (int32_t u = 0; u < per; ++u) sum += p[static_cast<int64_t>(u) * D];
-        static_cast<Elem*>(to.p)[row / L * to.sn + row % L * to.sl + h * to.sh + d] = Storage<Elem>::from_f32(sum);
+__global__ __launch_bounds__(kThreads) void shared_kernel(SharedArgs a) {
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kThreads;
+    for (int64_t id = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; id < a.items; id += stride) {
+        int which = 0;
+        while (which + 1 < a.count && id >= a.of[which + 1].first) ++which;
+        const Shared& s = a.of[which];
+        const int32_t runs = (s.D + 3) / 4;
+        const int64_t item = id - s.first, row_head = item / runs, row = row_head / s.heads;
+        const int32_t run = static_cast<int32_t>(item - row_head * runs), h = static_cast<int32_t>(row_head - row * s.heads);
+        const f32x4* p = reinterpret_cast<const f32x4*>(s.part) + row_head * s.per * runs + run;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int32_t u = 0; u < s.per; ++u) sum += p[static_cast<int64_t>(u) * runs];
+        const int64_t n = row / a.L;
+        Elem* to = static_cast<Elem*>(s.to.p) + n * s.to.sn + (row - n * a.L) * s.to.sl + h * s.to.sh + 4 * run;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (4 * run + e < s.D) to[e] = Storage<Elem>::from_f32(sum[e]);
     }
 }
 
@@ -1006,7 +1029,7 @@ hipError_t run_chains(Args a, const Chain* chains, int of, const Cut& cut, int d
 
 // Bytes of the parts that an input's gradient is summed from: none where no heads share it.
 size_t part_bytes(int64_t N, int64_t L, int64_t heads, int64_t H, int64_t D) {
-    return heads == H ? 0 : static_cast<size_t>((N * L * H * D * 4 + 15) / 16 * 16);
+    return heads == H ? 0 : static_cast<size_t>(N * L * H * ((D + 3) / 4)) * 16;
 }
 
 // The passes' channels: of the attention itself, and of its gradients dq, dk and dv.
@@ -1086,19 +1109,24 @@ template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_a
     }
     auto to = [&](int p) {
         if (!parts[p]) return out[p];
-        return HeadsOut{const_cast<float*>(parts[p]), a.L * H * dims[p], H * dims[p], dims[p], 1};
+        const int64_t D4 = (dims[p] + 3) / 4 * 4;
+        return HeadsOut{const_cast<float*>(parts[p]), a.L * H * D4, H * D4, D4, 1};
     };
     const int32_t segmented = cut.segments > 1;
     k.pass[0] = Pass{dy, v, kk, to(0), Dv, Dk, 0, s_in, nullptr, {1, Dv}, 1.0f, k.scale, 0, segmented};
     k.pass[1] = Pass{v, dy, q, to(1), Dv, Dk, 0, g_in, nullptr, {1, Dv}, k.scale, 1.0f, 1, segmented};
     k.pass[2] = Pass{kk, q, dy, to(2), Dk, Dv, 0, g_in, a.ds0, {Dv, 1}, k.scale, 1.0f, 1, segmented};
     if (const hipError_t e = run_passes<Elem, false>(k, 3, cut, D, stream)) return e;
+    SharedArgs s{};
+    s.L = k.L;
     for (int p = 0; p < 3; ++p) {
-        const int64_t all = a.N * a.L * heads[p] * dims[p];
-        if (!parts[p] || all == 0) continue;
-        const int64_t blocks = std::min<int64_t>((all + kThreads - 1) / kThreads, 0xffffffffLL / kThreads);
-        shared_kernel<Elem><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(
-            parts[p], out[p], a.N * a.L, k.L, static_cast<int32_t>(heads[p]), static_cast<int32_t>(H / heads[p]), dims[p]);
+        if (!parts[p]) continue;
+        s.of[s.count++] = Shared{parts[p], out[p], static_cast<int32_t>(heads[p]), static_cast<int32_t>(H / heads[p]), dims[p], s.items};
+        s.items += a.N * a.L * heads[p] * ((dims[p] + 3) / 4);
+    }
+    if (s.items > 0) {
+        const int64_t blocks = std::min<int64_t>((s.items + kThreads - 1) / kThreads, 0xffffffffLL / kThreads);
+        shared_kernel<Elem><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(s);
     }
     return hipGetLastError();
 }
