@@ -974,7 +974,7 @@ Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int
 hipError_t over_sequences(const Args& a, int passes, int segments, int dtype, int threads, void (*kernel)(Args), hipStream_t stream) {
     int64_t per = 0;          // workgroups of a sequence
     for (int p = 0; p < passes; ++p) per += static_cast<int64_t>(a.H) * a.pass[p].blocks;
-    const int64_t most = std::max<int64_t>(1, int64_t(0x7fffff) / per);
+    const int64_t most = std::max<int64_t>(1, 0xffffffffLL / threads / (per * segments));
     for (int64_t n0 = 0; n0 < a.N; n0 += most) {
         Args k = a;
         k.N = std::min(a.N - n0, most);
