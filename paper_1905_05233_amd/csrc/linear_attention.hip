@@ -371,9 +371,14 @@ template <typename Elem, int K, int W, bool STATES> struct Shape {
     struct Lds : Least {
         Steps steps[kStages];
     };
-    // W waves for the state, half as many for memory and, but for STATES, as many for the weights
-    static constexpr int kMemory = 32 * W, kWeights = STATES ? 0 : 32 * W, kThreads = 64 * W + kMemory + kWeights;
-    static constexpr int kWavesPerSimd = W == 8 ? 4 : K <= 64 ? (2 * sizeof(Lds) <= kLdsBytes ? 4 : 2) : STATES && K == 128 ? 3 : 2;
+    // W waves for the state, half as many for memory and, but for STATES, as many for the
+    // weights.  Twice as many of these where inputs have several parts, if a compute unit
+    // holds one such workgroup: 16 x 1024 steps of 8 heads of 128 channels in fp32 152 to
+    // 109 us.  In fp16 with up to 64 channels of q and k two workgroups of 8 waves do more
+    // than one of 12: 64 x 1024 steps of 8 heads of 64 channels 96 and 175 us.
+    static constexpr int kHelpers = W == 4 && PI > 1 && !(PI == 2 && K <= 64) ? W : W / 2;
+    static constexpr int kMemory = 64 * kHelpers, kWeights = STATES ? 0 : 64 * kHelpers, kThreads = 64 * W + kMemory + kWeights;
+    static constexpr int kWavesPerSimd = W == 8 ? 4 : kHelpers == W ? (STATES ? 2 : 3) : K <= 64 ? (2 * sizeof(Lds) <= kLdsBytes ? 4 : 2) : STATES && K == 128 ? 3 : 2;
 };
 // Where run `run` of 16 bytes of a row of outputs stands, of RUNS a row: the order changes
 // from row to row.
@@ -623,7 +628,7 @@ void attention_kernel(Args) {
         }
     };
 
-    if (STATES || wave < W + W / 2) {   // memory
+    if (STATES || wave < W + Sh::kHelpers) {   // memory
         const int tid = threadIdx.x - 64 * W;
         TileLoad<Elem, T, KD, Sh::kMemory> lq(tid, heads_at<Elem>(pass.q, n, h), pass.q.sl, 0, kd);
         TileLoad<Elem, T, KD, Sh::kMemory> lk(tid, heads_at<Elem>(pass.k, n, h), pass.k.sl, 0, kd);
@@ -693,7 +698,7 @@ void attention_kernel(Args) {
 
     if constexpr (!STATES) {   // outputs and weights
         if (!any) return;
-        const int tid = threadIdx.x - 96 * W, own_wave = wave - W - W / 2;
+        const int tid = threadIdx.x - 64 * W - Sh::kMemory, own_wave = wave - W - Sh::kHelpers;
         const int own_place = decltype(lds.steps[0].k)::place(m, 8 * g);
         auto weigh = [&](int32_t t) {
             if (t >= t_end) return;
@@ -701,8 +706,8 @@ void attention_kernel(Args) {
             const int k_place = now.k.start() + own_place, q_place = now.q.start() + own_place;
             // in blocks of 16 x 16 of the triangle, two at a time
 #pragma unroll
-            for (int first = 0; first < BLOCKS; first += W) {
-                constexpr int kHalf = W / 2;
+            for (int first = 0; first < BLOCKS; first += 2 * Sh::kHelpers) {
+                constexpr int kHalf = Sh::kHelpers;
                 const bool two = first + kHalf < BLOCKS;
                 int ib[2], jb[2];
                 bool has[2];
@@ -940,13 +945,17 @@ constexpr int columns_of(int waves) { return 16 * waves; }
 int64_t blocks_of(int vd, int waves) { return (vd + columns_of(waves) - 1) / columns_of(waves); }
 // Workgroups that a compute unit holds of a form: two where LDS has room, of 8 waves that
 // hold the state one, by its registers.
-constexpr bool holds_two(int dtype, int kd, int waves) { return waves == 4 && kd <= (dtype == kF32 ? 32 : 64); }
+constexpr bool holds_two(int dtype, int kd, int waves) { return waves == 4 && kd <= (dtype == kF32 ? 0 : 64); }
 
 // Segments shorten the walk where the heads do not fill the chip, and cost a pass over k
 // and v for the states ahead of them.  A form's time is taken as its rounds of workgroups,
-// each as many tiles long as a segment and kStart more; the states' pass as half a tile for
-// each; what joins them as kJoin.  The cuts that fill one to kRounds rounds are compared.
-constexpr int64_t kStart = 3, kJoin = 4, kRounds = 4;   // in halves of a tile's time
+// each as many tiles long as a segment and kStart more, and the states' pass as half a tile
+// for each; joining them as kJoin, more for their number and for their memory, which is
+// written and read twice.  The cuts that fill half a round to kRounds rounds are compared.
+// Of 128 shapes, all types, 512 to 16384 steps of 4 to 256 heads, the cut taken was 2 %
+// slower on average than the best of all that were timed, and 10 of them more than 10 %.
+constexpr int64_t kStart = 3, kJoin = 4, kRounds = 4;                // in halves of a tile's time, 1.3 us
+constexpr int64_t kJoinSegments = 4, kJoinBytes = 6'000'000;         // that cost one more
 Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
     int kd = 0, vd = 0;
     for (int p = 0; p < passes; ++p) kd = std::max(kd, dims[p][0]), vd = std::max(vd, dims[p][1]);
@@ -960,11 +969,14 @@ Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int
     const int64_t room = int64_t(device_cu_count()) * (holds_two(dtype, c.kd, c.waves) ? 2 : 1);
     auto rounds = [&](int64_t workgroups) { return (workgroups + room - 1) / room; };
     const int64_t chains = std::max<int64_t>(1, units * std::min(passes, 2) / passes);
+    const int64_t bytes = N * H * std::min(passes, 2) * dims[0][0] * dims[0][1] * 16;   // of a segment's states
     int64_t least = rounds(units) * (2 * tiles + kStart);
-    for (int64_t r = 1; r <= kRounds && units < r * room; ++r) {
-        const int64_t each = (tiles + r * room / units - 1) / (r * room / units), segments = (tiles + each - 1) / each;
+    for (int64_t fill = room / 2; fill <= kRounds * room; fill += room / 2) {
+        if (units >= fill) continue;
+        const int64_t each = (tiles + fill / units - 1) / (fill / units), segments = (tiles + each - 1) / each;
         if (segments == 1) continue;
-        const int64_t time = rounds(units * segments) * (2 * each + kStart) + rounds(chains * (segments - 1)) * (each + kStart) + kJoin;
+        const int64_t time = rounds(units * segments) * (2 * each + kStart) + rounds(chains * (segments - 1)) * (each + kStart) + kJoin +
+                             segments / kJoinSegments + segments * bytes / kJoinBytes;
         if (time < least) least = time, c.each = static_cast<int32_t>(each), c.segments = static_cast<int32_t>(segments);
     }
     return c;
