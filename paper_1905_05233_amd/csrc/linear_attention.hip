@@ -936,50 +936,90 @@ HeadsIn heads_in(const wg_heads& t, int64_t heads, int64_t H) {
 }
 HeadsOut heads_out(const wg_heads& t) { return {const_cast<void*>(t.data), t.stride_n, t.stride_l, t.stride_h, 0}; }
 
-// How a call is cut: the kernel's form and the segments of a sequence.
-struct Cut {
-    int kd, waves;            // channels of q and k, and waves that hold the state, of the kernel's form
-    int32_t segments, each;   // tiles of a segment
+// A form of the kernel: the channels of q and k, and the waves that hold the state.
+struct Form {
+    int kd, waves;
+    bool operator==(const Form& o) const { return kd == o.kd && waves == o.waves; }
 };
+Form form_of(int dtype, int kd, int vd) {
+    return {kd <= 32 ? 32 : kd <= 64 ? 64 : kd <= 128 ? 128 : 256, vd <= 64 || kd > 128 || dtype == kF32 ? 4 : 8};
+}
 constexpr int columns_of(int waves) { return 16 * waves; }
 int64_t blocks_of(int vd, int waves) { return (vd + columns_of(waves) - 1) / columns_of(waves); }
 // Workgroups that a compute unit holds of a form: two where LDS has room, of 8 waves that
 // hold the state one, by its registers.
-constexpr bool holds_two(int dtype, int kd, int waves) { return waves == 4 && kd <= (dtype == kF32 ? 0 : 64); }
+int64_t room_of(int dtype, const Form& f) { return device_cu_count() * (f.waves == 4 && f.kd <= (dtype == kF32 ? 0 : 64) ? 2 : 1); }
+
+// The time of a form's tile beside the others', in eighths: of 256 heads of 2048 steps in
+// bf16 4.2 us for 128 channels and 8 waves, 3.7 for 4 waves, 2.7 for 64 channels.
+constexpr int64_t tile_time(const Form& f) { return f.kd > 128 ? 10 : (f.kd > 64 ? 6 : 4) + f.waves / 4; }
+
+// How a call is cut: the forms of its passes and of the states' passes, and the segments
+// of a sequence, `each` tiles of `tile` steps.
+struct Cut {
+    Form form[3], states;
+    int tile;
+    int32_t segments, each;
+    double time;
+};
 
 // Segments shorten the walk where the heads do not fill the chip, and cost a pass over k
 // and v for the states ahead of them.  A form's time is taken as its rounds of workgroups,
 // each as many tiles long as a segment and kStart more, and the states' pass as half a tile
-// for each; joining them as kJoin, more for their number and for their memory, which is
+// for each, a launch more as kLaunch; joining the states as kJoin, more for their number and for their memory, which is
 // written and read twice.  The cuts that fill half a round to kRounds rounds are compared.
 // Of 128 shapes, all types, 512 to 16384 steps of 4 to 256 heads, the cut taken was 2 %
 // slower on average than the best of all that were timed, and 10 of them more than 10 %.
-constexpr int64_t kStart = 3, kJoin = 4, kRounds = 4;                // in halves of a tile's time, 1.3 us
-constexpr int64_t kJoinSegments = 4, kJoinBytes = 6'000'000;         // that cost one more
-Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
+constexpr int64_t kStart = 3, kLaunch = 2, kJoin = 4, kRounds = 4;   // in halves of a tile's time, 1.3 us
+constexpr int64_t kJoinSegments = 8, kJoinBytes = 6'000'000;         // that cost one more
+Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes, bool apart) {
+    Cut c{};
     int kd = 0, vd = 0;
     for (int p = 0; p < passes; ++p) kd = std::max(kd, dims[p][0]), vd = std::max(vd, dims[p][1]);
-    Cut c{kd <= 32 ? 32 : kd <= 64 ? 64 : kd <= 128 ? 128 : 256, vd <= 64 || kd > 128 || dtype == kF32 ? 4 : 8, 1, 1};
-    const int tile = tile_steps(dtype == kBF16, c.kd);
-    int64_t units = 0;
-    for (int p = 0; p < passes; ++p) units += N * H * blocks_of(dims[p][1], c.waves);
-    const int64_t tiles = std::max<int64_t>(1, (L + tile - 1) / tile);
-    c.each = static_cast<int32_t>(tiles);
-    if (units == 0) return c;
-    const int64_t room = int64_t(device_cu_count()) * (holds_two(dtype, c.kd, c.waves) ? 2 : 1);
-    auto rounds = [&](int64_t workgroups) { return (workgroups + room - 1) / room; };
-    const int64_t chains = std::max<int64_t>(1, units * std::min(passes, 2) / passes);
-    const int64_t bytes = N * H * std::min(passes, 2) * dims[0][0] * dims[0][1] * 16;   // of a segment's states
-    int64_t least = rounds(units) * (2 * tiles + kStart);
+    const Form joint = form_of(dtype, kd, vd);
+    for (int p = 0; p < passes; ++p) c.form[p] = apart ? form_of(dtype, dims[p][0], dims[p][1]) : joint;
+    c.states = c.form[passes - 1];   // dv's pass walks over the states' own channels
+    c.tile = tile_steps(dtype == kBF16, c.states.kd);
+    const int64_t tiles = std::max<int64_t>(1, (L + c.tile - 1) / c.tile);
+    c.segments = 1, c.each = static_cast<int32_t>(tiles);
+    if (N * H == 0) return c;
+    auto time_of = [&](const Form& f, int64_t workgroups, double each) {
+        const int64_t room = room_of(dtype, f);
+        return static_cast<double>((workgroups + room - 1) / room) * (each * static_cast<double>(tile_time(f)) / static_cast<double>(tile_time(joint)) + kStart);
+    };
+    auto passes_time = [&](int64_t segments, int64_t each) {   // those of one form go together
+        double time = 0.0;
+        for (int p = 0, next; p < passes; p = next) {
+            int64_t workgroups = 0;
+            for (next = p; next < passes && c.form[next] == c.form[p]; ++next)
+                workgroups += N * H * blocks_of(dims[next][1], c.form[p].waves) * segments;
+            time += time_of(c.form[p], workgroups, 2.0 * static_cast<double>(each)) + (p > 0 ? kLaunch : 0);
+        }
+        return time;
+    };
+    const int chains = std::min(passes, 2);
+    const int64_t units = N * H * blocks_of(dims[passes - 1][1], c.states.waves), room = room_of(dtype, c.states);
+    const int64_t bytes = N * H * chains * dims[0][0] * dims[0][1] * 16;   // of a segment's states
+    c.time = passes_time(1, tiles);
     for (int64_t fill = room / 2; fill <= kRounds * room; fill += room / 2) {
-        if (units >= fill) continue;
-        const int64_t each = (tiles + fill / units - 1) / (fill / units), segments = (tiles + each - 1) / each;
+        if (units * passes >= fill) continue;
+        const int64_t share = fill / (units * passes), each = (tiles + share - 1) / share, segments = (tiles + each - 1) / each;
         if (segments == 1) continue;
-        const int64_t time = rounds(units * segments) * (2 * each + kStart) + rounds(chains * (segments - 1)) * (each + kStart) + kJoin +
-                             segments / kJoinSegments + segments * bytes / kJoinBytes;
-        if (time < least) least = time, c.each = static_cast<int32_t>(each), c.segments = static_cast<int32_t>(segments);
+        const double time = passes_time(segments, each) + time_of(c.states, units * chains * (segments - 1), static_cast<double>(each)) +
+                            static_cast<double>(kJoin + segments / kJoinSegments + segments * bytes / kJoinBytes);
+        if (time < c.time) c.time = time, c.each = static_cast<int32_t>(each), c.segments = static_cast<int32_t>(segments);
     }
     return c;
+}
+
+// All passes in one form and one launch, or, where the forms' tiles are alike, each in the
+// form of its own channels: gradients of 16 x 4096 steps of 8 heads of 128 and 64 channels
+// in bf16 476 and 384 us, of one step of 64 of such a head 13 and 20 us.
+Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
+    const Cut joint = cut_of(dtype, N, L, H, dims, passes, false), apart = cut_of(dtype, N, L, H, dims, passes, true);
+    for (int p = 0; p < passes; ++p)
+        if (tile_steps(dtype == kBF16, apart.form[p].kd) != joint.tile) return joint;
+    return apart.time < joint.time ? apart : joint;
 }
 
 // HIP takes fewer than 2^32 threads: more sequences than that go in several launches.
@@ -1010,15 +1050,27 @@ hipError_t over_sequences(const Args& a, int passes, int segments, int dtype, in
 
 #define WG_ATTENTION_SHAPES(X) X(32, 4) X(32, 8) X(64, 4) X(64, 8) X(128, 4) X(128, 8) X(256, 4)
 
-template <typename Elem, bool STATES> hipError_t run_passes(Args& a, int passes, const Cut& cut, int dtype, hipStream_t stream) {
-    for (int p = 0; p < passes; ++p) a.pass[p].blocks = static_cast<int32_t>(blocks_of(a.pass[p].vd, cut.waves));
-    a.segments = cut.segments, a.each = cut.each;
-#define WG_ATTENTION_CASE(K, W) \
-    if constexpr (W == 4 || sizeof(Elem) == 2) \
-        if (cut.kd == K && cut.waves == W) return over_sequences(a, passes, STATES ? cut.segments - 1 : cut.segments, dtype, Shape<Elem, K, W, STATES>::kThreads, attention_kernel<Elem, K, W, STATES>, stream);
-    WG_ATTENTION_SHAPES(WG_ATTENTION_CASE)
+// A launch for the passes of one form that follow one another.
+template <typename Elem, bool STATES> hipError_t run_passes(const Args& all, int passes, const Cut& cut, int dtype, hipStream_t stream) {
+    for (int p = 0, next; p < passes; p = next) {
+        const Form form = STATES ? cut.states : cut.form[p];
+        Args a = all;
+        a.segments = cut.segments, a.each = cut.each;
+        for (next = p; next < passes && (STATES || cut.form[next] == form); ++next) {
+            a.pass[next - p] = all.pass[next];
+            a.pass[next - p].blocks = static_cast<int32_t>(blocks_of(all.pass[next].vd, form.waves));
+        }
+        hipError_t e = hipErrorInvalidValue;
+#define WG_ATTENTION_CASE(K, W)                                                                                        \
+    if constexpr (W == 4 || sizeof(Elem) == 2)                                                                         \
+        if (form == Form{K, W})                                                                                        \
+            e = over_sequences(a, next - p, STATES ? cut.segments - 1 : cut.segments, dtype,                           \
+                               Shape<Elem, K, W, STATES>::kThreads, attention_kernel<Elem, K, W, STATES>, stream);
+        WG_ATTENTION_SHAPES(WG_ATTENTION_CASE)
 #undef WG_ATTENTION_CASE
-    return hipErrorInvalidValue;
+        if (e) return e;
+    }
+    return hipSuccess;
 }
 
 // The states of `of` chains' segments: the pass that adds to each goes first.
@@ -1030,7 +1082,7 @@ hipError_t run_chains(Args a, const Chain* chains, int of, const Cut& cut, int d
     int32_t size = 0;
     for (int c = 0; c < of; ++c) k.chain[c] = chains[c], size = std::max(size, chains[c].size);
     k.heads = a.N * a.H, k.L = a.L, k.H = a.H, k.segments = cut.segments;
-    k.tile = tile_steps(dtype == kBF16, cut.kd), k.each_steps = cut.each * k.tile, k.blocks = (size + kThreads - 1) / kThreads, k.of = of;
+    k.tile = cut.tile, k.each_steps = cut.each * k.tile, k.blocks = (size + kThreads - 1) / kThreads, k.of = of;
     k.log_decay = a.log_decay, k.lengths = a.lengths;
     const unsigned grid = static_cast<unsigned>(k.heads * k.blocks * of);
     if (cut.segments <= 8) chain_kernel<8><<<grid, kThreads, 0, stream>>>(k);
