@@ -289,6 +289,39 @@ def test_operators_together(dtype):
     R.assert_close(_np(s), *ref["s_last"], "f32", "s")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gradients_together(dtype):
+    """A training pass of both: the gradients of queries, keys and values go in the slices
+    of one projection's gradient, and those through the norm and rotation in place; each
+    operator against the 64-bit formulas at what it was given."""
+    from paper_1905_05233_amd import sequence_ops as S
+    N, L, Hq, Hk, H, D, Dv = 3, 90, 4, 2, 4, 32, 24
+    widths, lengths = [Hq * D, Hk * D, Hk * Dv], np.array([90, 0, 61])
+    rows = _randn(N, L, sum(widths), dtype=dtype)
+    x, k0, v = [t.unflatten(2, (h, -1)) for t, h in zip(rows.split(widths, 2), (Hq, Hk, Hk))]
+    w, rot = [1.0 + 0.1 * _randn(D, dtype=dtype) for _ in range(2)], S.Rotary(32, adjacent=True)
+    g, n = torch.tensor([-0.01, -0.1, -0.5, -2.0], device="cuda"), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    q, k = S.head_norm_rotate(x, k0, *w, rot)
+    y, _ = S.linear_attention(q, k, v, g, lengths=n)
+    dy, drows = torch.randn_like(y), torch.full_like(rows, 7.0)
+    out = [t.unflatten(2, (h, -1)) for t, h in zip(drows.split(widths, 2), (Hq, Hk, Hk))]
+    S.linear_attention_backward(dy, q, k, v, g, lengths=n, out=out)
+    ref = A.attention(_np(q), _np(k), _np(v), _np(g), None, lengths, D ** -0.5, dtype, _np(dy))
+    R.assert_close(_np(y), *ref["y"], dtype, "y")
+    for name, t in zip(("dq", "dk", "dv"), out):
+        R.assert_close(_np(t), *ref[name], dtype, name)
+    before = [t.clone() for t in out[:2]]
+    dq, dk, dwq, dwk = S.head_norm_rotate_backward(*out[:2], x, k0, *w, rot, out=out[:2])
+    assert dq is out[0] and dk is out[1]
+    where, f = np.tile(np.arange(L), (N, 1)), [10000.0 ** (-i / 16) for i in range(16)]
+    for at, weight, d, dx, dw in ((x, w[0], before[0], dq, dwq), (k0, w[1], before[1], dk, dwk)):
+        (want, bound), (want_w, bound_w) = A.rotate(_np(at), _np(weight), f, where, 1e-6, True, _np(d))
+        R.assert_close(_np(dx), want, bound, dtype, "dx")
+        R.assert_close(_np(dw), want_w, bound_w, "f32", "dw")
+    for i in range(N):
+        assert not drows[i, lengths[i]:].any()
+
+
 def test_work_on_both_streams_at_once():
     """A call on the current stream and one on another, in flight together."""
     call = _calls()["attention"]
