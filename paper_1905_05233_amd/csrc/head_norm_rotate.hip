@@ -14,10 +14,12 @@
 //
 // A head's row is shared by 2^n lanes, each with two runs of 16 bytes: the two halves
 // of V pairs, or V pairs side by side.  The lanes keep a position's sines for its
-// heads.  Bound by memory: 65536 rows of 8 and 8 heads of 64 channels in bf16 take 50 us in
-// the kernel, 268 MB at 5.4 TB/s, their gradients 85 (403 MB, 4.7 TB/s).  Of odd channels,
-// whose last runs hold one, by the lanes' instructions: 65536 rows of 7 heads of 75, 85 us
-// where their bytes cost 27; one load instead of the last run's eight was no faster.
+// heads.  Bound by memory: 65536 rows of 8 and 8 heads of 64 channels in bf16 take 49 us in
+// the kernel, 268 MB at 5.4 TB/s, their gradients 80 (403 MB, 5.0 TB/s).  Of odd channels,
+// whose last runs hold one, by the lanes' instructions: 65536 rows of 7 heads of 75, 78 us
+// where their bytes cost 27; 16 bytes that end with the row, shifted, instead of the last
+// run's own loads were slower (82), and so were loads ahead of the sines (gradients 105 us
+// for 91, by their registers).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -158,19 +160,26 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs<Elem> a) {
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * GROUPS; first < units; first += step) {
         const int64_t unit = first + group;
         const bool has = unit < units;
-        const int64_t row = has ? unit / a.chunks : 0;
-        const int chunk = has ? static_cast<int>(unit % a.chunks) : 0;
-        const int64_t n = row / a.L, l = row - n * a.L;
+        int64_t row = 0, n = 0;
+        if (units >> 32 == 0) {   // 64-bit divisions take ten times the instructions
+            const uint32_t small = has ? static_cast<uint32_t>(unit) / static_cast<uint32_t>(a.chunks) : 0;
+            row = small, n = small / static_cast<uint32_t>(a.L);
+        } else if (has) {
+            row = unit / a.chunks;
+            n = row / a.L;
+        }
+        const int chunk = has ? static_cast<int>(unit - row * a.chunks) : 0;
+        const int64_t l = row - n * a.L;
         const int h_first = chunk * a.each, h_end = has ? min(h_first + a.each, a.side[0].heads + a.side[1].heads) : 0;
         const int64_t position = a.positions ? a.positions[row] : a.start + l;
         float co[V], si[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const int u = adjacent ? e / (V / 2) : 0, j = adjacent ? e % (V / 2) : e;
-            co[e] = 1.0f;
-            si[e] = 0.0f;
-            if (j < runs.pairs[u])
-                cos_sin(static_cast<uint32_t>((static_cast<uint64_t>(position) * a.turns[runs.pair[u] + j]) >> 32), co[e], si[e]);
+            // every lane loads, the last frequency where it turns no pair: all are in flight together
+            const uint64_t turns = a.turns[min(runs.pair[u] + j, a.R / 2 - 1)];
+            cos_sin(static_cast<uint32_t>((static_cast<uint64_t>(position) * turns) >> 32), co[e], si[e]);
+            if (j >= runs.pairs[u]) co[e] = 1.0f, si[e] = 0.0f;
             if (GRAD) si[e] = -si[e];
         }
         auto turn = [&](float (&x)[2][V]) {
@@ -212,6 +221,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs<Elem> a) {
                 }
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
+                    if (k > 0 && !__any(i + k < rounds)) break;   // few heads a group: 64 x 16 heads 7.7 to 6.4 us
                     float x[2][V], ss = 0.0f;
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
