@@ -891,9 +891,15 @@ struct StepArgs {
 
 // One step: a workgroup takes 64 columns of a head's state, a thread 4 of them in every
 // 16th row.  Bound by the states' memory, read and written once: 2048 states of 128 x 128
-// channels, 268 MB, in 57 us (4.7 TB/s).
+// channels, 268 MB, in 55 us (4.9 TB/s); of 75 x 75, whose rows end within 16 bytes, by the
+// second workgroup of a head, which has 11 columns (36 us where the bytes cost 18; by single
+// values there 45).
 constexpr int kStepColumns = 64, kStepRows = kThreads / (kStepColumns / 4);
-template <typename Elem>
+// Rows of a thread whose loads are in flight together: 128 states of 128 x 128 channels take
+// 6.4 us, with one row 9.0; 2048 of them 54.6, with eight 56.2.
+constexpr int kStepAhead = 4;
+// FULL: v's columns in whole fours, without the shifts (54.6 and 59.2 us there).
+template <typename Elem, bool FULL>
 __global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a) {
     using St = Storage<Elem>;
     __shared__ float lds[kStepRows][kStepColumns + 4];
@@ -911,19 +917,37 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = e < valid ? St::to_f32(v[j + e]) : 0.0f;
         const int64_t at = ((n * a.H + h) * a.kd) * static_cast<int64_t>(a.vd) + j;
-        for (int i = r0; i < a.kd; i += kStepRows) {
-            const float ki = St::to_f32(k[i]), qi = St::to_f32(q[i]);
-            const float* s = a.s + at + static_cast<int64_t>(i) * a.vd;
-            float* s_new = a.s_new + at + static_cast<int64_t>(i) * a.vd;
-            if (valid == 4) {
-                f32x4 w = __builtin_bit_cast(f32x4, reinterpret_cast<const Bytes16*>(s)->v);
+        if (valid > 0 && (FULL || a.vd >= 4)) {
+            // columns behind the last: the 16 bytes that end with the row, shifted
+            const int over = FULL ? 0 : 4 - valid;
+            for (int first = r0; first < a.kd; first += kStepAhead * kStepRows) {
+                f32x4 w[kStepAhead];
+                float ki[kStepAhead], qi[kStepAhead];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] = fmaf(keep, w[e], ki * x[e]);
-                    sum[e] = fmaf(qi, w[e], sum[e]);
+                for (int u = 0; u < kStepAhead; ++u) {   // rows behind the last are the last one's, and not used
+                    const int i = min(first + u * kStepRows, a.kd - 1);
+                    w[u] = __builtin_bit_cast(f32x4, reinterpret_cast<const Bytes16*>(a.s + at + static_cast<int64_t>(i) * a.vd - over)->v);
+                    ki[u] = St::to_f32(k[i]);
+                    qi[u] = St::to_f32(q[i]);
                 }
-                reinterpret_cast<Bytes16*>(s_new)->v = __builtin_bit_cast(u32x4, w);
-            } else {
+#pragma unroll
+                for (int u = 0; u < kStepAhead; ++u) {
+                    const int i = first + u * kStepRows;
+                    if (i >= a.kd) break;
+                    if (!FULL && over > 0) w[u] = __builtin_bit_cast(f32x4, drop_first<float>(__builtin_bit_cast(u32x4, w[u]), over));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        w[u][e] = fmaf(keep, w[u][e], ki[u] * x[e]);
+                        sum[e] = fmaf(qi[u], w[u][e], sum[e]);
+                    }
+                    store_run<float, FULL>(a.s_new + at + static_cast<int64_t>(i) * a.vd, valid, __builtin_bit_cast(u32x4, w[u]));
+                }
+            }
+        } else if (!FULL) {
+            for (int i = r0; i < a.kd; i += kStepRows) {
+                const float ki = St::to_f32(k[i]), qi = St::to_f32(q[i]);
+                const float* s = a.s + at + static_cast<int64_t>(i) * a.vd;
+                float* s_new = a.s_new + at + static_cast<int64_t>(i) * a.vd;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (e >= valid) continue;
@@ -1221,7 +1245,8 @@ template <int D> hipError_t launch_linear_attention_step_t(const wg_linear_atten
                      heads_out(a.y), a.N, static_cast<int32_t>(a.heads), static_cast<int32_t>(a.Dk), static_cast<int32_t>(a.Dv),
                      blocks, a.log_decay, a.s, a.s_new, static_cast<float>(a.scale)};
     const int64_t grid = std::min<int64_t>(a.N * a.heads * blocks, 0xffffffffLL / kThreads);
-    step_kernel<Elem><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(k);
+    if (a.Dv % 4 == 0) step_kernel<Elem, true><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(k);
+    else step_kernel<Elem, false><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(k);
     return hipGetLastError();
 }
 
