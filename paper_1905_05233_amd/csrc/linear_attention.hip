@@ -807,10 +807,12 @@ struct ChainArgs {
     const float* log_decay;
     const int32_t* lengths;
 };
-// A thread holds one value of a state and walks over the segments; U: those whose loads are
-// in flight together.  Bound by latency: 4 us for six segments of 39 states of 40 x 75, 7 us
-// for 32 of 4 of 128 x 128 channels, of which a launch takes 2.5; 12 us for 64 of them.
-template <int U> __global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
+// A thread holds one value of a state and walks over the segments, with the loads of U in
+// flight together (with 64 no faster, for all the code).  Bound by latency: 4 us for six
+// segments of 39 states of 40 x 75, of which a launch takes 2.5, 9 us for 64 of 4 states of
+// 128 x 128 channels.
+__global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
+    constexpr int U = 16;
     const Chain& c = a.chain[blockIdx.x % a.of];
     const uint32_t unit = blockIdx.x / a.of, head = unit / static_cast<uint32_t>(a.blocks);
     const int32_t i = static_cast<int32_t>(unit - head * a.blocks) * kThreads + threadIdx.x;
@@ -821,8 +823,14 @@ template <int U> __global__ __launch_bounds__(kThreads) void chain_kernel(ChainA
     const int64_t size = c.size;
     float* s = c.states + head * (a.segments * size) + i;
     float run = c.s_in ? c.s_in[head * size + i] : 0.0f;
-    const float whole = exact_power(log_decay, a.each_steps);
-    const int32_t adding = a.segments - 1;
+    // Segments have each_steps, but the reverse of a walk begins with a tile that may be short,
+    // the last one ends with the steps, and those behind it are empty.  Their decays are made
+    // ahead of the walk: a power in every turn made 25 KB of code of it, and 13 us of those 9.
+    const int64_t each = a.each_steps, end = steps + (c.reverse ? last : 0);
+    const int32_t cut = static_cast<int32_t>(end / each), rest = static_cast<int32_t>(end - cut * each);
+    const float whole = exact_power(log_decay, a.each_steps), at_cut = exact_power(log_decay, rest);
+    const float at_first = exact_power(log_decay, max(0, static_cast<int32_t>(min(each, end)) - (c.reverse ? last : 0)));
+    const int32_t adding = a.segments - 1, filled = cut + (rest > 0);
     for (int32_t w = 0; w < a.segments; w += U) {
         float add[U];
 #pragma unroll
@@ -831,13 +839,7 @@ template <int U> __global__ __launch_bounds__(kThreads) void chain_kernel(ChainA
         for (int u = 0; u < U; ++u) {
             if (w + u >= a.segments) break;
             s[(w + u) * size] = run;
-            if (w + u >= adding) break;
-            // steps of the segment: all but the last have each_steps, but the reverse of a
-            // walk begins with the tile that may be short
-            const int64_t from = static_cast<int64_t>(w + u) * a.each_steps - (c.reverse && w + u > 0 ? last : 0);
-            const int64_t to = static_cast<int64_t>(w + u + 1) * a.each_steps - (c.reverse ? last : 0);
-            const int32_t count = static_cast<int32_t>(min(to, static_cast<int64_t>(steps)) - from);
-            if (count > 0) run = fmaf(count == a.each_steps ? whole : exact_power(log_decay, count), run, add[u]);
+            if (w + u < min(adding, filled)) run = fmaf(w + u == 0 ? at_first : w + u == cut ? at_cut : whole, run, add[u]);
         }
     }
 }
@@ -1128,9 +1130,7 @@ hipError_t run_chains(Args a, const Chain* chains, int of, const Cut& cut, int d
     k.tile = cut.tile, k.each_steps = cut.each * k.tile, k.blocks = (size + kThreads - 1) / kThreads, k.of = of;
     k.log_decay = a.log_decay, k.lengths = a.lengths;
     const unsigned grid = static_cast<unsigned>(k.heads * k.blocks * of);
-    if (cut.segments <= 8) chain_kernel<8><<<grid, kThreads, 0, stream>>>(k);
-    else if (cut.segments <= 24) chain_kernel<24><<<grid, kThreads, 0, stream>>>(k);
-    else chain_kernel<64><<<grid, kThreads, 0, stream>>>(k);
+    chain_kernel<<<grid, kThreads, 0, stream>>>(k);
     return hipGetLastError();
 }
 
