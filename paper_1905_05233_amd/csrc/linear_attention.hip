@@ -712,6 +712,16 @@ void attention_kernel(Args) {
         if (!any) return;
         const int tid = threadIdx.x - 64 * W - Sh::kMemory, own_wave = wave - W - Sh::kHelpers;
         const int own_place = decltype(lds.steps[0].k)::place(m, 8 * g);
+        // the decays between steps of one block, of neighbouring blocks, and by 16 and 32 steps more
+        const int d0 = reverse ? 4 * g - m : m - 4 * g;
+        float here[4], next[4];
+        const float far_by[2] = {power(log2_decay, 16), power(log2_decay, 32)};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = d0 + (reverse ? r : -r);
+            here[r] = a.scale * power(log2_decay, max(0, d));
+            next[r] = a.scale * power(log2_decay, 16 + d);
+        }
         auto weigh = [&](int32_t t) {
             if (t >= t_end) return;
             const auto& now = stage_of(t);
@@ -758,11 +768,14 @@ void attention_kernel(Args) {
                 for (int u = 0; u < 2; ++u) {
                     if (!has[u] || (u == 1 && !two)) continue;
                     float x[4];
-                    const int d0 = reverse ? 16 * (jb[u] - ib[u]) + 4 * g - m : 16 * (ib[u] - jb[u]) + m - 4 * g;
+                    const int apart = reverse ? jb[u] - ib[u] : ib[u] - jb[u];
+                    if (apart == 0) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int d = reverse ? d0 + r : d0 - r;
-                        x[r] = d < 0 ? 0.0f : w[u][r] * (a.scale * power(log2_decay, d));
+                        for (int r = 0; r < 4; ++r) x[r] = d0 + (reverse ? r : -r) < 0 ? 0.0f : w[u][r] * here[r];
+                    } else {
+                        const float more = apart == 1 ? 1.0f : apart == 2 ? far_by[0] : far_by[1];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[r] = w[u][r] * (next[r] * more);
                     }
                     Split<PS, 4, false> parts;
                     parts.of(x);
