@@ -27,11 +27,11 @@
 // what each adds to the state, chain_kernel the states ahead of them, and a launch the outputs.
 //
 // Bound, for bf16 heads of 128 channels, by a tile's latency close to memory: 256 sequences
-// and heads of 2048 steps take 135 us, 4.0 TB/s of the 5.1 that a copy reaches; of 64
-// channels 88 us (3.1 TB/s), of 128 in fp32, where nine products stand for one and every
-// value is taken apart, 410 us (2.6 TB/s at twice the bytes).  A single head's sequences are
-// bound by the start of the three launches, some 8 us each: 16384 steps of 4 heads of 128
-// channels take 57 us where their bytes cost 13.
+// and heads of 2048 steps take 138 us, 3.9 TB/s of the 5.1 that a copy reaches; of 64
+// channels 85 us (3.2 TB/s); of 128 in fp32, where nine products stand for one and every
+// value is taken apart, 410 us (2.6 TB/s at twice the bytes).  A few heads' sequences are
+// bound by the start of the three launches, 4 to 8 us each, of which the code's own way to the
+// compute units is a part: 16381 steps of 4 heads of 128 channels take 52 us, their bytes 13.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1057,12 +1057,12 @@ Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int
     };
     const int chains = std::min(passes, 2);
     const int64_t units = N * H * blocks_of(dims[passes - 1][1], c.states.waves), room = room_of(dtype, c.states);
-    const int64_t bytes = N * H * chains * dims[0][0] * dims[0][1] * 16;   // of a segment's states
     c.time = passes_time(1, tiles);
     for (int64_t fill = room / 2; fill <= kRounds * room; fill += room / 2) {
         if (units * passes >= fill) continue;
         const int64_t share = fill / (units * passes), each = (tiles + share - 1) / share, segments = (tiles + each - 1) / each;
         if (segments == 1) continue;
+        const int64_t bytes = N * H * chains * dims[0][0] * dims[0][1] * 16;   // of a segment's states
         const double time = passes_time(segments, each) + time_of(c.states, units * chains * (segments - 1), static_cast<double>(each)) +
                             static_cast<double>(kJoin + segments / kJoinSegments + segments * bytes / kJoinBytes);
         if (time < c.time) c.time = time, c.each = static_cast<int32_t>(each), c.segments = static_cast<int32_t>(segments);
