@@ -697,14 +697,16 @@ void attention_kernel(Args) {
         }
         if constexpr (STATES) return;
         // padding, of which each segment takes a share of rows
-        const int width = min(VB, vd - v0), share = (a.L - steps + a.segments - 1) / a.segments;
-        const int32_t row0 = steps + min(segment * static_cast<int64_t>(share), static_cast<int64_t>(a.L - steps));
-        const int64_t values = static_cast<int64_t>(min(share, a.L - row0)) * width;
-        for (int64_t i = tid; i < values; i += Sh::kMemory) {
-            const int64_t at = n * pass.y.sn + (row0 + i / width) * pass.y.sl + h * pass.y.sh + v0 + i % width;
-            if (y_f32) static_cast<float*>(pass.y.p)[at] = 0.0f;
-            else static_cast<Elem*>(pass.y.p)[at] = Storage<Elem>::from_f32(0.0f);
-        }
+        const int32_t share = (a.L - steps + a.segments - 1) / a.segments;
+        const int64_t row0 = min(steps + static_cast<int64_t>(segment) * share, static_cast<int64_t>(a.L));
+        const int64_t row1 = min(row0 + share, static_cast<int64_t>(a.L));
+        // (of parts in fp32 nothing is read there)
+        constexpr int V = Vec<Elem>::V, RUNS = VB / V;
+        const int run = tid % RUNS, valid = y_f32 ? 0 : min(V, vd - v0 - run * V);
+        if (valid <= 0) return;
+        Elem* y = static_cast<Elem*>(pass.y.p) + n * pass.y.sn + h * pass.y.sh + v0 + run * V;
+        for (int64_t row = row0 + tid / RUNS; row < row1; row += Sh::kMemory / RUNS)
+            store_run<Elem, false>(y + row * pass.y.sl, valid, u32x4{0, 0, 0, 0});
         return;
     }
 
@@ -859,7 +861,7 @@ __global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
 
 // Gradients of inputs that heads share: the sums over them of their parts [N][L][H][D4]
 // in fp32 (D4 is D up to a multiple of 4), in the order of the heads, so that results repeat
-// (atomics would not).  A thread takes four channels.  14 us for 8000 steps of 8 heads on 2
+// (atomics would not); those of padding are not there.  A thread takes four channels.  14 us for 8000 steps of 8 heads on 2
 // of 128 channels: 65 MB of parts read at 4.7 TB/s.
 struct Shared {
     const float* part;
@@ -871,6 +873,7 @@ struct SharedArgs {
     Shared of[3];
     int32_t count, L;
     int64_t items;
+    const int32_t* lengths;
 };
 template <typename Elem>
 __global__ __launch_bounds__(kThreads) void shared_kernel(SharedArgs a) {
@@ -884,8 +887,9 @@ __global__ __launch_bounds__(kThreads) void shared_kernel(SharedArgs a) {
         const int32_t run = static_cast<int32_t>(item - row_head * runs), h = static_cast<int32_t>(row_head - row * s.heads);
         const f32x4* p = reinterpret_cast<const f32x4*>(s.part) + row_head * s.per * runs + run;
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int32_t u = 0; u < s.per; ++u) sum += p[static_cast<int64_t>(u) * runs];
         const int64_t n = row / a.L;
+        if (row - n * a.L < steps_of(a.lengths, n, a.L))
+            for (int32_t u = 0; u < s.per; ++u) sum += p[static_cast<int64_t>(u) * runs];
         Elem* to = static_cast<Elem*>(s.to.p) + n * s.to.sn + (row - n * a.L) * s.to.sl + h * s.to.sh + 4 * run;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -1238,7 +1242,7 @@ template <int D> hipError_t launch_linear_attention_backward_t(const wg_linear_a
     k.pass[2] = Pass{kk, q, dy, to(2), Dk, Dv, 0, g_in, a.ds0, {Dv, 1}, k.scale, 1.0f, 1, segmented};
     if (const hipError_t e = run_passes<Elem, false>(k, 3, cut, D, stream)) return e;
     SharedArgs s{};
-    s.L = k.L;
+    s.L = k.L, s.lengths = a.lengths;
     for (int p = 0; p < 3; ++p) {
         if (!parts[p]) continue;
         s.of[s.count++] = Shared{parts[p], out[p], static_cast<int32_t>(heads[p]), static_cast<int32_t>(H / heads[p]), dims[p], s.items};

@@ -322,6 +322,29 @@ def test_gradients_together(dtype):
         assert not drows[i, lengths[i]:].any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads", [(2, 2), (1, 2)], ids=str)
+@pytest.mark.parametrize("Dv", [3, 20, 72, 150])
+def test_padding_is_cleared_and_nothing_beside_it(Dv, heads, dtype):
+    from paper_1905_05233_amd import sequence_ops as S
+    N, L, Dk, lengths = 4, 700, 24, [0, 1, 650, 699]
+    q, k, v, dy = _inputs(N, L, *heads, 2, 2, Dk, Dv, dtype)
+    g, n = torch.tensor([-0.1, -0.01], device="cuda"), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    width = 2 * Dv + (heads[0] + heads[1]) * Dk
+    buf = torch.full((N, L, width + 1), 7.0, dtype=TORCH[dtype], device="cuda")
+    parts = buf[:, :, 1:].split([2 * Dv, heads[0] * Dk, heads[1] * Dk], 2)
+    dv, dq, dk = [t.unflatten(2, (h, -1)) for t, h in zip(parts, (2, *heads))]
+    want = _run(q, k, v, g, dy, lengths=n)
+    S.linear_attention(q, k, v, g, lengths=n, y=dv)
+    assert torch.equal(dv, want[0])
+    S.linear_attention_backward(dy, q, k, v, g, lengths=n, out=(dq, dk, dv))
+    for a, b in zip((dq, dk, dv), want[2:5]):
+        assert torch.equal(a, b)
+        for i, e in enumerate(lengths):
+            assert not a[i, e:].any() and (e == 0 or bool(a[i, :e].any()))
+    assert bool((buf[:, :, 0] == 7.0).all())
+
+
 def test_work_on_both_streams_at_once():
     """A call on the current stream and one on another, in flight together."""
     call = _calls()["attention"]
