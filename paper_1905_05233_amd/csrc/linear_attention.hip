@@ -1010,7 +1010,7 @@ constexpr int columns_of(int waves) { return 16 * waves; }
 int64_t blocks_of(int vd, int waves) { return (vd + columns_of(waves) - 1) / columns_of(waves); }
 // Workgroups that a compute unit holds of a form: two where LDS has room, of 8 waves that
 // hold the state one, by its registers.
-int64_t room_of(int dtype, const Form& f) { return device_cu_count() * (f.waves == 4 && f.kd <= (dtype == kF32 ? 0 : 64) ? 2 : 1); }
+int64_t room_of(int dtype, const Form& f, int64_t units) { return units * (f.waves == 4 && f.kd <= (dtype == kF32 ? 0 : 64) ? 2 : 1); }
 
 // The time of a form's tile beside the others', in eighths: of 256 heads of 2048 steps in
 // bf16 4.2 us for 128 channels and 8 waves, 3.7 for 4 waves, 2.7 for 64 channels.
@@ -1034,7 +1034,7 @@ struct Cut {
 // slower on average than the best of all that were timed, and 10 of them more than 10 %.
 constexpr int64_t kStart = 3, kLaunch = 2, kJoin = 4, kRounds = 4;   // in halves of a tile's time, 1.3 us
 constexpr int64_t kJoinSegments = 8, kJoinBytes = 6'000'000;         // that cost one more
-Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes, bool apart) {
+Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes, bool apart, int64_t cus) {
     Cut c{};
     int kd = 0, vd = 0;
     for (int p = 0; p < passes; ++p) kd = std::max(kd, dims[p][0]), vd = std::max(vd, dims[p][1]);
@@ -1046,7 +1046,7 @@ Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int
     c.segments = 1, c.each = static_cast<int32_t>(tiles);
     if (N * H == 0) return c;
     auto time_of = [&](const Form& f, int64_t workgroups, double each) {
-        const int64_t room = room_of(dtype, f);
+        const int64_t room = room_of(dtype, f, cus);
         return static_cast<double>((workgroups + room - 1) / room) * (each * static_cast<double>(tile_time(f)) / static_cast<double>(tile_time(joint)) + kStart);
     };
     auto passes_time = [&](int64_t segments, int64_t each) {   // those of one form go together
@@ -1060,7 +1060,7 @@ Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int
         return time;
     };
     const int chains = std::min(passes, 2);
-    const int64_t units = N * H * blocks_of(dims[passes - 1][1], c.states.waves), room = room_of(dtype, c.states);
+    const int64_t units = N * H * blocks_of(dims[passes - 1][1], c.states.waves), room = room_of(dtype, c.states, cus);
     c.time = passes_time(1, tiles);
     for (int64_t fill = room / 2; fill <= kRounds * room; fill += room / 2) {
         if (units * passes >= fill) continue;
@@ -1078,9 +1078,16 @@ Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int
 // form of its own channels: gradients of 16 x 4096 steps of 8 heads of 128 and 64 channels
 // in bf16 476 and 384 us, of one step of 64 of such a head 13 and 20 us.
 Cut cut_of(int dtype, int64_t N, int64_t L, int64_t H, const int (*dims)[2], int passes) {
-    const Cut joint = cut_of(dtype, N, L, H, dims, passes, false), apart = cut_of(dtype, N, L, H, dims, passes, true);
-    for (int p = 0; p < passes; ++p)
-        if (tile_steps(dtype == kBF16, apart.form[p].kd) != joint.tile) return joint;
+    const int64_t cus = device_cu_count();   // asked once: a call computes this twice, in some tenths of a microsecond
+    const Cut joint = cut_of(dtype, N, L, H, dims, passes, false, cus);
+    bool same = true;
+    for (int p = 0; p < passes; ++p) {
+        const Form own = form_of(dtype, dims[p][0], dims[p][1]);
+        if (tile_steps(dtype == kBF16, own.kd) != joint.tile) return joint;
+        same = same && own == joint.form[p];
+    }
+    if (same) return joint;
+    const Cut apart = cut_of(dtype, N, L, H, dims, passes, true, cus);
     return apart.time < joint.time ? apart : joint;
 }
 

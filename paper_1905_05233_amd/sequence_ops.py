@@ -152,8 +152,10 @@ def _out_heads(t, name, shape, like):
 
 
 def _new_f32(like, *shape):
-    """A contiguous fp32 tensor of two or three dimensions on like's GPU."""
+    """A contiguous fp32 tensor of two to four dimensions on like's GPU."""
     strides = (shape[1], 1) if len(shape) == 2 else (shape[1] * shape[2], shape[2], 1)
+    if len(shape) == 4:
+        strides = (shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3], 1)
     return torch.empty_strided(shape, strides, dtype=torch.float32, device=like.device)
 
 
@@ -365,7 +367,7 @@ def linear_attention(q, k, v, log_decay, s0=None, lengths=None, scale=None, y=No
     y, yh = _out_heads(y, "y", (Nn, L, H, Dv), v)
     sp = 0 if s0 is None else _dense(s0, "s0", (Nn, H, Dk, Dv), torch.float32, dev)
     lp = 0 if lengths is None else _dense(lengths, "lengths", (Nn,), torch.int32, dev)
-    s_last = torch.empty((Nn, H, Dk, Dv), dtype=torch.float32, device=q.device)
+    s_last = _new_f32(q, Nn, H, Dk, Dv)
     need = _attention_size(dev, 0, code, Nn, L, sizes)
     ws = _workspace(need, q)
     st = N.lib().winograd_linear_attention(
@@ -399,7 +401,7 @@ def linear_attention_backward(dy, q, k, v, log_decay, s0=None, ds_last=None, len
     dq, dqh = _out_heads(out[0], "dq", q.shape, q)
     dk, dkh = _out_heads(out[1], "dk", k.shape, k)
     dv, dvh = _out_heads(out[2], "dv", v.shape, v)
-    ds0 = torch.empty((Nn, H, Dk, Dv), dtype=torch.float32, device=q.device)
+    ds0 = _new_f32(q, Nn, H, Dk, Dv)
     need = _attention_size(dev, 1, code, Nn, L, sizes)
     ws = _workspace(need, q)
     st = N.lib().winograd_linear_attention_backward(
