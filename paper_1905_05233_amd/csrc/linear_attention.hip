@@ -383,6 +383,11 @@ template <typename Elem, int K, int W, bool STATES> struct Shape {
     struct Lds : Least {
         Steps steps[kStages];
     };
+    // Whether the weights' waves load and unpack q: where unpacking is what a tile waits for, with
+    // inputs in several parts or one stage.  32 x 1024 steps of 8 heads of 64 channels in fp16,
+    // gradients, 152 to 137 us; 16 x 1024 of 128 in fp32 315 to 298; 8 x 1024 of 256 in bf16 257
+    // to 249; but 32 x 2048 of 128 in bf16, whose loads would crowd them, 411 to 432.
+    static constexpr bool kOwnQ = PI > 1 || kStages == 1;
     // W waves for the state, half as many for memory and, but for STATES, as many for the
     // weights.  Twice as many of these where inputs have several parts, if a compute unit
     // holds one such workgroup: 16 x 1024 steps of 8 heads of 128 channels in fp32 152 to
@@ -401,7 +406,8 @@ template <int RUNS> __device__ __forceinline__ int output_at(int row, int run) {
 //   * W hold the state, 16 columns each: they multiply it by q, add what the tile's own
 //     steps give (weights times v), and bring the state over the tile;
 //   * W / 2 load the tile after the next and unpack the next one;
-//   * W / 2 store the last tile's outputs and make the weights (q.k, decayed) of the next.
+//   * W / 2 store the last tile's outputs and make the weights (q.k, decayed) of the next; of
+//     some forms they load and unpack q, too.
 // Two barriers a tile: ahead of the first, tile t's outputs are made, those of tile t - 1
 // leave and tile t + 1 is unpacked; ahead of the second, the state is brought over tile t
 // and the weights of tile t + 1 are made.  Loads go out on both sides of the first, since
@@ -650,7 +656,7 @@ void attention_kernel(Args) {
         };
         auto load_others = [&](int32_t t) {
             if (t >= t_end) return;
-            if constexpr (!STATES) lq.load(row_of(t), rows_of(t), kd);
+            if constexpr (!STATES && !Sh::kOwnQ) lq.load(row_of(t), rows_of(t), kd);
             lv.load(row_of(t), rows_of(t), vd);
         };
         auto unpack = [&](int32_t t) {
@@ -660,7 +666,7 @@ void attention_kernel(Args) {
             auto& to = stage_of(t);
             lk.trim(whole, rows, kd);
             lk.template store<true, PI>(to.k);
-            if constexpr (!STATES) {
+            if constexpr (!STATES && !Sh::kOwnQ) {
                 lq.trim(whole, rows, kd);
                 lq.template store<false, PI>(to.q);
             }
@@ -788,6 +794,20 @@ void attention_kernel(Args) {
                 }
             }
         };
+        TileLoad<Elem, T, KD, Sh::kWeights> lq(tid, heads_at<Elem>(pass.q, n, h), pass.q.sl, 0, kd);
+        auto load_q = [&](int32_t t) {
+            if constexpr (Sh::kOwnQ)
+                if (t < t_end) lq.load(row_of(t), rows_of(t), kd);
+        };
+        auto unpack_q = [&](int32_t t) {
+            if constexpr (Sh::kOwnQ) {
+                if (t >= t_end) return;
+                const int rows = rows_of(t);
+                lq.trim(kd == KD && rows == T, rows, kd);
+                lq.template store<false, PI>(stage_of(t).q);
+            }
+        };
+        if constexpr (STAGES == 2) load_q(t_first);
         // weights above the diagonal are zeros that nothing writes
         for (int i = tid; i < static_cast<int>(sizeof(lds.own.weights) / 4); i += Sh::kWeights)
             reinterpret_cast<uint32_t*>(&lds.own.weights)[i] = 0;
@@ -795,10 +815,13 @@ void attention_kernel(Args) {
         __syncthreads();
         for (int32_t t = t_first - 1; t < t_end; ++t) {
             if (!y_f32 && t > t_first) put(lds.own, static_cast<Elem*>(pass.y.p), t - 1, tid, [] { return Sh::kWeights; });
+            if constexpr (STAGES == 2) unpack_q(t + 1);
+            load_q(t + STAGES);
             __syncthreads();
             if constexpr (STAGES == 2) weigh(t + 1);
             __syncthreads();
             if constexpr (STAGES == 1) {
+                unpack_q(t + 1);
                 __syncthreads();
                 weigh(t + 1);
                 __syncthreads();
