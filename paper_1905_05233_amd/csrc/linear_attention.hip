@@ -29,7 +29,7 @@
 // Bound, for bf16 heads of 128 channels, by a tile's latency close to memory: 256 sequences
 // and heads of 2048 steps take 138 us, 3.9 TB/s of the 5.1 that a copy reaches; of 64
 // channels 85 us (3.2 TB/s); of 128 in fp32, where nine products stand for one and every
-// value is taken apart, 410 us (2.6 TB/s at twice the bytes).  A few heads' sequences are
+// value is taken apart, about 400 us (2.7 TB/s at twice the bytes).  A few heads' sequences are
 // bound by the start of the three launches, 4 to 8 us each, of which the code's own way to the
 // compute units is a part: 16381 steps of 4 heads of 128 channels take 52 us, their bytes 13.
 #include <hip/hip_runtime.h>
