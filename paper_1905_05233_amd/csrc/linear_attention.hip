@@ -114,10 +114,10 @@ __device__ __forceinline__ int32_t steps_of(const int32_t* lengths, int64_t n, i
     return v < 0 ? 0 : (v > L ? L : v);
 }
 
-// log2(lambda); where lambda is 0 a number whose every multiple but that by 0 is a
-// power that is 0 in fp32.
+// log2(lambda); from -1e30 on down, infinity included, a number whose every multiple by a
+// step count is finite and, but that by 0, a power that is 0 in fp32.
 __device__ __forceinline__ float log2_of(float log_decay) {
-    return log_decay == -__builtin_inff() ? -1e30f : log_decay * kLog2e;
+    return log_decay < -1e30f ? -1e30f : log_decay * kLog2e;
 }
 __device__ __forceinline__ float power(float log2_decay, int n) {
     return __builtin_amdgcn_exp2f(log2_decay * static_cast<float>(n));
