@@ -556,7 +556,9 @@ typedef struct {
  * [N][heads][Dk][Dv] and lengths [N] are contiguous; log_decay is 0 or less (minus
  * infinity: nothing is kept).  lengths (NULL: every sequence has L steps; values are
  * clipped to [0, L]): steps from lengths[n] on are padding; nothing there is used, y
- * is 0 and the state stays.  An infinity or NaN at a step reaches no y ahead of it.
+ * is 0 and the state stays.  An infinity or NaN at a step reaches no y ahead of it, and
+ * goes on from there as the recurrence has it.  (Where a sum exceeds fp32's range, or an
+ * fp32 value is not below 2^128 (1 - 2^-9), NaN may stand for an infinity.)
  * workspace: of winograd_linear_attention_workspace bytes, 16-byte aligned (NULL if
  * that is 0).  N >= 1, 0 <= L <= 2^31 - 2^16, heads <= 65536, 1 <= Dk, Dv <= 256. */
 typedef struct {

@@ -55,6 +55,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;   // of the kernels beside the attention itself
 constexpr size_t kLdsBytes = 160 * 1024;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLeastLog = -103.972077f;   // -150 log(2), up to which a decay is 0 in fp32
 
 // bf16 parts of an input; of the values computed in fp32 that outputs are made of, whose
 // 2^-16 is small beside the outputs' rounding (2^-9; three parts: 166 us for 138 at 256 heads
@@ -206,6 +207,15 @@ template <int PLANES, int ROWS, int WIDTH> struct alignas(512) TileLds {
     // instruction.
     template <typename T> static __device__ __forceinline__ T read(int place) {
         return *(const __attribute__((address_space(3))) T*)(static_cast<uint32_t>(place));
+    }
+    // the values of 4 channels side by side
+    static __device__ __forceinline__ void four(int place, float (&x)[4]) {
+#pragma unroll
+        for (int p = PLANES - 1; p >= 0; --p) {
+            const bf16x4 f = read<bf16x4>(place + p * kPlane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = p == PLANES - 1 ? static_cast<float>(f[e]) : x[e] + static_cast<float>(f[e]);
+        }
     }
     // 8 channels, as a matrix instruction takes them of its row (or column): lane m + 16 g
     // holds those from 8 g on of row m
@@ -372,7 +382,8 @@ template <typename Elem, int K, int W, bool STATES> struct Shape {
         TileLds<PS, 32 * kPanels, 32> weights;
         // a tile's outputs: two tiles in the storage type, or one in fp32
         u32x4 outputs[T * kColumns / 4 * (sizeof(Elem) == 4 ? 2 : 1)];
-        int32_t odd[2];                   // the tile (+ 1) of which v holds an infinity or NaN
+        int32_t odd[2];                   // the tile (+ 1) of which q, k or v holds an infinity or NaN
+        float whole[2];                   // the decay over a tile, and over the sequence's last one
     };
     struct Least {
         alignas(16) float in_decay[T];    // from a tile's steps to the state behind it
@@ -404,7 +415,8 @@ template <int RUNS> __device__ __forceinline__ int output_at(int row, int run) {
 // A pass, or (STATES) only what its segments add to the state.  The waves of a workgroup
 // have three tasks, so that some work where others wait:
 //   * W hold the state, 16 columns each: they multiply it by q, add what the tile's own
-//     steps give (weights times v), and bring the state over the tile;
+//     steps give (weights times v), and bring the state over the tile; where q, k, v or the
+//     state holds an infinity or NaN they go step by step instead;
 //   * W / 2 load the tile after the next and unpack the next one;
 //   * W / 2 store the last tile's outputs and make the weights (q.k, decayed) of the next; of
 //     some forms they load and unpack q, too.
@@ -489,6 +501,83 @@ void attention_kernel(Args) {
         }
         float whole = 1.0f, out_decay[IB];   // the decays over a tile, and from the state to its steps
         int decays_of = 0;
+        auto has_infinity = [&] {            // of the wave's columns of the state
+            bool found = false;
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) found = found || __builtin_isinf(S[b][r]);
+            return __any(found) != 0;
+        };
+        bool infinite = !STATES && pass.s_in && has_infinity();
+        // A tile by the recurrence itself, which needs of the state only the lane's own values: where
+        // an infinity or NaN takes part, products with weights of zero or with lower parts would make
+        // NaN of what the recurrence keeps finite or infinite.  64 steps of 128 channels take 100 us so.
+        auto step_by_step = [&](const auto& now, auto& own, int32_t t, int live) {
+            // all from numbers that are taken to be new ones, or registers hold it over all tiles
+            const int place = renewed(lane), g = place / 16, c = 16 * wave + place % 16, rows = kd - 8 * g;
+            float log_keep = log_decay;
+            asm volatile("" : "+v"(log_keep));
+            const float keep = expf(log_keep);
+#pragma unroll 1
+            for (int i = 0; i < live; ++i) {
+                const int j = reverse ? live - 1 - i : i, at = K::place(j, 8 * g), swap = j >> 3 & 1;
+                const float x = pass.in_scale * now.v.value(j, c);
+                float sum = 0.0f;
+#pragma unroll
+                for (int b = 0; b < KD / 16; ++b) {
+                    float fk[4], fq[4];
+                    K::four(((now.k.start() + at) ^ 64 * (b / 2)) + 8 * (b % 2 ^ swap), fk);
+                    K::four(((now.q.start() + at) ^ 64 * (b / 2)) + 8 * (b % 2), fq);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (32 * (b / 2) + 4 * (b % 2) + r >= rows) continue;
+                        const float s = reverse ? fmaf(fk[r], x, S[b][r]) : fmaf(keep, S[b][r], fk[r] * x);
+                        sum = fmaf(fq[r], s, sum);
+                        S[b][r] = reverse ? keep * s : s;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                const float y = pass.out_scale * sum;
+                if (g != 0) continue;
+                if (y_f32) {
+                    reinterpret_cast<float*>(&own.outputs[output_at<VB / 4>(j, c / 4)])[c % 4] = y;
+                } else {
+                    constexpr int kPer = 16 / sizeof(Elem), RUNS = VB / kPer;
+                    auto* run = &own.outputs[(t & 1) * T * RUNS + output_at<RUNS>(j, c / kPer)];
+                    reinterpret_cast<Elem*>(run)[c % kPer] = Storage<Elem>::from_f32(y);
+                }
+            }
+            infinite = has_infinity();
+        };
+        // The same for a segment's sums, in which an infinity or NaN stays: from memory, behind all
+        // tiles, which costs those of other segments nothing (256 steps of 128 channels: 340 us).
+        auto segment_step_by_step = [&] {
+            const Elem* k = heads_at<Elem>(pass.k, n, h);
+            const Elem* v = heads_at<Elem>(pass.v, n, h) + min(column, vd - 1);
+            const float keep = expf(log_decay);
+            const int32_t low = reverse ? t_end - 1 : t_first, high = reverse ? t_first : t_end - 1;
+            const int32_t first = row_of(low), end = row_of(high) + rows_of(high);
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b) S[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (int32_t i = 0; i < end - first; ++i) {
+                const int64_t row = reverse ? end - 1 - i : first + i;
+                const float x = pass.in_scale * Storage<Elem>::to_f32(v[row * pass.v.sl]);
+                const int l = renewed(kd - 1);
+#pragma unroll
+                for (int b = 0; b < KD / 16; ++b) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float kk = Storage<Elem>::to_f32(k[row * pass.k.sl + min(row_of_state(b, r), l)]);
+                        S[b][r] = reverse ? keep * fmaf(kk, x, S[b][r]) : fmaf(keep, S[b][r], kk * x);
+                    }
+                    if (b % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        };
         if (any) {                           // the first tile and its weights
 #pragma unroll
             for (int i = 0; i < 2 * (STATES ? 0 : 1) + (STAGES == 2 ? 1 : STATES ? 2 : 3); ++i) __syncthreads();
@@ -497,9 +586,12 @@ void attention_kernel(Args) {
             const auto& now = stage_of(t);
             const int live = rows_of(t);
             const int v_place[2] = {now.v.start() + v_own[0], now.v.start() + v_own[1]};
+            int flag = 0;
+            if constexpr (!STATES) flag = lds.own.odd[t & 1], whole = lds.own.whole[live < T];
+            bool odd = false;
             if (live != decays_of) {
                 decays_of = live;
-                whole = exact_power(log_decay, live);
+                if constexpr (STATES) whole = exact_power(log_decay, live);
                 const int j = threadIdx.x;
                 if (j < T) lds.in_decay[j] = pass.in_scale * power(log2_decay, reverse ? j + 1 : max(0, live - 1 - j));
                 if constexpr (STATES) __syncthreads();
@@ -508,7 +600,6 @@ void attention_kernel(Args) {
                     out_decay[i] = pass.out_scale * power(log2_decay, reverse ? max(0, live - 1 - (16 * i + m)) : 16 * i + m + 1);
             }
             if constexpr (!STATES) {
-                const bool odd = lds.own.odd[t & 1] == t + 1;
                 const int q_place = now.q.start() + q_own;
                 f32x4 O[IB];
 #pragma unroll
@@ -526,9 +617,10 @@ void attention_kernel(Args) {
                     for (int i = 0; i < IB; ++i) now.q.across(place + 32 * i * KD, fq[i]);
                     multiply<PS, PI, PS>([&](int, int p) { return fs.part[p]; }, [&](int i, int p) { return fq[i][p]; }, O);
                 }
-#pragma unroll
-                for (int i = 0; i < IB; ++i) O[i] *= out_decay[i];
+                odd = infinite || __builtin_amdgcn_readfirstlane(flag) == t + 1;   // (behind the products: it waits for the flag)
                 if (!odd) {
+#pragma unroll
+                    for (int i = 0; i < IB; ++i) O[i] *= out_decay[i];
                     using P = decltype(lds.own.weights);
                     const int p_place = lds.own.weights.start() + P::place(m, 8 * g);
 #pragma unroll
@@ -546,79 +638,72 @@ void attention_kernel(Args) {
                             O[i] = pair[0], O[i + 1] = pair[1];
                         }
                     }
-                } else {
-                    // step by step: a weight of zero would not remove an infinity or NaN of a later v
-#pragma unroll 1
-                    for (int j = 0; j < T; ++j)
+                    const int c = 4 * wave + g;
+                    if (y_f32) {
+#pragma unroll
+                        for (int i = 0; i < IB; ++i)
+                            lds.own.outputs[output_at<VB / 4>(16 * i + m, c)] = __builtin_bit_cast(u32x4, O[i]);
+                    } else {
+                        struct alignas(4 * sizeof(Elem)) Four {
+                            Elem v[4];
+                        };
+                        constexpr int kPer = 16 / sizeof(Four), RUNS = VB * sizeof(Elem) / 16;
 #pragma unroll
                         for (int i = 0; i < IB; ++i) {
-                            const int row = 16 * i + m;
-                            if (reverse ? j < row : j > row) continue;
-                            const float w = lds.own.weights.value(32 * (i / 2 + j / 32) + 16 * (i % 2) + m, j % 32);
+                            Four four;
+                            if constexpr (std::is_same_v<Elem, bf16_t>) {   // in pairs
+                                const bf16x4 e = {static_cast<__bf16>(O[i][0]), static_cast<__bf16>(O[i][1]), static_cast<__bf16>(O[i][2]),
+                                                  static_cast<__bf16>(O[i][3])};
+                                four = __builtin_bit_cast(Four, e);
+                            } else {
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) O[i][r] += w * now.v.value(j, 16 * wave + 4 * g + r);
+                                for (int r = 0; r < 4; ++r) four.v[r] = Storage<Elem>::from_f32(O[i][r]);
+                            }
+                            auto* run = &lds.own.outputs[(t & 1) * T * RUNS + output_at<RUNS>(16 * i + m, c / kPer)];
+                            reinterpret_cast<Four*>(run)[c % kPer] = four;
                         }
-                }
-                const int c = 4 * wave + g;
-                if (y_f32) {
-#pragma unroll
-                    for (int i = 0; i < IB; ++i)
-                        lds.own.outputs[output_at<VB / 4>(16 * i + m, c)] = __builtin_bit_cast(u32x4, O[i]);
-                } else {
-                    struct alignas(4 * sizeof(Elem)) Four {
-                        Elem v[4];
-                    };
-                    constexpr int kPer = 16 / sizeof(Four), RUNS = VB * sizeof(Elem) / 16;
-#pragma unroll
-                    for (int i = 0; i < IB; ++i) {
-                        Four four;
-                        if constexpr (std::is_same_v<Elem, bf16_t>) {   // in pairs
-                            const bf16x4 e = {static_cast<__bf16>(O[i][0]), static_cast<__bf16>(O[i][1]), static_cast<__bf16>(O[i][2]),
-                                              static_cast<__bf16>(O[i][3])};
-                            four = __builtin_bit_cast(Four, e);
-                        } else {
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) four.v[r] = Storage<Elem>::from_f32(O[i][r]);
-                        }
-                        auto* run = &lds.own.outputs[(t & 1) * T * RUNS + output_at<RUNS>(16 * i + m, c / kPer)];
-                        reinterpret_cast<Four*>(run)[c % kPer] = four;
                     }
                 }
+            }
+            if constexpr (!STATES) {
+                if (odd) step_by_step(now, lds.own, t, live);
                 __syncthreads();
             }
+            if (!odd) {
 #pragma unroll
-            for (int b = 0; b < KD / 16; ++b) S[b] *= whole;
-            Split<kStateParts, 8, false> late[JS];
-#pragma unroll
-            for (int s = 0; s < JS; ++s) {
-                bf16x8 fv[PI];
-                now.v.down(v_place[0] + 64 * s * VB, v_place[1] + 64 * s * VB, fv);
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float sum = static_cast<float>(fv[PI - 1][e]);
-#pragma unroll
-                    for (int p = PI - 2; p >= 0; --p) sum += static_cast<float>(fv[p][e]);
-                    x[e] = sum * lds.in_decay[32 * s + 8 * g + e];
-                }
-                late[s].of(x);
-            }
-            const int k_place[2] = {now.k.start() + k_own[0], now.k.start() + k_own[1]};
-#pragma unroll
-            for (int b = 0; b < KD / 16; b += 2) {
-                f32x4 pair[2] = {S[b], S[b + 1]};
-                int own[2][2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) own[u][0] = renewed(k_place[0]) ^ (32 * b + 8 * u), own[u][1] = renewed(k_place[1]) ^ (32 * b + 8 * u);
+                for (int b = 0; b < KD / 16; ++b) S[b] *= whole;
+                Split<kStateParts, 8, false> late[JS];
 #pragma unroll
                 for (int s = 0; s < JS; ++s) {
-                    bf16x8 fk[2][PI];
+                    bf16x8 fv[PI];
+                    now.v.down(v_place[0] + 64 * s * VB, v_place[1] + 64 * s * VB, fv);
+                    float x[8];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) now.k.down(own[u][0] + 64 * s * KD, own[u][1] + 64 * s * KD, fk[u]);
-                    multiply<PI, kStateParts, kStateParts>([&](int i, int p) { return fk[i][p]; },
-                                                           [&](int, int p) { return late[s].part[p]; }, pair);
+                    for (int e = 0; e < 8; ++e) {
+                        float sum = static_cast<float>(fv[PI - 1][e]);
+#pragma unroll
+                        for (int p = PI - 2; p >= 0; --p) sum += static_cast<float>(fv[p][e]);
+                        x[e] = sum * lds.in_decay[32 * s + 8 * g + e];
+                    }
+                    late[s].of(x);
                 }
-                S[b] = pair[0], S[b + 1] = pair[1];
+                const int k_place[2] = {now.k.start() + k_own[0], now.k.start() + k_own[1]};
+#pragma unroll
+                for (int b = 0; b < KD / 16; b += 2) {
+                    f32x4 pair[2] = {S[b], S[b + 1]};
+                    int own[2][2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) own[u][0] = renewed(k_place[0]) ^ (32 * b + 8 * u), own[u][1] = renewed(k_place[1]) ^ (32 * b + 8 * u);
+#pragma unroll
+                    for (int s = 0; s < JS; ++s) {
+                        bf16x8 fk[2][PI];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) now.k.down(own[u][0] + 64 * s * KD, own[u][1] + 64 * s * KD, fk[u]);
+                        multiply<PI, kStateParts, kStateParts>([&](int i, int p) { return fk[i][p]; },
+                                                               [&](int, int p) { return late[s].part[p]; }, pair);
+                    }
+                    S[b] = pair[0], S[b + 1] = pair[1];
+                }
             }
             __syncthreads();
             if constexpr (STAGES == 1) {
@@ -626,8 +711,17 @@ void attention_kernel(Args) {
                 if constexpr (!STATES) __syncthreads();
             }
         }
-        if constexpr (STATES) store_state(pass.s_out + by_segment);
-        else if (pass.s_out && segment == a.segments - 1) store_state(pass.s_out + head * size);
+        if constexpr (STATES) {
+            bool finite = true;
+#pragma unroll
+            for (int b = 0; b < KD / 16; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(S[b][r]);
+            if (!__all(finite)) segment_step_by_step();
+            store_state(pass.s_out + by_segment);
+        } else if (pass.s_out && segment == a.segments - 1) {
+            store_state(pass.s_out + head * size);
+        }
         return;
     }
 
@@ -671,9 +765,9 @@ void attention_kernel(Args) {
                 lq.template store<false, PI>(to.q);
             }
             lv.trim(whole, rows, vd);
+            lv.template store<false, PI>(to.v);
             if constexpr (!STATES)
                 if (!lv.finite()) lds.own.odd[t & 1] = t + 1;
-            lv.template store<false, PI>(to.v);
         };
         if (STAGES == 2 && any) {
             load_k(t_first);
@@ -734,6 +828,7 @@ void attention_kernel(Args) {
             if (t >= t_end) return;
             const auto& now = stage_of(t);
             const int k_place = now.k.start() + own_place, q_place = now.q.start() + own_place;
+            float size = 0.0f;   // on the diagonal, where every step's q and k take part
             // in blocks of 16 x 16 of the triangle, two at a time
 #pragma unroll
             for (int first = 0; first < BLOCKS; first += 2 * Sh::kHelpers) {
@@ -779,7 +874,10 @@ void attention_kernel(Args) {
                     const int apart = reverse ? jb[u] - ib[u] : ib[u] - jb[u];
                     if (apart == 0) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) x[r] = d0 + (reverse ? r : -r) < 0 ? 0.0f : w[u][r] * here[r];
+                        for (int r = 0; r < 4; ++r) {
+                            x[r] = d0 + (reverse ? r : -r) < 0 ? 0.0f : w[u][r] * here[r];
+                            size += fabsf(w[u][r]);
+                        }
                     } else {
                         const float more = apart == 1 ? 1.0f : apart == 2 ? far_by[0] : far_by[1];
 #pragma unroll
@@ -793,6 +891,7 @@ void attention_kernel(Args) {
                     for (int p = 0; p < PS; ++p) to.template at<bf16x4>(to.place(row, c), p) = parts.part[p];
                 }
             }
+            if (!__builtin_isfinite(size)) lds.own.odd[t & 1] = t + 1;
         };
         TileLoad<Elem, T, KD, Sh::kWeights> lq(tid, heads_at<Elem>(pass.q, n, h), pass.q.sl, 0, kd);
         auto load_q = [&](int32_t t) {
@@ -812,6 +911,8 @@ void attention_kernel(Args) {
         for (int i = tid; i < static_cast<int>(sizeof(lds.own.weights) / 4); i += Sh::kWeights)
             reinterpret_cast<uint32_t*>(&lds.own.weights)[i] = 0;
         if (tid < 2) lds.own.odd[tid] = 0;
+        // (here, since its constants would take registers of the waves that hold the state)
+        if (tid < 2) lds.own.whole[tid] = exact_power(log_decay, tid == 0 ? T : steps - (tiles - 1) * T);
         __syncthreads();
         for (int32_t t = t_first - 1; t < t_end; ++t) {
             if (!y_f32 && t > t_first) put(lds.own, static_cast<Elem*>(pass.y.p), t - 1, tid, [] { return Sh::kWeights; });
@@ -869,6 +970,7 @@ __global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
     const float whole = exact_power(log_decay, a.each_steps), at_cut = exact_power(log_decay, rest);
     const float at_first = exact_power(log_decay, max(0, static_cast<int32_t>(min(each, end)) - (c.reverse ? last : 0)));
     const int32_t adding = a.segments - 1, filled = cut + (rest > 0);
+    const bool lasts = log_decay > kLeastLog;   // an infinity stays one, though its decay over a segment be 0
     for (int32_t w = 0; w < a.segments; w += U) {
         float add[U];
 #pragma unroll
@@ -877,7 +979,9 @@ __global__ __launch_bounds__(kThreads) void chain_kernel(ChainArgs a) {
         for (int u = 0; u < U; ++u) {
             if (w + u >= a.segments) break;
             s[(w + u) * size] = run;
-            if (w + u < min(adding, filled)) run = fmaf(w + u == 0 ? at_first : w + u == cut ? at_cut : whole, run, add[u]);
+            if (w + u >= min(adding, filled)) continue;
+            const float decay = lasts && __builtin_isinf(run) ? 1.0f : w + u == 0 ? at_first : w + u == cut ? at_cut : whole;
+            run = fmaf(decay, run, add[u]);
         }
     }
 }

@@ -1,5 +1,6 @@
 """Linear attention at the ends of its numbers' ranges: decays down to the lowest finite
-one, for sequences, their gradients and the single step."""
+one, and infinities and NaN, which go on as the recurrence has them; for sequences, their
+gradients and the single step."""
 import numpy as np
 import pytest
 import torch
@@ -54,3 +55,102 @@ def test_decays_that_keep_nothing(decay, dtype):
     ref = A.attention(*[_np(t[:, :1]) for t in (q, k, v)], _np(g), _np(s0), None, 24 ** -0.5, dtype)
     R.assert_close(_np(y)[:, None], *ref["y"], dtype, "y")
     R.assert_close(_np(s), *ref["s_last"], "f32", "s")
+
+
+def _hold(got, ref, dtype, lengths=None):
+    """Infinities and NaN where the reference has them, all else within its bound."""
+    for name in got:
+        (want, bound), t = ref[name], _np(got[name])
+        if lengths is not None and name in ("y", "dq"):   # padding, of which the reference makes 0 times the state
+            for n, e in enumerate(lengths):
+                want[n, e:] = bound[n, e:] = 0.0
+        fine = np.isfinite(want)
+        assert np.array_equal(np.isnan(t), np.isnan(want)), (name, "NaN", np.argwhere(np.isnan(t) != np.isnan(want))[:4].tolist())
+        assert np.array_equal(t[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), (name, "infinity")
+        assert np.isfinite(bound[fine]).all()
+        R.assert_close(t[fine], want[fine], bound[fine], "f32" if name in ("s_last", "ds0") else dtype, name)
+
+
+# sequences, steps, heads, channels of q and k and of v: one for each width of a state and of
+# its columns, the last ones long enough to go in segments
+SHAPES = [(2, 70, 2, 24, 40), (1, 100, 1, 64, 64), (1, 130, 1, 100, 128), (1, 90, 1, 40, 100), (1, 70, 1, 200, 30),
+          (1, 65, 1, 130, 256), (1, 3, 1, 5, 3), (1, 1500, 1, 32, 80), (2, 700, 2, 64, 64), (1, 900, 1, 130, 70)]
+INPUTS = ("q", "k", "v", "dy", "s0", "ds")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("which", INPUTS)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_infinities_go_on_as_the_recurrence_has_them(shape, which, dtype):
+    print(f"[infinities] {shape} {which} {dtype}", flush=True)
+    N, L, H, Dk, Dv = shape
+    g = torch.tensor([-0.01, -0.3][:H], device="cuda")
+    for bad in ([float("inf")], [float("inf"), -float("inf"), float("nan")]):
+        inputs = _inputs(*shape, dtype)
+        t = inputs[INPUTS.index(which)]
+        for i, b in enumerate(bad):
+            if which in ("s0", "ds"):
+                t[0, 0, (5 * i + 1) % Dk, (7 * i + 2) % Dv] = b
+            else:
+                t[0, (L // 3 + 19 * i) % L, 0, (5 * i + 1) % t.shape[-1]] = b
+        got = _run(*inputs, g)
+        with np.errstate(all="ignore"):
+            _hold(got, _reference(*inputs, g, dtype), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("L", [150, 1500])
+def test_infinities_with_lengths_and_shared_heads(L, dtype):
+    N, H, Dk, Dv, lengths = 4, 2, 48, 40, [L, 0, L - 70, 33]
+    q, k, v, dy, s0, ds = _inputs(N, L, H, Dk, Dv, dtype)
+    k, v = k[:, :, :1], v[:, :, 1:]
+    g, n = torch.tensor([-0.02, -0.2], device="cuda"), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    v[0, L // 2, 0, 7] = k[2, 30, 0, 3] = dy[3, 20, 1, 0] = float("inf")
+    q[2, 31, 0, 5] = s0[1, 0, 2, 2] = ds[1, 1, 3, 3] = -float("inf")
+    for i, e in enumerate(lengths):
+        for t in (q, k, v, dy):
+            t[i, e:] = float("inf")      # padding is not used
+    got = _run(q, k, v, dy, s0, ds, g, lengths=n)
+    with np.errstate(all="ignore"):
+        _hold(got, _reference(q, k, v, dy, s0, ds, g, dtype, np.array(lengths)), dtype, lengths)
+    for name in ("y", "dq", "dk", "dv"):
+        for i, e in enumerate(lengths):
+            assert not got[name][i, e:].any(), name
+
+
+def test_infinities_last_over_segments_whose_decay_is_zero():
+    """The decay over a segment may be below fp32's range: an infinity stays all the same."""
+    inputs = _inputs(1, 2000, 1, 24, 40, "bf16")
+    inputs[2][0, 3, 0, 5], inputs[3][0, 1990, 0, 6] = float("inf"), -float("inf")
+    g = torch.tensor([-0.9], device="cuda")
+    got = _run(*inputs, g)
+    with np.errstate(all="ignore"):
+        _hold(got, _reference(*inputs, g, "bf16"), "bf16")
+    assert bool(torch.isinf(got["s_last"][0, 0, :, 5]).all()) and bool(torch.isinf(got["ds0"][0, 0, :, 6]).all())
+
+
+def test_products_beyond_fp32():
+    """q.k of finite inputs may exceed fp32's range where the state and its product with q do not."""
+    N, L, D = 1, 70, 32
+    inputs = [t.clone() for t in _inputs(N, L, 1, D, D, "f32")]
+    inputs[0][0, 20, 0] *= 2.0 ** 70
+    inputs[1][0, 20, 0] *= 2.0 ** 70
+    inputs[2][0, 20, 0] *= 2.0 ** -90
+    g = torch.tensor([-0.1], device="cuda")
+    got, ref = _run(*inputs, g), _reference(*inputs, g, "f32")
+    for name in ("y", "s_last"):
+        assert np.isfinite(ref[name][0]).all() and np.abs(ref[name][0]).max() < 2.0 ** 127
+        R.assert_close(_np(got[name]), *ref[name], "f32", name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("which", ("q", "k", "v", "s0"))
+def test_infinities_in_a_step(which, dtype):
+    from paper_1905_05233_amd import sequence_ops as S
+    inputs, g = _inputs(2, 1, 2, 24, 37, dtype), torch.tensor([-0.01, -0.3], device="cuda")
+    inputs[INPUTS.index(which)][0, 0, 1, 3] = -float("inf")
+    q, k, v, _, s0, _ = inputs
+    y, s = S.linear_attention_step(q[:, 0], k[:, 0], v[:, 0], g, s0)
+    with np.errstate(all="ignore"):
+        ref = A.attention(*[_np(t) for t in (q, k, v)], _np(g), _np(s0), None, 24 ** -0.5, dtype)
+        _hold({"y": y[:, None], "s_last": s}, ref, dtype)
