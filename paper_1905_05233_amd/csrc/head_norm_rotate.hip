@@ -179,26 +179,26 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs<Elem> a) {
             // every lane loads, the last frequency where it turns no pair: all are in flight together
             const uint64_t turns = a.turns[min(runs.pair[u] + j, a.R / 2 - 1)];
             cos_sin(static_cast<uint32_t>((static_cast<uint64_t>(position) * turns) >> 32), co[e], si[e]);
-            if (j >= runs.pairs[u]) co[e] = 1.0f, si[e] = 0.0f;
             if (GRAD) si[e] = -si[e];
         }
+        // Channels that are not turned are chosen as they are: a sine of zero would not keep their
+        // neighbour's infinity out.
+        auto turn_pair = [](float& p, float& q, float c, float s, bool turned) {
+            float a = fmaf(p, c, -(q * s)), b = fmaf(p, s, q * c);
+            asm volatile("" : "+v"(a), "+v"(b));   // a choice, not a branch: the compiler loses values in those
+            p = turned ? a : p;
+            q = turned ? b : q;
+        };
         auto turn = [&](float (&x)[2][V]) {
             if (adjacent) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int j = 0; j < V / 2; ++j) {
-                        const float p = x[u][2 * j], q = x[u][2 * j + 1], cc = co[u * (V / 2) + j], ss = si[u * (V / 2) + j];
-                        x[u][2 * j] = fmaf(p, cc, -(q * ss));
-                        x[u][2 * j + 1] = fmaf(p, ss, q * cc);
-                    }
+                    for (int j = 0; j < V / 2; ++j)
+                        turn_pair(x[u][2 * j], x[u][2 * j + 1], co[u * (V / 2) + j], si[u * (V / 2) + j], j < runs.pairs[u]);
             } else {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float p = x[0][e], q = x[1][e];
-                    x[0][e] = fmaf(p, co[e], -(q * si[e]));
-                    x[1][e] = fmaf(p, si[e], q * co[e]);
-                }
+                for (int e = 0; e < V; ++e) turn_pair(x[0][e], x[1][e], co[e], si[e], runs.pairs[0] > 0);
             }
         };
 #pragma unroll

@@ -1,6 +1,7 @@
 """Linear attention at the ends of its numbers' ranges: decays down to the lowest finite
 one, and infinities and NaN, which go on as the recurrence has them; for sequences, their
-gradients and the single step."""
+gradients and the single step.  And the norm of heads with rotation, where infinities stay
+in the channels that the formula brings them to."""
 import numpy as np
 import pytest
 import torch
@@ -154,3 +155,34 @@ def test_infinities_in_a_step(which, dtype):
     with np.errstate(all="ignore"):
         ref = A.attention(*[_np(t) for t in (q, k, v)], _np(g), _np(s0), None, 24 ** -0.5, dtype)
         _hold({"y": y[:, None], "s_last": s}, ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("D, R_", [(40, 30), (64, 32), (75, 10), (17, 16), (16, 16)])
+def test_infinities_stay_in_channels_that_are_not_turned(D, R_, adjacent, dtype):
+    """An infinite weight is in its channel's outputs alone, or in its pair's; an infinite
+    dy in the gradients of its row, and of the weights of its channel or pair alone."""
+    from paper_1905_05233_amd import sequence_ops as S
+    half = R_ // 2
+    x, dy = [torch.randn((2, 5, 2, D), device="cuda").to(TORCH[dtype]) for _ in range(2)]
+    w, rot, f = torch.ones(D, dtype=TORCH[dtype], device="cuda"), S.Rotary(R_, adjacent=adjacent), [10000.0 ** (-i / half) for i in range(half)]
+    where = np.tile(3 + np.arange(5), (2, 1))      # no angle whose sine or cosine is 0
+    want, bound = A.rotate(_np(x), _np(w), f, where, 1e-6, adjacent)
+    _, (want_w, bound_w) = A.rotate(_np(x), _np(w), f, where, 1e-6, adjacent, _np(dy))
+    for c in range(D):
+        pair = {c} if c >= R_ else {c, c ^ 1} if adjacent else {c, c + half if c < half else c - half}
+        rest = [i for i in range(D) if i not in pair]
+        bad = w.clone()
+        bad[c] = float("inf")
+        y, _ = S.head_norm_rotate(x, x, bad, w, rot, start=3)
+        assert not np.isfinite(_np(y)[..., sorted(pair)]).any()
+        R.assert_close(_np(y)[..., rest], want[..., rest], bound[..., rest], dtype, "y")
+        bad = dy.clone()
+        bad[1, 2, 0, c] = float("inf")
+        dx, _, dw, _ = S.head_norm_rotate_backward(bad, dy, x, x, w, w, rot, start=3)
+        assert not np.isfinite(_np(dw)[sorted(pair)]).any()
+        R.assert_close(_np(dw)[rest], want_w[rest], bound_w[rest], "f32", "dw")
+        keep = torch.ones((2, 5, 2), dtype=torch.bool, device="cuda")
+        keep[1, 2, 0] = False
+        assert bool(torch.isfinite(dx[keep]).all())
