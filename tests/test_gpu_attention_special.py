@@ -58,6 +58,22 @@ def test_decays_that_keep_nothing(decay, dtype):
     R.assert_close(_np(s), *ref["s_last"], "f32", "s")
 
 
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 2, 3, 24, 40), (2, 5, 3, 64, 64), (1, 33, 3, 100, 128), (1, 70, 3, 130, 200), (1, 1500, 3, 64, 72)], ids=str)
+def test_states_of_16_bits_are_fp32s(shape, dtype):
+    """The last state and its gradient come in fp32, whatever the inputs: a term enters the
+    products in three parts (2^-24 of it is left, and 2^-24 by a product of fp16's parts that is
+    left out), and a run of 32 steps in five matrix instructions at most, whose sums may drop
+    2^-23 each: 12 2^-24 of the terms' size, which is the bound of fp32 inputs.  (Two parts, with
+    2^-16 left, would be up to 5 times beyond it here.)"""
+    print(f"[states] {shape} {dtype}", flush=True)
+    inputs, g = _inputs(*shape, dtype), torch.tensor([-0.02, -0.3, -1.0], device="cuda")
+    got, ref = _run(*inputs, g), _reference(*inputs, g, "f32")
+    for name in ("s_last", "ds0"):
+        R.assert_close(_np(got[name]), *ref[name], "f32", name)
+
+
 def _hold(got, ref, dtype, lengths=None):
     """Infinities and NaN where the reference has them, all else within its bound."""
     for name in got:
