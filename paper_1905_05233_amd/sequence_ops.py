@@ -349,7 +349,9 @@ def _attention_size(dev, backward, code, Nn, L, sizes):
 
 
 def _scale(scale, Dk):
-    return float(Dk) ** -0.5 if scale is None and Dk > 0 else scale
+    if scale is None:
+        return float(max(Dk, 1)) ** -0.5   # without channels the library refuses the call
+    return scale
 
 
 def linear_attention(q, k, v, log_decay, s0=None, lengths=None, scale=None, y=None, stream=None):

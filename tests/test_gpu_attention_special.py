@@ -202,3 +202,15 @@ def test_infinities_stay_in_channels_that_are_not_turned(D, R_, adjacent, dtype)
         keep = torch.ones((2, 5, 2), dtype=torch.bool, device="cuda")
         keep[1, 2, 0] = False
         assert bool(torch.isfinite(dx[keep]).all())
+
+
+def test_heads_without_channels_are_refused():
+    from paper_1905_05233_amd import sequence_ops as S
+    from paper_1905_05233_amd._native import WinogradError
+    q, v, g = torch.zeros((2, 5, 1, 0), device="cuda"), torch.zeros((2, 5, 1, 8), device="cuda"), torch.zeros(1, device="cuda")
+    with pytest.raises(WinogradError, match="positive"):
+        S.linear_attention(q, q, v, g)
+    with pytest.raises(WinogradError, match="positive"):
+        S.linear_attention_backward(v, q, q, v, g)
+    with pytest.raises(WinogradError, match="positive"):
+        S.linear_attention_step(q[:, 0], q[:, 0], v[:, 0], g, torch.zeros((2, 1, 0, 8), device="cuda"))
