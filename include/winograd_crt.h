@@ -557,8 +557,9 @@ typedef struct {
  * infinity: nothing is kept).  lengths (NULL: every sequence has L steps; values are
  * clipped to [0, L]): steps from lengths[n] on are padding; nothing there is used, y
  * is 0 and the state stays.  An infinity or NaN at a step reaches no y ahead of it, and
- * goes on from there as the recurrence has it.  (Where a sum exceeds fp32's range, or an
- * fp32 value is not below 2^128 (1 - 2^-9), NaN may stand for an infinity.)
+ * goes on from there as the recurrence has it.  (Where a sum, q.k among them, exceeds
+ * fp32's range, or an fp32 value is not below 2^128 (1 - 2^-9), outputs that it reaches
+ * may be infinities or NaN.)
  * workspace: of winograd_linear_attention_workspace bytes, 16-byte aligned (NULL if
  * that is 0).  N >= 1, 0 <= L <= 2^31 - 2^16, heads <= 65536, 1 <= Dk, Dv <= 256. */
 typedef struct {

@@ -16,9 +16,10 @@
 // All products are the matrix cores' bf16 ones, with sums in fp32.  A value that 8
 // bits do not hold goes in as the sum of two or three bf16 parts, each the rounding
 // of what the ones ahead of it leave: fp16 inputs are exact in two, fp32 ones in
-// three; the state, the weights q.k and the decayed v are held in fp32 and enter in
-// two parts (2^-16 of a value is left) or, for fp32 rows, three.  Products of parts
-// below that are left out.  bf16 has fp32's range, so no state overflows on the way.
+// three; the state and the weights q.k are held in fp32 and enter in two parts (2^-16 of
+// a value is left) or, for fp32 rows, three; the decayed v, of which the state is made, in
+// three.  Products of parts below that are left out.  bf16 has fp32's range, so no state
+// overflows on the way.
 //
 // A workgroup takes a head of a sequence and a block of v's columns, whose state stays in
 // the registers of four or eight waves, 16 columns each, while the tiles go by; other waves
@@ -28,7 +29,7 @@
 //
 // Bound, for bf16 heads of 128 channels, by a tile's latency close to memory: 256 sequences
 // and heads of 2048 steps take 138 us, 3.9 TB/s of the 5.1 that a copy reaches; of 64
-// channels 85 us (3.2 TB/s); of 128 in fp32, where nine products stand for one and every
+// channels 85 us (3.2 TB/s); of 128 in fp32, where six products stand for one and every
 // value is taken apart, about 400 us (2.7 TB/s at twice the bytes).  A few heads' sequences are
 // bound by the start of the three launches, 4 to 8 us each, of which the code's own way to the
 // compute units is a part: 16381 steps of 4 heads of 128 channels take 52 us, their bytes 13.
@@ -58,9 +59,11 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLeastLog = -103.972077f;   // -150 log(2), up to which a decay is 0 in fp32
 
 // bf16 parts of an input; of the values computed in fp32 that outputs are made of, whose
-// 2^-16 is small beside the outputs' rounding (2^-9; three parts: 166 us for 138 at 256 heads
-// of 2048 steps of 128 channels); and of those that the state is made of, which is returned in
-// fp32 (two parts: 134 us)
+// 2^-16 is small beside the outputs' rounding (2^-8 in bf16, 2^-11 in fp16: 2 of 1000 and 10 of
+// 1000 outputs are rounded to the neighbour of what fp32 sums give; with three parts a tenth
+// of these, at 180 us for 151 for 256 heads of 2048 steps of 128 channels, and 323 us for 187 for
+// the gradients of 128 heads of 4096 steps of 64, of which LDS then has no room for two
+// workgroups); and of those that the state is made of, which is returned in fp32 (two parts: 3 % less time)
 template <typename Elem> constexpr int kParts = std::is_same_v<Elem, bf16_t> ? 1 : std::is_same_v<Elem, _Float16> ? 2 : 3;
 template <typename Elem> constexpr int kSums = std::is_same_v<Elem, float> ? 3 : 2;
 constexpr int kStateParts = 3;
@@ -395,10 +398,10 @@ template <typename Elem, int K, int W, bool STATES> struct Shape {
         Steps steps[kStages];
     };
     // Whether the weights' waves load and unpack q: where unpacking is what a tile waits for, with
-    // inputs in several parts or one stage.  32 x 1024 steps of 8 heads of 64 channels in fp16,
-    // gradients, 152 to 137 us; 16 x 1024 of 128 in fp32 315 to 298; 8 x 1024 of 256 in bf16 257
-    // to 249; but 32 x 2048 of 128 in bf16, whose loads would crowd them, 411 to 432.
-    static constexpr bool kOwnQ = PI > 1 || kStages == 1;
+    // inputs in several parts.  Gradients of 32 x 1024 steps of 8 heads of 64 channels in fp16 152
+    // to 137 us, of 16 x 1024 of 128 in fp32 315 to 298; but of 32 x 2048 of 128 in bf16, whose
+    // loads would crowd them, 411 to 432.
+    static constexpr bool kOwnQ = PI > 1;
     // W waves for the state, half as many for memory and, but for STATES, as many for the
     // weights.  Twice as many of these where inputs have several parts, if a compute unit
     // holds one such workgroup: 16 x 1024 steps of 8 heads of 128 channels in fp32 152 to
@@ -417,9 +420,9 @@ template <int RUNS> __device__ __forceinline__ int output_at(int row, int run) {
 //   * W hold the state, 16 columns each: they multiply it by q, add what the tile's own
 //     steps give (weights times v), and bring the state over the tile; where q, k, v or the
 //     state holds an infinity or NaN they go step by step instead;
-//   * W / 2 load the tile after the next and unpack the next one;
-//   * W / 2 store the last tile's outputs and make the weights (q.k, decayed) of the next; of
-//     some forms they load and unpack q, too.
+//   * kHelpers (W / 2, or W) load the tile after the next and unpack the next one;
+//   * as many store the last tile's outputs and make the weights (q.k, decayed) of the next; of
+//     inputs in several parts they load and unpack q, too.
 // Two barriers a tile: ahead of the first, tile t's outputs are made, those of tile t - 1
 // leave and tile t + 1 is unpacked; ahead of the second, the state is brought over tile t
 // and the weights of tile t + 1 are made.  Loads go out on both sides of the first, since
@@ -1125,7 +1128,10 @@ HeadsOut heads_out(const wg_heads& t) { return {const_cast<void*>(t.data), t.str
 // A form of the kernel: the channels of q and k, and the waves that hold the state.  Eight
 // where v has more than 64 columns, so that q and k are read once and their weights made once:
 // 138 us instead of 254 for 256 heads of 2048 steps of 128 channels in bf16, 101 instead of
-// 118 with 64 of q and k.  In fp32 and for wider heads their tiles find no room in LDS.
+// 118 with 64 of q and k.  In fp32 and for wider heads it goes either way, and four are taken: of
+// 256 channels eight make 116 to 180 us of 64 heads of 1024 steps in fp16, 205 to 269 in fp32
+// and 100 to 109 in bf16, but 743 to 456 of 256 heads of 2048; in fp32 99 to 144 of 128 heads
+// of 2048 steps with 32 channels of q and k and 128 of v, but 203 to 180 with 128.
 struct Form {
     int kd, waves;
     bool operator==(const Form& o) const { return kd == o.kd && waves == o.waves; }
